@@ -28,8 +28,9 @@
  * Calls with no passage of the paper behind them are infrastructure: sizing
  * (ee_*_bytes), ee_create / ee_destroy, ee_seq_state, ee_use_graphs,
  * ee_last_error, the test aids (ee_get_logits, ee_read_kv, ee_load_kv,
- * ee_capture) and the measurement aids (ee_profile, ee_profile_read,
- * ee_time_gemm, ee_time_stream_read).  Every other call names the passage
+ * ee_capture), the measurement aids (ee_profile, ee_profile_read,
+ * ee_time_gemm, ee_time_stream_read) and the operators of sparse decoders
+ * (ee_linear, ee_moe_*).  Every other call names the passage
  * it implements.
  */
 #ifndef EE_H
@@ -443,6 +444,89 @@ int32_t ee_time_gemm(ee_ctx* ctx, uint32_t cls, int32_t rows, int32_t reps, doub
  * buffer is only read.  EE_EINVAL for a smaller or misaligned size, a null
  * buffer or output, or reps < 1. */
 int32_t ee_time_stream_read(ee_ctx* ctx, const void* dev_buf, size_t bytes, int32_t reps, double* us_per_pass);
+
+/* Stand-alone operators of sparse (mixture-of-experts) decoders.
+ *
+ * They need no context: device pointers, sizes and a hipStream_t, on the
+ * device that is current and owns the stream.  They are asynchronous on that
+ * stream, allocate nothing, keep nothing between calls and may be captured
+ * into a graph.  Arguments are checked before anything is launched (EE_EINVAL,
+ * EE_ECAPACITY for a small workspace, EE_EHIP for a failed launch; the message
+ * is ee_last_error(NULL)); zero rows are EE_OK.  Strides (ld*) count elements
+ * between rows.  Sums are fp32 (the routing float64) with one rounding at the
+ * end, and a row's result does not depend on the other rows of a call.
+ * Outputs must not overlap inputs, except that `y` / `out` may be exactly
+ * `residual` (same pointer, stride and type). */
+enum { EE_ACT_NONE = 0, EE_ACT_SILU = 1, EE_ACT_GELU = 2 /* erf */, EE_ACT_GELU_TANH = 3, EE_ACT_RELU = 4 };
+enum { EE_SCORE_SOFTMAX = 0, EE_SCORE_SIGMOID = 1 };
+
+/* y[t][n] = act(sum_k x[t][k] w[n][k] + bias[n]) + residual[t][n].
+ * rows <= 2^22; `in` a multiple of 32 (bf16) or 16 (f32); any `out` up to 2^20.
+ * x and w: 16-byte aligned, row strides multiples of 16 bytes.  out_dtype
+ * (of y and residual): dtype or EE_F32. */
+typedef struct {
+  const void* x;            /* [rows][ldx] dtype                              */
+  const void* w;            /* [out][ldw] dtype                               */
+  const float* bias;        /* [out] or NULL                                  */
+  const void* residual;     /* [rows][ldr] out_dtype or NULL                  */
+  void* y;                  /* [rows][ldy] out_dtype                          */
+  int64_t ldx, ldw, ldr, ldy;
+  int32_t rows, in, out;
+  int32_t dtype, out_dtype, act;
+} ee_linear_args;
+int32_t ee_linear(const ee_linear_args* args, void* hip_stream);
+
+/* Experts and weights of every row from the router's logits.
+ *   score = softmax over the row's experts, or the sigmoid of each
+ *   key   = score + bias (bias NULL: score); it decides, the weight is the score
+ * An expert whose logit is NaN or -inf, or whose bias is, is never selected
+ * (and takes no part in the softmax where its logit is); +inf counts as the
+ * largest finite float.  n_groups > 1: experts form n_groups runs of
+ * n_experts / n_groups; a group's score is the sum of its best group_top keys (1
+ * or 2; those there are), and only the best top_groups groups stay.  Then the
+ * top_k largest keys, in descending order; ties of keys and of groups go to
+ * the lower index.  weights = the scores, divided by their sum when
+ * renormalize != 0 (0 if the sum is 0), times scale.  Slots with no expert
+ * left hold id -1 and weight 0.  Everything is float64 up to the stored weight.
+ * n_experts <= 1024, top_k <= 32 and at most the experts of top_groups groups,
+ * n_groups <= 64 (a divisor of n_experts; 1: no groups). */
+typedef struct {
+  const void* logits;       /* [rows][ld] dtype                               */
+  const float* bias;        /* [n_experts] or NULL                            */
+  int32_t* ids;             /* [rows][top_k]                                  */
+  float* weights;           /* [rows][top_k]                                  */
+  int64_t ld;
+  int32_t rows, n_experts, top_k, dtype;
+  int32_t score, renormalize;
+  int32_t n_groups, top_groups, group_top;
+  float scale;
+} ee_moe_route_args;
+int32_t ee_moe_route(const ee_moe_route_args* args, void* hip_stream);
+
+/* out[t] = residual[t] + sum_j weights[t][j] * FFN_{ids[t][j]}(x[t]), slots in
+ * order, FFN_e(x) = (silu(x Wg_e^T) * (x Wu_e^T)) Wd_e^T with the product in
+ * parentheses rounded to dtype.  Slots whose id is outside [0, n_experts) are
+ * skipped (a row with none: its residual, or zeros).  d_model and ffn: multiples of 32 (bf16)
+ * or 16 (f32), at most 32768; rows * top_k <= 2^24.  workspace: at least
+ * ee_moe_ffn_workspace_bytes (0 for invalid sizes), 256-byte aligned, in use
+ * until the call's work is done; calls that may overlap need one each. */
+typedef struct {
+  const void* x;            /* [rows][ldx] dtype, 16-byte aligned rows        */
+  const void* w_gate_up;    /* [n_experts][2 ffn][d_model] dtype: gate, up    */
+  const void* w_down;       /* [n_experts][d_model][ffn] dtype                */
+  const int32_t* ids;       /* [rows][top_k]                                  */
+  const float* weights;     /* [rows][top_k]                                  */
+  const void* residual;     /* [rows][ldr] out_dtype or NULL                  */
+  void* out;                /* [rows][ldo] out_dtype                          */
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t ldx, ldr, ldo;
+  int32_t rows, n_experts, top_k, d_model, ffn;
+  int32_t dtype, out_dtype;
+} ee_moe_ffn_args;
+size_t ee_moe_ffn_workspace_bytes(int32_t rows, int32_t n_experts, int32_t top_k, int32_t d_model, int32_t ffn,
+                                  int32_t dtype);
+int32_t ee_moe_ffn(const ee_moe_ffn_args* args, void* hip_stream);
 
 /* Message for the last failed call on ctx (or the last failed context-free
  * call when ctx is NULL).  Never NULL; the pointer stays valid until the next

@@ -82,6 +82,37 @@ ee_time_stream_read = _sig("ee_time_stream_read", _i32, [_vp, _vp, _sz, _i32, ct
 ee_profile_read = _sig("ee_profile_read", _i32, [_vp, ctypes.POINTER(ctypes.c_double),
                                                  ctypes.POINTER(ctypes.c_int64), _i32])
 
+_i64 = ctypes.c_int64
+
+
+class EELinearArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("w", _vp), ("bias", _vp), ("residual", _vp), ("y", _vp),
+                ("ldx", _i64), ("ldw", _i64), ("ldr", _i64), ("ldy", _i64),
+                ("rows", _i32), ("in_", _i32), ("out", _i32), ("dtype", _i32), ("out_dtype", _i32), ("act", _i32)]
+
+
+class EEMoeRouteArgs(ctypes.Structure):
+    _fields_ = [("logits", _vp), ("bias", _vp), ("ids", _vp), ("weights", _vp), ("ld", _i64),
+                ("rows", _i32), ("n_experts", _i32), ("top_k", _i32), ("dtype", _i32),
+                ("score", _i32), ("renormalize", _i32), ("n_groups", _i32), ("top_groups", _i32), ("group_top", _i32),
+                ("scale", ctypes.c_float)]
+
+
+class EEMoeFfnArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("w_gate_up", _vp), ("w_down", _vp), ("ids", _vp), ("weights", _vp), ("residual", _vp),
+                ("out", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("ldx", _i64), ("ldr", _i64), ("ldo", _i64),
+                ("rows", _i32), ("n_experts", _i32), ("top_k", _i32), ("d_model", _i32), ("ffn", _i32),
+                ("dtype", _i32), ("out_dtype", _i32)]
+
+
+ee_linear = _sig("ee_linear", _i32, [ctypes.POINTER(EELinearArgs), _vp])
+ee_moe_route = _sig("ee_moe_route", _i32, [ctypes.POINTER(EEMoeRouteArgs), _vp])
+ee_moe_ffn = _sig("ee_moe_ffn", _i32, [ctypes.POINTER(EEMoeFfnArgs), _vp])
+ee_moe_ffn_workspace_bytes = _sig("ee_moe_ffn_workspace_bytes", _sz, [_i32] * 6)
+
+ACTIVATIONS = ("none", "silu", "gelu", "gelu_tanh", "relu")
+SCORES = ("softmax", "sigmoid")
+
 PROF_CLASSES = ("norm", "qkv", "attn", "combine", "oproj", "gateup", "down", "lmhead", "argmax",
                 "accept", "compact", "finish")
 
@@ -126,6 +157,148 @@ def make_config(shape, max_ctx: int, max_seqs: int = 1, k_max: int = 64) -> EEMo
                          shape.head_dim, shape.ffn, shape.vocab,
                          EE_BF16 if shape.dtype == "bf16" else EE_F32,
                          shape.rms_eps, shape.rope_theta, max_ctx, max_seqs, k_max, 64)
+
+
+# -- stand-alone operators ---------------------------------------------------
+#
+# Device tensors in, device tensors out, on the tensors' device and its current
+# stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given.
+
+_TYPES = {torch.float32: EE_F32, torch.bfloat16: EE_BF16}
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise EEError(EE_EINVAL, f"{what} must be float32 or bfloat16") from None
+
+
+def _matrix(t: torch.Tensor, what: str, shape, dtype, dev) -> torch.Tensor:
+    """Checks a [rows, cols] operand of unit column stride; returns it."""
+    if t.dim() != 2 or tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
+        raise EEError(EE_EINVAL, f"{what} must be {list(shape)} {dtype} on {dev}, "
+                                 f"not {list(t.shape)} {t.dtype} on {t.device}")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise EEError(EE_EINVAL, f"{what} must have unit column stride")
+    return t
+
+
+def _whole(t: torch.Tensor, what: str, shape, dtype, dev) -> torch.Tensor:
+    """Checks a contiguous operand; returns it."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev or not t.is_contiguous():
+        raise EEError(EE_EINVAL, f"{what} must be contiguous {list(shape)} {dtype} on {dev}")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    # (a single row may carry any stride)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _operator(fn, args, dev):
+    """Calls an operator on ``dev`` and its current stream."""
+    if dev.index == torch.cuda.current_device():
+        rc = fn(ctypes.byref(args), torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(ctypes.byref(args), torch.cuda.current_stream(dev).cuda_stream)
+    _check(rc)
+
+
+def _operand(x: torch.Tensor, what: str):
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.device.type != "cuda":
+        raise EEError(EE_EINVAL, f"{what} must be a two-dimensional tensor on a GPU")
+    return x.device
+
+
+def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtype=None):
+    """act(x w^T + bias) + residual (ee_linear).  x [rows, in] and w [out, in]
+    in float32 or bfloat16, bias [out] float32, residual [rows, out] in the
+    output's dtype (``out_dtype``: x's, or float32).  ``out`` may be the residual."""
+    dev = _operand(x, "x")
+    dt = _type(x, "x")
+    if act not in ACTIVATIONS:
+        raise EEError(EE_EINVAL, f"act must be one of {ACTIVATIONS}")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise EEError(EE_EINVAL, "w must be [out, in]")
+    rows, cols, n = x.shape[0], x.shape[1], w.shape[0]
+    _matrix(x, "x", (rows, cols), x.dtype, dev)
+    _matrix(w, "w", (n, cols), x.dtype, dev)
+    odt = out_dtype or (out.dtype if out is not None else x.dtype)
+    if out is None:
+        out = torch.empty((rows, n), dtype=odt, device=dev)
+    else:
+        _matrix(out, "out", (rows, n), odt, dev)
+    if bias is not None:
+        _whole(bias, "bias", (n,), torch.float32, dev)
+    if residual is not None:
+        _matrix(residual, "residual", (rows, n), odt, dev)
+    a = EELinearArgs(x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
+                     residual.data_ptr() if residual is not None else None, out.data_ptr(), _ld(x), _ld(w),
+                     _ld(residual) if residual is not None else 0, _ld(out), rows, cols, n, dt, _type(out, "out"),
+                     ACTIVATIONS.index(act))
+    _operator(ee_linear, a, dev)
+    return out
+
+
+def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize: bool = True, scale: float = 1.0,
+              n_groups: int = 1, top_groups: int = 1, group_top: int = 1):
+    """Experts and weights of every row of the router's logits [rows, experts]
+    (ee_moe_route): (ids int32, weights float32), both [rows, top_k]."""
+    dev = _operand(logits, "logits")
+    dt = _type(logits, "logits")
+    if score not in SCORES:
+        raise EEError(EE_EINVAL, f"score must be one of {SCORES}")
+    rows, n = logits.shape
+    _matrix(logits, "logits", (rows, n), logits.dtype, dev)
+    if bias is not None:
+        _whole(bias, "bias", (n,), torch.float32, dev)
+    k = int(top_k)
+    ids = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
+    weights = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
+    a = EEMoeRouteArgs(logits.data_ptr(), bias.data_ptr() if bias is not None else None, ids.data_ptr(),
+                       weights.data_ptr(), _ld(logits), rows, n, k, dt, SCORES.index(score), int(bool(renormalize)),
+                       int(n_groups), int(top_groups), int(group_top), float(scale))
+    _operator(ee_moe_route, a, dev)
+    return ids, weights
+
+
+def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dtype=None, workspace=None):
+    """residual + the weighted sum of the experts' SwiGLU products of every row
+    (ee_moe_ffn).  x [rows, d], w_gate_up [experts, 2 ffn, d] (gate rows, then
+    up rows) and w_down [experts, d, ffn] in float32 or bfloat16; ids int32 and
+    weights float32 [rows, top_k] as from ``moe_route``; residual and out
+    [rows, d] in ``out_dtype`` (x's, or float32).  ``workspace``: a uint8 tensor
+    of at least ee_moe_ffn_workspace_bytes, else one is allocated."""
+    dev = _operand(x, "x")
+    dt = _type(x, "x")
+    if not (isinstance(w_gate_up, torch.Tensor) and isinstance(w_down, torch.Tensor)
+            and w_gate_up.dim() == 3 and w_down.dim() == 3 and isinstance(ids, torch.Tensor) and ids.dim() == 2):
+        raise EEError(EE_EINVAL, "w_gate_up and w_down must be three-dimensional, ids [rows, top_k]")
+    (rows, d), (E, _, f), k = x.shape, w_down.shape, ids.shape[1]
+    _matrix(x, "x", (rows, d), x.dtype, dev)
+    _whole(w_gate_up, "w_gate_up", (E, 2 * f, d), x.dtype, dev)
+    _whole(w_down, "w_down", (E, d, f), x.dtype, dev)
+    _whole(ids, "ids", (rows, k), torch.int32, dev)
+    _whole(weights, "weights", (rows, k), torch.float32, dev)
+    odt = out_dtype or (out.dtype if out is not None else x.dtype)
+    if out is None:
+        out = torch.empty((rows, d), dtype=odt, device=dev)
+    else:
+        _matrix(out, "out", (rows, d), odt, dev)
+    if residual is not None:
+        _matrix(residual, "residual", (rows, d), odt, dev)
+    if workspace is None:
+        workspace = torch.empty(ee_moe_ffn_workspace_bytes(rows, E, k, d, f, dt), dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+        raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on {dev}")
+    a = EEMoeFfnArgs(x.data_ptr(), w_gate_up.data_ptr(), w_down.data_ptr(), ids.data_ptr(), weights.data_ptr(),
+                     residual.data_ptr() if residual is not None else None, out.data_ptr(), workspace.data_ptr(),
+                     workspace.numel(), _ld(x), _ld(residual) if residual is not None else 0, _ld(out),
+                     rows, E, k, d, f, dt, _type(out, "out"))
+    _operator(ee_moe_ffn, a, dev)
+    return out
 
 
 def match_reuse(generated, original, cursor: int, min_ngram: int = 1, max_ngram: int = 8):

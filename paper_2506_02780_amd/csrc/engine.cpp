@@ -17,6 +17,7 @@
 
 #include "../../include/ee.h"
 #include "kernels.h"
+#include "operators.h"
 
 namespace {
 
@@ -37,6 +38,16 @@ constexpr int MAX_DEVICES = 64;
 thread_local std::string g_err = "no error";
 
 }  // namespace
+
+namespace ee {
+int op_fail(int code, const char* msg) {
+  try {
+    g_err = msg;
+  } catch (...) {   // (no memory for the text: the code still tells)
+  }
+  return code;
+}
+}  // namespace ee
 
 static __device__ __align__(256) unsigned char scratch[NOALLOC_SCRATCH_BYTES];
 

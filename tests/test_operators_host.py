@@ -1,0 +1,115 @@
+"""Refusals of the stand-alone operators, without a GPU: every bad argument is
+reported before anything is launched, and zero rows are no work.  (The pointers
+are plausible numbers that nothing may follow.)"""
+
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2506_02780_amd", "libee.so")
+
+pytestmark = pytest.mark.skipif(not os.path.exists(LIB), reason="libee.so not built")
+
+P = 1 << 20   # an aligned address
+
+
+@pytest.fixture(scope="module")
+def ee():
+    import paper_2506_02780_amd as mod
+    return mod
+
+
+def _linear(ee, **kw):
+    d = dict(x=P, w=P, bias=P, residual=P, y=P, ldx=64, ldw=64, ldr=48, ldy=48, rows=0, in_=64, out=48,
+             dtype=ee.EE_BF16, out_dtype=ee.EE_BF16, act=0)
+    d.update(kw)
+    return ee.ee_linear(ctypes.byref(ee.EELinearArgs(**d)), None)
+
+
+def _route(ee, **kw):
+    d = dict(logits=P, bias=P, ids=P, weights=P, ld=64, rows=0, n_experts=64, top_k=8, dtype=ee.EE_F32, score=0,
+             renormalize=1, n_groups=1, top_groups=1, group_top=1, scale=1.0)
+    d.update(kw)
+    return ee.ee_moe_route(ctypes.byref(ee.EEMoeRouteArgs(**d)), None)
+
+
+def _ffn(ee, **kw):
+    d = dict(x=P, w_gate_up=P, w_down=P, ids=P, weights=P, residual=P, out=P, workspace=P, workspace_bytes=1 << 30,
+             ldx=64, ldr=64, ldo=64, rows=0, n_experts=8, top_k=2, d_model=64, ffn=32, dtype=ee.EE_BF16,
+             out_dtype=ee.EE_BF16)
+    d.update(kw)
+    return ee.ee_moe_ffn(ctypes.byref(ee.EEMoeFfnArgs(**d)), None)
+
+
+def test_zero_rows_are_no_work(ee):
+    assert _linear(ee) == _route(ee) == _ffn(ee) == ee.EE_OK
+    assert _linear(ee, x=None, w=None, y=None) == ee.EE_OK
+    assert ee.ee_linear(None, None) == ee.ee_moe_route(None, None) == ee.ee_moe_ffn(None, None) == ee.EE_EINVAL
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(rows=-1), "rows"), (dict(rows=(1 << 22) + 1), "rows"), (dict(in_=0), "in and out"), (dict(out=0), "in and out"),
+    (dict(out=(1 << 20) + 1), "in and out"), (dict(in_=48), "multiple of 32"), (dict(in_=24, dtype=0, out_dtype=0), "multiple of 32"),
+    (dict(dtype=2), "dtype"), (dict(dtype=0, out_dtype=1), "dtype"), (dict(out_dtype=-1), "dtype"),
+    (dict(act=5), "activation"), (dict(act=-1), "activation"),
+    (dict(x=None, rows=1), "non-NULL"), (dict(w=None, rows=1), "non-NULL"), (dict(y=None, rows=1), "non-NULL"),
+    (dict(x=P + 8, rows=1), "16-byte"), (dict(w=P + 2, rows=1), "16-byte"), (dict(ldx=63, rows=1), "16-byte"),
+    (dict(ldw=56, rows=1), "16-byte"), (dict(ldx=68, rows=1), "16-byte"), (dict(ldx=-64, rows=1), "16-byte"),
+    (dict(y=P + 1, rows=1), "y must"), (dict(ldy=47, rows=1), "y must"), (dict(ldr=47, rows=1), "residual"),
+    (dict(residual=P + 1, rows=1), "residual"), (dict(bias=P + 2, rows=1), "bias"),
+    (dict(rows=1 << 22, out=1 << 20, ldy=1 << 20, ldr=1 << 20), "tiles"),
+])
+def test_linear_refusals(ee, kw, word):
+    assert _linear(ee, **kw) == ee.EE_EINVAL and word in ee.ee_last_error(None).decode()
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(rows=-1), "rows"), (dict(n_experts=0), "n_experts"), (dict(n_experts=1025), "n_experts"),
+    (dict(top_k=0), "top_k"), (dict(top_k=33), "top_k"), (dict(n_experts=4, top_k=5), "top_k"), (dict(dtype=7), "dtype"),
+    (dict(score=2), "score"), (dict(n_groups=0), "n_groups"), (dict(n_groups=5), "n_groups"),
+    (dict(n_experts=260, n_groups=65), "n_groups"), (dict(n_groups=4, top_groups=5), "top_groups"),
+    (dict(top_groups=0), "top_groups"), (dict(n_groups=4, group_top=3), "group_top"), (dict(group_top=0), "group_top"),
+    (dict(n_groups=16, top_groups=1), "top_k exceeds"), (dict(scale=float("nan")), "scale"),
+    (dict(scale=float("inf")), "scale"), (dict(logits=None, rows=1), "non-NULL"), (dict(ids=None, rows=1), "non-NULL"),
+    (dict(weights=None, rows=1), "non-NULL"), (dict(logits=P + 2, rows=1), "logits"), (dict(ld=63, rows=1), "logits"),
+    (dict(ids=P + 2, rows=1), "aligned"), (dict(weights=P + 1, rows=1), "aligned"), (dict(bias=P + 2, rows=1), "aligned"),
+])
+def test_route_refusals(ee, kw, word):
+    assert _route(ee, **kw) == ee.EE_EINVAL and word in ee.ee_last_error(None).decode()
+
+
+@pytest.mark.parametrize("kw,word", [
+    (dict(rows=-1), "rows"), (dict(rows=1 << 24, top_k=2), "rows"), (dict(n_experts=0), "n_experts"),
+    (dict(n_experts=1025), "n_experts"), (dict(top_k=0), "top_k"), (dict(top_k=9), "top_k"),
+    (dict(n_experts=64, top_k=33), "top_k"), (dict(d_model=48), "multiples"), (dict(ffn=16), "multiples"),
+    (dict(ffn=0), "d_model"), (dict(d_model=32800), "d_model"), (dict(dtype=3), "dtype"),
+    (dict(dtype=0, out_dtype=1), "out_dtype"), (dict(x=None, rows=1), "non-NULL"), (dict(w_gate_up=None, rows=1), "non-NULL"),
+    (dict(w_down=None, rows=1), "non-NULL"), (dict(ids=None, rows=1), "non-NULL"), (dict(weights=None, rows=1), "non-NULL"),
+    (dict(out=None, rows=1), "non-NULL"), (dict(workspace=None, rows=1), "non-NULL"), (dict(x=P + 2, rows=1), "x must"),
+    (dict(ldx=65, rows=1), "x must"), (dict(ldx=56, rows=1), "x must"), (dict(w_gate_up=P + 2, rows=1), "w_gate_up"),
+    (dict(w_down=P + 8, rows=1), "w_down"), (dict(ids=P + 2, rows=1), "ids"), (dict(ldo=63, rows=1), "out must"),
+    (dict(out=P + 1, rows=1), "out must"), (dict(ldr=63, rows=1), "residual"), (dict(workspace=P + 128, rows=1), "workspace"),
+])
+def test_ffn_refusals(ee, kw, word):
+    assert _ffn(ee, **kw) == ee.EE_EINVAL and word in ee.ee_last_error(None).decode()
+
+
+def test_ffn_workspace(ee):
+    n = ee.ee_moe_ffn_workspace_bytes(100, 8, 2, 64, 32, ee.EE_BF16)
+    assert n >= 100 * 2 * 32 * 2
+    assert _ffn(ee, rows=100, workspace_bytes=n - 1) == ee.EE_ECAPACITY
+    assert ee.ee_moe_ffn_workspace_bytes(100, 8, 9, 64, 32, ee.EE_BF16) == 0
+    assert ee.ee_moe_ffn_workspace_bytes(100, 8, 2, 48, 32, ee.EE_BF16) == 0
+    assert ee.ee_moe_ffn_workspace_bytes(-1, 8, 2, 64, 32, ee.EE_BF16) == 0
+
+
+def test_python_refusals_without_a_gpu(ee):
+    import torch
+    x, w = torch.zeros(2, 64), torch.zeros(48, 64)
+    for call in (lambda: ee.linear(x, w), lambda: ee.moe_route(x, 4), lambda: ee.linear(None, w),
+                 lambda: ee.moe_ffn(x, w, w, None, None)):
+        with pytest.raises(ee.EEError) as e:
+            call()
+        assert e.value.code == ee.EE_EINVAL
