@@ -113,6 +113,38 @@ int32_t ee_create(const ee_model_config* cfg, const ee_weights* w, void* packed,
                   void* kv_pool, void* workspace, void* hip_stream, ee_ctx** out);
 int32_t ee_destroy(ee_ctx* ctx);
 
+/* Models with sparse layers: every layer's FFN is a bank of n_experts SwiGLU
+ * experts of cfg->ffn columns, top_k of which serve a row.  x = RMSNorm(h) *
+ * ffn_gain (rounded to dtype), logits = x router^T (fp32), ee_moe_route's
+ * selection and weights with these settings, h += ee_moe_ffn's weighted sum.
+ * All other calls take such a context as they take a dense one (ee_capture
+ * and ee_time_gemm of the FFN's projections excepted: EE_EINVAL), with the same
+ * guarantees: a row's arithmetic does not depend on the block it is in. */
+typedef struct {
+  int32_t n_experts, top_k;                     /* bounds as ee_moe_route      */
+  int32_t score, renormalize;                   /* EE_SCORE_*                  */
+  int32_t n_groups, top_groups, group_top;      /* 1, 1, 1: no groups          */
+  float scale;
+} ee_moe_config;
+
+/* Per-layer host arrays of n_layers device pointers, row-major in the model
+ * dtype; copied into the arena by ee_moe_create.  Of ee_weights, w_gate, w_up
+ * and w_down are not read (may be NULL). */
+typedef struct {
+  const void* const* router;                    /* [n_experts, d_model]        */
+  const float* const* router_bias;              /* [n_experts] fp32 each; the array or an entry may be NULL */
+  const void* const* w_gate_up;                 /* [n_experts, 2 ffn, d_model]: gate rows, then up rows */
+  const void* const* w_down;                    /* [n_experts, d_model, ffn]   */
+} ee_moe_weights;
+
+/* Sizes and creation as ee_packed_weight_bytes, ee_workspace_bytes and
+ * ee_create (ee_kv_pool_bytes is the dense model's). */
+size_t ee_moe_packed_weight_bytes(const ee_model_config* cfg, const ee_moe_config* moe);
+size_t ee_moe_workspace_bytes(const ee_model_config* cfg, const ee_moe_config* moe);
+int32_t ee_moe_create(const ee_model_config* cfg, const ee_moe_config* moe, const ee_weights* w,
+                      const ee_moe_weights* mw, void* packed, void* kv_pool, void* workspace, void* hip_stream,
+                      ee_ctx** out);
+
 /* Run the prompt tokens[0..n-1] of sequence `seq` (which must be empty),
  * commit all n positions to the KV cache (in blocks of up to
  * max(k_max + 1, 512) rows; results do not depend on the blocks, and
@@ -398,7 +430,7 @@ enum {
   EE_PROF_ATTN = 2,     /* split attention over the paged KV cache      */
   EE_PROF_COMBINE = 3,  /* merge of the attention splits                */
   EE_PROF_OPROJ = 4,    /* O-projection GEMM                            */
-  EE_PROF_GATEUP = 5,   /* gate/up GEMM                                 */
+  EE_PROF_GATEUP = 5,   /* gate/up GEMM; sparse layers: the experts     */
   EE_PROF_DOWN = 6,     /* down-projection GEMM                         */
   EE_PROF_LMHEAD = 7,   /* LM-head GEMM                                 */
   EE_PROF_ARGMAX = 8,   /* top-k selection / stochastic sums            */
@@ -406,7 +438,8 @@ enum {
                         /* or the stochastic acceptance and draw        */
   EE_PROF_COMPACT = 10, /* tree KV compaction                           */
   EE_PROF_FINISH = 11,  /* GEMM epilogues: rotary + KV append, SwiGLU,  */
-                        /* logits + per-chunk maxima                    */
+                        /* logits + per-chunk maxima; sparse layers:    */
+                        /* the router and the routing                   */
   EE_PROF_N = 12
 };
 

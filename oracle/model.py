@@ -40,6 +40,16 @@ kernel):
 Residual stream, scores, softmax and logits stay float64.  fp32 models are
 not rounded at all.
 
+Models with sparse layers (shape.n_experts > 0) have in the FFN's place
+
+      x = RMSNorm(h) * g_ffn                  (rounded as x_ffn)
+      l = x Wr^T                              the router's logits
+      s = softmax(l) or sigmoid(l); key = s + bias
+      the best top_groups of n_groups runs of experts, each with the sum of its
+      best group_top keys, then the top_k best keys (ties: lower index);
+      w = s of those, divided by their sum (renormalize), times route_scale
+      h = h + sum_j w_j (silu(x Wg_j^T) * (x Wu_j^T)) Wd_j^T   (z rounded)
+
 A norm followed by a projection, RMSNorm(h) * g W^T, is evaluated as
 r * ((h * g) W^T) with the row's scale r = 1 / sqrt(mean(h^2) + eps): the
 same value, with h * g as the quantity that is stored (and so rounded) before
@@ -126,6 +136,42 @@ def tree_structure(parent):
     return depth, vis
 
 
+def route(logits, shape, bias=None):
+    """[T, E] logits -> (ids [T, top_k], weights [T, top_k])."""
+    if shape.score == "softmax":
+        e = np.exp(logits - logits.max(axis=1, keepdims=True))
+        s = e / e.sum(axis=1, keepdims=True)
+    else:
+        s = 1.0 / (1.0 + np.exp(-logits))
+    key = s if bias is None else s + np.asarray(bias, dtype=np.float64)
+    t, E = key.shape
+    if shape.n_groups > 1:
+        g = key.reshape(t, shape.n_groups, -1)
+        value = np.sort(g, axis=2)[:, :, ::-1][:, :, :shape.group_top].sum(axis=2)
+        best = np.argsort(-value, axis=1, kind="stable")[:, :shape.top_groups]
+        keep = np.zeros(value.shape, dtype=bool)
+        np.put_along_axis(keep, best, True, axis=1)
+        key = np.where(keep[:, :, None], g, -np.inf).reshape(t, E)
+    ids = np.argsort(-key, axis=1, kind="stable")[:, :shape.top_k]
+    w = np.take_along_axis(s, ids, axis=1)
+    if shape.renormalize:
+        w = w / w.sum(axis=1, keepdims=True)
+    return ids, w * shape.route_scale
+
+
+def sparse_ffn(x, lw, shape, rnd):
+    """The experts' weighted sum for rows x [T, d]; rnd rounds the inner product z."""
+    dt, f = shape.dtype, shape.ffn
+    ids, w = route(x @ to_f64(lw["router"], dt).T, shape, lw.get("router_bias"))
+    out = np.zeros_like(x)
+    for e in np.unique(ids):
+        row, slot = np.nonzero(ids == e)
+        gu = x[row] @ to_f64(lw["w_gate_up"][e], dt).T
+        z = rnd(silu(gu[:, :f]) * gu[:, f:])
+        out[row] += w[row, slot][:, None] * (z @ to_f64(lw["w_down"][e], dt).T)
+    return out
+
+
 ROUNDING_SITES = ("x_attn", "q", "k", "v", "o", "x_ffn", "z", "x_final")
 
 
@@ -184,6 +230,10 @@ def forward_block(shape, weights, cache, tokens, depth, vis, rounding=None):
         vals = np.concatenate([vc, v], axis=0)
         o = rnd("o", l, attention(q, keys, vals, mask, scale).reshape(t, H * hd))
         h = h + o @ to_f64(lw["wo"], dt).T
+        if getattr(shape, "n_experts", 0):
+            x = rnd("x_ffn", l, rmsnorm(h, lw["ffn_gain"].astype(np.float64), shape.rms_eps))
+            h = h + sparse_ffn(x, lw, shape, lambda z: rnd("z", l, z))
+            continue
         x = rnd("x_ffn", l, h * lw["ffn_gain"].astype(np.float64))
         r = norm_scale(h, shape.rms_eps)
         z = rnd("z", l, silu((x @ to_f64(lw["w_gate"], dt).T) * r) * ((x @ to_f64(lw["w_up"], dt).T) * r))

@@ -45,6 +45,15 @@ class EEWeights(ctypes.Structure):
                 ("attn_gain", ctypes.POINTER(_vp)), ("ffn_gain", ctypes.POINTER(_vp))]
 
 
+class EEMoeConfig(ctypes.Structure):
+    _fields_ = [("n_experts", _i32), ("top_k", _i32), ("score", _i32), ("renormalize", _i32), ("n_groups", _i32),
+                ("top_groups", _i32), ("group_top", _i32), ("scale", ctypes.c_float)]
+
+
+class EEMoeWeights(ctypes.Structure):
+    _fields_ = [(n, ctypes.POINTER(_vp)) for n in ("router", "router_bias", "w_gate_up", "w_down")]
+
+
 def _sig(name, res, args):
     f = getattr(_lib, name)
     f.restype, f.argtypes = res, args
@@ -56,6 +65,12 @@ ee_kv_pool_bytes = _sig("ee_kv_pool_bytes", _sz, [ctypes.POINTER(EEModelConfig)]
 ee_workspace_bytes = _sig("ee_workspace_bytes", _sz, [ctypes.POINTER(EEModelConfig)])
 ee_create = _sig("ee_create", _i32, [ctypes.POINTER(EEModelConfig), ctypes.POINTER(EEWeights),
                                      _vp, _vp, _vp, _vp, ctypes.POINTER(_vp)])
+ee_moe_packed_weight_bytes = _sig("ee_moe_packed_weight_bytes", _sz,
+                                  [ctypes.POINTER(EEModelConfig), ctypes.POINTER(EEMoeConfig)])
+ee_moe_workspace_bytes = _sig("ee_moe_workspace_bytes", _sz, [ctypes.POINTER(EEModelConfig), ctypes.POINTER(EEMoeConfig)])
+ee_moe_create = _sig("ee_moe_create", _i32, [ctypes.POINTER(EEModelConfig), ctypes.POINTER(EEMoeConfig),
+                                             ctypes.POINTER(EEWeights), ctypes.POINTER(EEMoeWeights),
+                                             _vp, _vp, _vp, _vp, ctypes.POINTER(_vp)])
 ee_destroy = _sig("ee_destroy", _i32, [_vp])
 ee_prefill = _sig("ee_prefill", _i32, [_vp, _i32, _pi32, _i32, _pi32])
 ee_verify = _sig("ee_verify", _i32, [_vp, _i32, _pi32, _i32, _pi32, _pi32, _pi32, _pi32])
@@ -157,6 +172,12 @@ def make_config(shape, max_ctx: int, max_seqs: int = 1, k_max: int = 64) -> EEMo
                          shape.head_dim, shape.ffn, shape.vocab,
                          EE_BF16 if shape.dtype == "bf16" else EE_F32,
                          shape.rms_eps, shape.rope_theta, max_ctx, max_seqs, k_max, 64)
+
+
+def make_moe_config(shape) -> EEMoeConfig:
+    """The routing of a shape with sparse layers."""
+    return EEMoeConfig(shape.n_experts, shape.top_k, SCORES.index(shape.score), int(shape.renormalize),
+                       shape.n_groups, shape.top_groups, shape.group_top, shape.route_scale)
 
 
 # -- stand-alone operators ---------------------------------------------------
@@ -324,7 +345,9 @@ class Engine:
 
     ``weights`` provides numpy arrays in the model dtype (``embed``,
     ``lm_head``, ``final_gain``, ``layer(l)`` mapping), as drawn by
-    ``workloads.gen_weights``.
+    ``workloads.gen_weights``.  A shape with ``n_experts`` has sparse layers
+    (ee_moe_create): its layers map router, w_gate_up, w_down and, optionally,
+    router_bias.
     """
 
     def __init__(self, shape, weights, max_ctx: int, max_seqs: int = 1, k_max: int = 64,
@@ -334,7 +357,10 @@ class Engine:
         self.shape, self.device = shape, torch.device(device)
         self.cfg = make_config(shape, max_ctx, max_seqs, k_max)
         cfgp = ctypes.byref(self.cfg)
+        moe = make_moe_config(shape) if getattr(shape, "n_experts", 0) else None
         nb_packed, nb_kv, nb_ws = ee_packed_weight_bytes(cfgp), ee_kv_pool_bytes(cfgp), ee_workspace_bytes(cfgp)
+        if moe is not None:
+            nb_packed, nb_ws = (f(cfgp, ctypes.byref(moe)) for f in (ee_moe_packed_weight_bytes, ee_moe_workspace_bytes))
         if not (nb_packed and nb_kv and nb_ws):
             raise EEError(EE_EINVAL, "invalid model config for the library")
         with torch.cuda.device(self.device):
@@ -351,19 +377,26 @@ class Engine:
 
             L = shape.n_layers
             arr = lambda: (_vp * L)()
-            ptrs = {k: arr() for k in ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down",
-                                       "attn_gain", "ffn_gain")}
+            names = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "attn_gain", "ffn_gain")
+            sparse = ("router", "router_bias", "w_gate_up", "w_down") if moe is not None else ()
+            own = [k for k in names if not sparse or not k.startswith("w_")]   # (sparse layers: no dense FFN)
+            ptrs = {k: arr() for k in (*own, *sparse)}
             for l in range(L):
                 lw = weights.layer(l)
                 for k in ptrs:
-                    ptrs[k][l] = dev(lw[k])
+                    ptrs[k][l] = dev(lw[k]) if k != "router_bias" or k in lw else None
+            cast = lambda k: ctypes.cast(ptrs[k], ctypes.POINTER(_vp)) if k in ptrs else None
             w = EEWeights(dev(weights.embed), dev(weights.lm_head), dev(weights.final_gain),
-                          *[ctypes.cast(ptrs[k], ctypes.POINTER(_vp)) for k in
-                            ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down", "attn_gain", "ffn_gain")])
+                          *[cast(k) if k in own else None for k in names])
             torch.cuda.synchronize(self.device)
             ctx = _vp()
-            _check(ee_create(cfgp, ctypes.byref(w), self.packed.data_ptr(), self.kv_pool.data_ptr(),
-                             self.workspace.data_ptr(), self.stream.cuda_stream, ctypes.byref(ctx)))
+            buffers = (self.packed.data_ptr(), self.kv_pool.data_ptr(), self.workspace.data_ptr(),
+                       self.stream.cuda_stream, ctypes.byref(ctx))
+            if moe is None:
+                _check(ee_create(cfgp, ctypes.byref(w), *buffers))
+            else:
+                mw = EEMoeWeights(*[cast(k) for k in sparse])
+                _check(ee_moe_create(cfgp, ctypes.byref(moe), ctypes.byref(w), ctypes.byref(mw), *buffers))
             self.ctx = ctx
             del keep
         self._last_rows = 0

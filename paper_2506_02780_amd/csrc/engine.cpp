@@ -82,10 +82,11 @@ struct Seq {
 // Byte offsets of every buffer inside the three caller allocations.
 struct Layout {
   int Tmax, Rmax, Pmax, MT, G, max_splits, pages_per_seq, ptable_len, n_pages;
-  // packed arena
-  size_t embed, lm_head, final_gain, layers0, per_layer, l_wqkv, l_wo, l_wgu, l_wd, l_again, l_fgain,
-      packed_total;
+  // packed arena (sparse layers: router, its bias and the experts instead of wgu and wd)
+  size_t embed, lm_head, final_gain, layers0, per_layer, l_wqkv, l_wo, l_wgu, l_wd, l_again, l_fgain, l_router,
+      l_rbias, packed_total;
   // workspace
+  size_t mx, mlogits, mids, mweights, mws;   // sparse layers
   size_t h, ssq, xbuf, x2buf, ssqt, zbuf, q, part, gpart, logits, amax, greedy, verdict, rowstat, result, stage, rope, ws_total;
   // staging sub-offsets (relative to `stage`)
   size_t s_tok, s_pos, s_prow, s_slot, s_path, s_ptable, s_info, s_eps, s_unif, s_sparam, stage_bytes;
@@ -170,7 +171,8 @@ int prompt_rows(const ee_model_config& g) {
   return Tmax;
 }
 
-Layout make_layout(const ee_model_config* c) {
+// `moe`: the routing of a model with sparse layers, else null.
+Layout make_layout(const ee_model_config* c, const ee_moe_config* moe = nullptr) {
   Layout L{};
   const size_t esz = c->dtype == EE_BF16 ? 2 : 4;
   const int ks = c->dtype == EE_BF16 ? 32 : 16;
@@ -195,11 +197,15 @@ Layout make_layout(const ee_model_config* c) {
   L.l_wqkv = 0;
   size_t lo = 0;
   lo += up((H + 2 * Hkv) * hd * d * esz); L.l_wo = lo;
+  const size_t E = moe ? moe->n_experts : 1;
   lo += up(d * H * hd * esz); L.l_wgu = lo;
-  lo += up(2 * F * d * esz); L.l_wd = lo;
-  lo += up(d * F * esz); L.l_again = lo;
+  lo += up(E * 2 * F * d * esz); L.l_wd = lo;
+  lo += up(E * d * F * esz); L.l_again = lo;
   lo += up(d * 4); L.l_fgain = lo;
-  lo += up(d * 4);
+  lo += up(d * 4); L.l_router = lo;
+  if (moe) lo += up(E * d * esz);
+  L.l_rbias = lo;
+  if (moe) lo += up(E * 4);
   L.per_layer = lo;
   L.packed_total = o + lo * c->n_layers;
   // workspace
@@ -211,7 +217,8 @@ Layout make_layout(const ee_model_config* c) {
   L.xbuf = o; o += up(Tpad * xcols * esz);
   L.x2buf = o; o += up(Tpad * d * esz);
   L.ssqt = o; o += up(Rall * (d / 16) * 4);
-  L.zbuf = o; o += up(Tpad * F * esz);
+  L.zbuf = o;
+  if (!moe) o += up(Tpad * F * esz);
   L.q = o; o += up(Rall * H * hd * esz);
   // attention split states, and the split-K partials of the largest GEMM,
   // [slices][rows][N] (the LM head of a prompt block: its last rows from the
@@ -252,12 +259,37 @@ Layout make_layout(const ee_model_config* c) {
   L.stage_bytes = up(so);
   L.stage = o; o += L.stage_bytes;
   L.rope = o; o += up((size_t)c->max_ctx * (hd / 2) * 8);
+  if (moe) {
+    L.mx = o; o += up(Rall * d * esz);
+    L.mlogits = o; o += up(Rall * E * 4);
+    L.mids = o; o += up(Rall * moe->top_k * 4);
+    L.mweights = o; o += up(Rall * moe->top_k * 4);
+    L.mws = o; o += ee::ffn_workspace((int)Rall, moe->n_experts, moe->top_k, (int)d, (int)F, c->dtype == EE_BF16 ? ee::DT_BF16 : ee::DT_F32);
+  }
   L.ws_total = o;
   (void)ks;
   // KV pool: [layer][page][2][Hkv][64 * hd]
   L.kv_layer = (size_t)L.n_pages * 2 * Hkv * PAGE * hd * esz;
   L.kv_total = L.kv_layer * c->n_layers;
   return L;
+}
+
+// Whether the routing of a model with sparse layers is valid for the operators.
+bool valid_moe(const ee_model_config* c, const ee_moe_config* q, std::string* why) {
+  auto bad = [&](const char* m) { if (why) *why = m; return false; };
+  if (!valid_cfg(c, why)) return false;
+  if (!q) return bad("the routing config is NULL");
+  if (q->n_experts < 1 || q->n_experts > ee::ROUTE_MAX_E) return bad("n_experts must be in [1, 1024]");
+  if (q->top_k < 1 || q->top_k > ee::ROUTE_MAX_K || q->top_k > q->n_experts) return bad("top_k must be in [1, min(32, n_experts)]");
+  if (q->score < 0 || q->score >= ee::SCORE_N) return bad("unknown score function");
+  if (q->n_groups < 1 || q->n_groups > 64 || q->n_experts % q->n_groups) return bad("n_groups must be in [1, 64] and divide n_experts");
+  if (q->top_groups < 1 || q->top_groups > q->n_groups) return bad("top_groups must be in [1, n_groups]");
+  if (q->group_top < 1 || q->group_top > 2) return bad("group_top must be 1 or 2");
+  if (q->top_k > q->n_experts / q->n_groups * q->top_groups) return bad("top_k exceeds the experts of top_groups groups");
+  if (!isfinite(q->scale)) return bad("scale must be finite");
+  const size_t rows = std::max<size_t>((size_t)(c->k_max + 1) * c->max_seqs, prompt_rows(*c));
+  if (rows * q->top_k > (size_t(1) << 24)) return bad("max_seqs * (k_max + 1) * top_k must be at most 2^24");
+  return true;
 }
 
 }  // namespace
@@ -330,6 +362,11 @@ void bind_work(ee_ctx* c) {
   w.ssqt = reinterpret_cast<float*>(ws + L.ssqt);
   w.zbuf = reinterpret_cast<uint4*>(ws + L.zbuf);
   w.q = ws + L.q;
+  w.mx = ws + L.mx;
+  w.mlogits = reinterpret_cast<float*>(ws + L.mlogits);
+  w.mids = reinterpret_cast<int*>(ws + L.mids);
+  w.mweights = reinterpret_cast<float*>(ws + L.mweights);
+  w.mws = ws + L.mws;
   w.attn_part = reinterpret_cast<float*>(ws + L.part);
   w.part = reinterpret_cast<float*>(ws + L.gpart);
   w.logits = reinterpret_cast<float*>(ws + L.logits);
@@ -713,27 +750,27 @@ size_t ee_workspace_bytes(const ee_model_config* cfg) {
   return make_layout(cfg).ws_total;
 }
 
-int32_t ee_create(const ee_model_config* cfg, const ee_weights* wts, void* packed, void* kv_pool,
-                  void* workspace, void* hip_stream, ee_ctx** out) {
-  std::string why;
-  if (!out) return fail(nullptr, EE_EINVAL, "out is NULL");
-  *out = nullptr;
-  if (!valid_cfg(cfg, &why)) return fail(nullptr, EE_EINVAL, why);
+// ee_create, and (moe, mw non-null) ee_moe_create.
+static int32_t create(const ee_model_config* cfg, const ee_moe_config* moe, const ee_weights* wts,
+                      const ee_moe_weights* mw, void* packed, void* kv_pool, void* workspace, void* hip_stream,
+                      ee_ctx** out) {
   if (!wts || !packed || !kv_pool || !workspace)
     return fail(nullptr, EE_EINVAL, "weights, packed arena, KV pool and workspace must be non-NULL");
   const int nl = cfg->n_layers;
   if (!wts->embed || !wts->lm_head || !wts->final_gain || !wts->wq || !wts->wk || !wts->wv ||
-      !wts->wo || !wts->w_gate || !wts->w_up || !wts->w_down || !wts->attn_gain || !wts->ffn_gain)
+      !wts->wo || !wts->attn_gain || !wts->ffn_gain ||
+      (moe ? !mw->router || !mw->w_gate_up || !mw->w_down : !wts->w_gate || !wts->w_up || !wts->w_down))
     return fail(nullptr, EE_EINVAL, "a weight pointer is NULL");
   for (int l = 0; l < nl; ++l)
-    if (!wts->wq[l] || !wts->wk[l] || !wts->wv[l] || !wts->wo[l] || !wts->w_gate[l] ||
-        !wts->w_up[l] || !wts->w_down[l] || !wts->attn_gain[l] || !wts->ffn_gain[l])
+    if (!wts->wq[l] || !wts->wk[l] || !wts->wv[l] || !wts->wo[l] || !wts->attn_gain[l] || !wts->ffn_gain[l] ||
+        (moe ? !mw->router[l] || !mw->w_gate_up[l] || !mw->w_down[l]
+             : !wts->w_gate[l] || !wts->w_up[l] || !wts->w_down[l]))
       return fail(nullptr, EE_EINVAL, "a per-layer weight pointer is NULL");
 
   ee_ctx* c = new (std::nothrow) ee_ctx();
   if (!c) return fail(nullptr, EE_EINVAL, "out of host memory");
   c->cfg = *cfg;
-  c->lay = make_layout(cfg);
+  c->lay = make_layout(cfg, moe);
   c->user_st = reinterpret_cast<hipStream_t>(hip_stream);
   c->st = c->user_st;   // packing runs on the caller's stream
   c->packed = reinterpret_cast<unsigned char*>(packed);
@@ -795,17 +832,32 @@ int32_t ee_create(const ee_model_config* cfg, const ee_weights* wts, void* packe
     ee::LayerPtrs& lp = c->layers[l];
     lp.wqkv = reinterpret_cast<const uint4*>(lb + L.l_wqkv);
     lp.wo = reinterpret_cast<const uint4*>(lb + L.l_wo);
-    lp.wgu = reinterpret_cast<const uint4*>(lb + L.l_wgu);
-    lp.wd = reinterpret_cast<const uint4*>(lb + L.l_wd);
+    if (moe) {
+      lp.router = lb + L.l_router;
+      lp.router_bias = mw->router_bias && mw->router_bias[l] ? reinterpret_cast<const float*>(lb + L.l_rbias) : nullptr;
+      lp.x_wgu = lb + L.l_wgu;
+      lp.x_wd = lb + L.l_wd;
+    } else {
+      lp.wgu = reinterpret_cast<const uint4*>(lb + L.l_wgu);
+      lp.wd = reinterpret_cast<const uint4*>(lb + L.l_wd);
+    }
     lp.attn_gain = reinterpret_cast<const float*>(lb + L.l_again);
     lp.ffn_gain = reinterpret_cast<const float*>(lb + L.l_fgain);
     const ee::PackSrc parts[] = {
         {wts->wq[l], H * hd, 0}, {wts->wk[l], Hkv * hd, H * hd}, {wts->wv[l], Hkv * hd, (H + Hkv) * hd}};
     for (const auto& p : parts) ok = ok && run(ee::launch_pack(p, lb + L.l_wqkv, d, dt, c->st), "pack wqkv");
     ok = ok && run(ee::launch_pack({wts->wo[l], d, 0}, lb + L.l_wo, H * hd, dt, c->st), "pack wo");
-    ok = ok && run(ee::launch_pack({wts->w_gate[l], F, 0}, lb + L.l_wgu, d, dt, c->st), "pack w_gate");
-    ok = ok && run(ee::launch_pack({wts->w_up[l], F, F}, lb + L.l_wgu, d, dt, c->st), "pack w_up");
-    ok = ok && run(ee::launch_pack({wts->w_down[l], d, 0}, lb + L.l_wd, F, dt, c->st), "pack w_down");
+    if (moe) {   // (the operators read rows as they are)
+      const size_t E = moe->n_experts, bank = E * F * d * esz;
+      ok = ok && run(ee::launch_copy(mw->router[l], lb + L.l_router, E * d * esz, c->st), "copy router");
+      if (lp.router_bias) ok = ok && run(ee::launch_copy(mw->router_bias[l], lb + L.l_rbias, E * 4, c->st), "copy router bias");
+      ok = ok && run(ee::launch_copy(mw->w_gate_up[l], lb + L.l_wgu, 2 * bank, c->st), "copy w_gate_up") &&
+           run(ee::launch_copy(mw->w_down[l], lb + L.l_wd, bank, c->st), "copy w_down");
+    } else {
+      ok = ok && run(ee::launch_pack({wts->w_gate[l], F, 0}, lb + L.l_wgu, d, dt, c->st), "pack w_gate");
+      ok = ok && run(ee::launch_pack({wts->w_up[l], F, F}, lb + L.l_wgu, d, dt, c->st), "pack w_up");
+      ok = ok && run(ee::launch_pack({wts->w_down[l], d, 0}, lb + L.l_wd, F, dt, c->st), "pack w_down");
+    }
     ok = ok && run(ee::launch_copy(wts->attn_gain[l], lb + L.l_again, (size_t)d * 4, c->st), "copy gain") &&
          run(ee::launch_copy(wts->ffn_gain[l], lb + L.l_fgain, (size_t)d * 4, c->st), "copy gain");
   }
@@ -834,6 +886,11 @@ int32_t ee_create(const ee_model_config* cfg, const ee_weights* wts, void* packe
   ee::Model& m = c->m;
   m.L = nl; m.d = d; m.H = H; m.Hkv = Hkv; m.hd = hd; m.F = F; m.V = cfg->vocab; m.dt = dt;
   m.eps = cfg->rms_eps; m.max_ctx = cfg->max_ctx; m.max_pages = L.n_pages;
+  if (moe) {
+    m.moe.E = moe->n_experts; m.moe.k = moe->top_k; m.moe.score = moe->score; m.moe.renorm = moe->renormalize != 0;
+    m.moe.groups = moe->n_groups; m.moe.top_groups = moe->top_groups; m.moe.group_top = moe->group_top;
+    m.moe.scale = moe->scale;
+  }
   m.embed = c->packed + L.embed;
   m.lm_head = reinterpret_cast<const uint4*>(c->packed + L.lm_head);
   m.final_gain = reinterpret_cast<const float*>(c->packed + L.final_gain);
@@ -846,6 +903,34 @@ int32_t ee_create(const ee_model_config* cfg, const ee_weights* wts, void* packe
   for (int p = L.n_pages - 1; p >= 0; --p) c->free_pages.push_back(p);
   *out = c;
   return EE_OK;
+}
+
+int32_t ee_create(const ee_model_config* cfg, const ee_weights* wts, void* packed, void* kv_pool,
+                  void* workspace, void* hip_stream, ee_ctx** out) {
+  std::string why;
+  if (!out) return fail(nullptr, EE_EINVAL, "out is NULL");
+  *out = nullptr;
+  if (!valid_cfg(cfg, &why)) return fail(nullptr, EE_EINVAL, why);
+  return create(cfg, nullptr, wts, nullptr, packed, kv_pool, workspace, hip_stream, out);
+}
+
+size_t ee_moe_packed_weight_bytes(const ee_model_config* cfg, const ee_moe_config* moe) {
+  return valid_moe(cfg, moe, nullptr) ? make_layout(cfg, moe).packed_total : 0;
+}
+
+size_t ee_moe_workspace_bytes(const ee_model_config* cfg, const ee_moe_config* moe) {
+  return valid_moe(cfg, moe, nullptr) ? make_layout(cfg, moe).ws_total : 0;
+}
+
+int32_t ee_moe_create(const ee_model_config* cfg, const ee_moe_config* moe, const ee_weights* wts,
+                      const ee_moe_weights* mw, void* packed, void* kv_pool, void* workspace, void* hip_stream,
+                      ee_ctx** out) {
+  std::string why;
+  if (!out) return fail(nullptr, EE_EINVAL, "out is NULL");
+  *out = nullptr;
+  if (!valid_moe(cfg, moe, &why)) return fail(nullptr, EE_EINVAL, why);
+  if (!mw) return fail(nullptr, EE_EINVAL, "the sparse layers' weights are NULL");
+  return create(cfg, moe, wts, mw, packed, kv_pool, workspace, hip_stream, out);
 }
 
 int32_t ee_destroy(ee_ctx* c) {
@@ -1166,6 +1251,7 @@ size_t ee_capture_bytes(const ee_model_config* cfg, int32_t rows) {
 int32_t ee_capture(ee_ctx* c, void* dev_buf, size_t bytes) {
   if (!c) return fail(nullptr, EE_EINVAL, "context is NULL");
   if (dev_buf && bytes == 0) return fail(c, EE_EINVAL, "a capture buffer needs a size");
+  if (dev_buf && c->m.moe.E) return fail(c, EE_EINVAL, "rounding sites are recorded for dense models only");
   c->cap = reinterpret_cast<unsigned char*>(dev_buf);
   c->cap_bytes = dev_buf ? bytes : 0;
   return EE_OK;
@@ -1216,6 +1302,8 @@ int32_t ee_time_gemm(ee_ctx* c, uint32_t cls, int32_t rows, int32_t reps, double
   if (cls != EE_PROF_QKV && cls != EE_PROF_OPROJ && cls != EE_PROF_GATEUP && cls != EE_PROF_DOWN &&
       cls != EE_PROF_LMHEAD)
     return fail(c, EE_EINVAL, "class must be one of the four projections or the LM head");
+  if (c->m.moe.E && (cls == EE_PROF_GATEUP || cls == EE_PROF_DOWN))
+    return fail(c, EE_EINVAL, "a sparse model has no gate/up or down projection of its own");
   if (rows < 1 || rows > c->lay.Rmax) return fail(c, EE_EINVAL, "rows outside [1, max_seqs * (k_max + 1)]");
   hipEvent_t e0 = nullptr, e1 = nullptr;
   HIP_TRY(c, hipEventCreate(&e0));

@@ -36,6 +36,12 @@ int gemm_slices_for(int K, int dt);
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, hipStream_t st);
 
 struct LayerPtrs {
+  // sparse layers (wgu and wd null): the router [E, d], its bias or null, and
+  // the experts [E, 2F, d] and [E, d, F], all row-major in the model dtype
+  const void* router;
+  const float* router_bias;
+  const void* x_wgu;
+  const void* x_wd;
   const uint4* wqkv;   // packed [(H + 2 Hkv) * hd, d]: q rows, k rows, v rows
   const uint4* wo;     // packed [d, H * hd]
   const uint4* wgu;    // packed [2F, d]: gate rows, then up rows
@@ -44,8 +50,16 @@ struct LayerPtrs {
   const float* ffn_gain;
 };
 
+// Routing of sparse layers (ee_moe_config).
+struct Moe {
+  int E = 0, k = 0;         // experts (0: dense layers) and experts per row
+  int score = 0, renorm = 0, groups = 1, top_groups = 1, group_top = 1;
+  float scale = 1.f;
+};
+
 struct Model {
   int L, d, H, Hkv, hd, F, V, dt;
+  Moe moe;
   float eps;
   int max_ctx, max_pages;   // pages per layer in the pool
   const void* embed;        // [V, d] row-major, model dtype
@@ -71,6 +85,13 @@ struct Work {
   float* ssqt;              // [Rmax, d / 16] sums of h^2 per 16-column tile (that norm's row scales)
   uint4* zbuf;              // packed activations, F columns
   void* q;                  // [Rmax, H, hd] model dtype
+  // sparse layers: the normed rows [Rmax, d], the router's logits [Rmax, E],
+  // the rows' experts and weights [Rmax, k], and run_ffn's workspace
+  void* mx;
+  float* mlogits;
+  int* mids;
+  float* mweights;
+  unsigned char* mws;
   float* attn_part;         // [splits][Hkv][Rmax*G][hd + 2]
   float* part;              // GEMM slice partials [SK][R][N]
   float* logits;            // [Rmax, V]

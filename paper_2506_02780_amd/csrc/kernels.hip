@@ -23,6 +23,7 @@
 
 #include "device.h"
 #include "kernels.h"
+#include "operators.h"
 
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -3299,6 +3300,76 @@ size_t capture_bytes(int L, int d, int qdim, int kvdim, int F, int dt, int R) {
   return layer * L + esz * R16 * d;
 }
 
+// x[t] = RMSNorm(h[t]) * gain, rounded to the model dtype, in rows: the input of
+// a sparse layer's router and experts.  One workgroup per row, whose sums run
+// in a fixed order.  (The dense layers' norms keep h * gain and the row's scale
+// apart; here the scale has to be in the row, since the router's scores are not
+// linear in it.)
+constexpr int MOE_NORM_THREADS = 256;
+template <int DT>
+__global__ __launch_bounds__(MOE_NORM_THREADS) void moe_norm_kernel(const float* __restrict__ h,
+                                                                    const float* __restrict__ gain, int d, float eps,
+                                                                    void* __restrict__ x) {
+  const int t = blockIdx.x, i0 = threadIdx.x * 4;
+  const float* row = h + (size_t)t * d;
+  __shared__ float part[MOE_NORM_THREADS / 64];
+  float s = 0.f;
+  for (int i = i0; i < d; i += MOE_NORM_THREADS * 4) {
+    const float4 v = *reinterpret_cast<const float4*>(row + i);
+    s += v.x * v.x + v.y * v.y + v.z * v.z + v.w * v.w;
+  }
+  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = part[0];
+#pragma unroll
+  for (int i = 1; i < MOE_NORM_THREADS / 64; ++i) s += part[i];
+  const float r = 1.0f / sqrtf(s / (float)d + eps);
+  for (int i = i0; i < d; i += MOE_NORM_THREADS * 4) {
+    const float4 v = *reinterpret_cast<const float4*>(row + i), g = *reinterpret_cast<const float4*>(gain + i);
+    const size_t o = (size_t)t * d + i;
+    store_elt<DT>(x, o, v.x * r * g.x);
+    store_elt<DT>(x, o + 1, v.y * r * g.y);
+    store_elt<DT>(x, o + 2, v.z * r * g.z);
+    store_elt<DT>(x, o + 3, v.w * r * g.w);
+  }
+}
+
+// The sparse FFN of R rows: norm, router, routing and the experts' weighted sum,
+// left in w.part as one fp32 slice [R][d] for the residual update that follows.
+template <int DT>
+static hipError_t moe_ffn(const Model& m, const Work& w, const LayerPtrs& lp, int R, Prof* prof, hipStream_t st) {
+  const int d = m.d;
+  hipError_t e;
+  if ((e = timed(prof, PC_NORM, st, [&] {
+         hipLaunchKernelGGL((moe_norm_kernel<DT>), dim3(R), dim3(MOE_NORM_THREADS), 0, st, w.h, lp.ffn_gain, d, m.eps, w.mx);
+         return hipGetLastError();
+       })) != hipSuccess)
+    return e;
+  if ((e = timed(prof, PC_FINISH, st, [&] {
+         LinearArgs la{};
+         la.x = w.mx; la.w = lp.router; la.y = w.mlogits;
+         la.ldx = la.ldw = d; la.ldy = m.moe.E;
+         la.T = R; la.K = d; la.N = m.moe.E; la.dt = DT; la.odt = DT_F32;
+         const hipError_t le = run_linear(la, st);
+         if (le != hipSuccess) return le;
+         RouteArgs ra{};
+         ra.logits = w.mlogits; ra.bias = lp.router_bias; ra.ids = w.mids; ra.weights = w.mweights; ra.ld = m.moe.E;
+         ra.T = R; ra.E = m.moe.E; ra.k = m.moe.k; ra.dt = DT_F32; ra.score = m.moe.score; ra.renorm = m.moe.renorm;
+         ra.groups = m.moe.groups; ra.top_groups = m.moe.top_groups; ra.group_top = m.moe.group_top; ra.scale = m.moe.scale;
+         return run_route(ra, st);
+       })) != hipSuccess)
+    return e;
+  return timed(prof, PC_GATEUP, st, [&] {
+    FfnArgs fa{};
+    fa.x = w.mx; fa.wgu = lp.x_wgu; fa.wd = lp.x_wd; fa.ids = w.mids; fa.weights = w.mweights; fa.out = w.part;
+    fa.ldx = fa.ldo = d;
+    fa.T = R; fa.E = m.moe.E; fa.k = m.moe.k; fa.d = d; fa.F = m.F; fa.dt = DT; fa.odt = DT_F32;
+    fa.ws = w.mws;
+    return run_ffn(fa, st);
+  });
+}
+
 template <int DT, int HD>
 static hipError_t forward_t(const Model& m, const Work& w, const Step& s, Prof* prof, hipStream_t st) {
   constexpr int KS = Geo<DT>::KS;
@@ -3447,6 +3518,12 @@ static hipError_t forward_t(const Model& m, const Work& w, const Step& s, Prof* 
       return e;
     if (s.cap && (e = cap(l, c_xf, w.xbuf, R16 * d * ESZ)) != hipSuccess) return e;
     }
+    // the FFN's product as slices in w.part: a sparse layer's experts, or
+    int sk_ffn = 1;
+    if (m.moe.E) {
+      if ((e = moe_ffn<DT>(m, w, lp, R, prof, st)) != hipSuccess) return e;
+    } else {
+    sk_ffn = sk_f;
     // gate/up projection and SwiGLU: fused for d / KS <= FK_MAX_S, else
     // split-K partials and a SwiGLU launch
     if (fused_swiglu(d, DT)) {
@@ -3467,13 +3544,15 @@ static hipError_t forward_t(const Model& m, const Work& w, const Step& s, Prof* 
         return e;
     }
     if (s.cap && (e = cap(l, c_z, w.zbuf, R16 * m.F * ESZ)) != hipSuccess) return e;
-    // down projection; residual add + the next norm (layer l+1 attention side, or final)
+    // down projection
     if ((e = timed(prof, PC_DOWN, st, [&] { return gemm<DT>(lp.wd, w.zbuf, d, m.F, R, w.part, st); })) != hipSuccess)
       return e;
+    }
+    // residual add + the next norm (layer l+1 attention side, or final)
     const float* gn = (l + 1 < m.L) ? m.layers[l + 1].attn_gain : m.final_gain;
     if ((e = timed(prof, PC_NORM, st, [&] {
            hipLaunchKernelGGL((resid_kernel<DT, 1>), dim3((d + RES_COLS - 1) / RES_COLS, R), dim3(RES_THREADS), 0,
-                              st, nullptr, nullptr, w.h, w.part, sk_f, R, gn, d, (void*)w.xbuf, Sd, w.ssq);
+                              st, nullptr, nullptr, w.h, w.part, sk_ffn, R, gn, d, (void*)w.xbuf, Sd, w.ssq);
            return last();
          })) != hipSuccess)
       return e;

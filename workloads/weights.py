@@ -9,6 +9,7 @@ that does not fit in host memory) can be regenerated on its own:
     lm_head          (2,)
     layer l gain j   (3, l, j)    j: 0 attention-side norm, 1 FFN-side norm
     final norm gain  (4,)
+    sparse layer l   (5, l, j)    j: 0 router, 1 w_gate_up, 2 w_down, 3 router bias (N(0, 0.1^2))
 
 Linear weights are N(0, std^2) (std = 0.02 unless a test asks for a larger
 spread, which keeps a small random model's greedy output from collapsing onto
@@ -30,6 +31,7 @@ import torch
 from .configs import ModelShape
 
 LAYER_TENSORS = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
+MOE_TENSORS = ("router", "w_gate_up", "w_down")   # of sparse layers, in the place of w_gate, w_up and w_down
 STD = 0.02
 
 
@@ -49,6 +51,9 @@ def bf16_bits_to_f32(bits: np.ndarray) -> np.ndarray:
 
 def tensor_shape(shape: ModelShape, name: str) -> tuple:
     d, qd, kd, f = shape.d_model, shape.q_dim, shape.kv_dim, shape.ffn
+    if shape.n_experts and name in MOE_TENSORS:
+        return {"router": (shape.n_experts, d), "w_gate_up": (shape.n_experts, 2 * f, d),
+                "w_down": (shape.n_experts, d, f)}[name]
     return {
         "embed": (shape.vocab, d), "lm_head": (shape.vocab, d),
         "wq": (qd, d), "wk": (kd, d), "wv": (kd, d), "wo": (d, qd),
@@ -105,12 +110,16 @@ class WeightSet:
     def _make_layer(self, l: int, ex: ThreadPoolExecutor | None = None) -> LayerWeights:
         s = self.shape
         jobs = [(name, (1, l, j)) for j, name in enumerate(LAYER_TENSORS)]
+        if s.n_experts:
+            jobs = jobs[:4] + [(name, (5, l, j)) for j, name in enumerate(MOE_TENSORS)]
         if ex is None:
             arrs = [draw_tensor(s, self.seed, k, tensor_shape(s, n), self.std) for n, k in jobs]
         else:
             arrs = list(ex.map(lambda nk: draw_tensor(s, self.seed, nk[1], tensor_shape(s, nk[0]),
                                                       self.std), jobs))
-        lw = LayerWeights(zip(LAYER_TENSORS, arrs))
+        lw = LayerWeights(zip([n for n, _ in jobs], arrs))
+        if s.n_experts and s.router_bias:
+            lw["router_bias"] = (0.1 * _rng(self.seed, (5, l, 3)).standard_normal(s.n_experts)).astype(np.float32)
         lw["attn_gain"] = draw_gain(s, self.seed, (3, l, 0), self.gains)
         lw["ffn_gain"] = draw_gain(s, self.seed, (3, l, 1), self.gains)
         return lw
@@ -121,15 +130,18 @@ class WeightSet:
         with ThreadPoolExecutor(self._threads) as ex:
             return self._make_layer(l, ex)
 
+    def _tensors(self) -> tuple:
+        return LAYER_TENSORS[:4] + MOE_TENSORS if self.shape.n_experts else LAYER_TENSORS
+
     def nbytes(self) -> int:
         tot = self.embed.nbytes + self.lm_head.nbytes
         for l in range(self.shape.n_layers):
             lw = self.layer(l) if self._layers is not None else None
             if lw is None:
                 esz = 2 if self.shape.dtype == "bf16" else 4
-                tot += esz * sum(int(np.prod(tensor_shape(self.shape, n))) for n in LAYER_TENSORS)
+                tot += esz * sum(int(np.prod(tensor_shape(self.shape, n))) for n in self._tensors())
             else:
-                tot += sum(lw[n].nbytes for n in LAYER_TENSORS)
+                tot += sum(lw[n].nbytes for n in self._tensors())
         return tot
 
 
