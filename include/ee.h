@@ -495,7 +495,7 @@ enum { EE_SCORE_SOFTMAX = 0, EE_SCORE_SIGMOID = 1 };
 
 /* y[t][n] = act(sum_k x[t][k] w[n][k] + bias[n]) + residual[t][n].
  * rows <= 2^22; `in` a multiple of 32 (bf16) or 16 (f32); any `out` up to 2^20.
- * x and w: 16-byte aligned, row strides multiples of 16 bytes.  out_dtype
+ * x and w: 16-byte aligned, row strides multiples of 16 bytes, at most 2^21.  out_dtype
  * (of y and residual): dtype or EE_F32. */
 typedef struct {
   const void* x;            /* [rows][ldx] dtype                              */
@@ -540,7 +540,8 @@ int32_t ee_moe_route(const ee_moe_route_args* args, void* hip_stream);
  * order, FFN_e(x) = (silu(x Wg_e^T) * (x Wu_e^T)) Wd_e^T with the product in
  * parentheses rounded to dtype.  Slots whose id is outside [0, n_experts) are
  * skipped (a row with none: its residual, or zeros).  d_model and ffn: multiples of 32 (bf16)
- * or 16 (f32), at most 32768; rows * top_k <= 2^24.  workspace: at least
+ * or 16 (f32), at most 32768, an expert's w_gate_up below 2 GiB; rows * top_k
+ * <= 2^24, ldx <= 2^21.  workspace: at least
  * ee_moe_ffn_workspace_bytes (0 for invalid sizes), 256-byte aligned, in use
  * until the call's work is done; calls that may overlap need one each. */
 typedef struct {

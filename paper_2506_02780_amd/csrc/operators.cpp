@@ -23,9 +23,10 @@ int ks(int t) { return t == EE_BF16 ? 32 : 16; }
 int dt_of(int t) { return t == EE_BF16 ? ee::DT_BF16 : ee::DT_F32; }
 
 // Rows of `cols` elements, `ld` elements apart, whose 16-byte pieces the
-// kernels load whole.
+// kernels load whole, at 32-bit offsets within a tile's 256 rows.
+constexpr int64_t MAX_LD = 1 << 21;
 bool rows_ok(const void* p, int64_t ld, int cols, int type) {
-  return aligned(p, 16) && ld >= cols && ld * esz(type) % 16 == 0 && ld < (int64_t(1) << 40);
+  return aligned(p, 16) && ld >= cols && ld <= MAX_LD && ld * esz(type) % 16 == 0;
 }
 // Rows that are read and written element by element (or more where aligned).
 bool out_ok(const void* p, int64_t ld, int cols, int type) {
@@ -50,7 +51,7 @@ int32_t ee_linear(const ee_linear_args* p, void* stream) {
   if (q.rows == 0) return EE_OK;
   if (!q.x || !q.w || !q.y) return bad("x, w and y must be non-NULL");
   if (!rows_ok(q.x, q.ldx, q.in, q.dtype) || !rows_ok(q.w, q.ldw, q.in, q.dtype))
-    return bad("x and w must be 16-byte aligned with row strides of at least `in` and a multiple of 16 bytes");
+    return bad("x and w must be 16-byte aligned with row strides of at least `in`, at most 2^21, and a multiple of 16 bytes");
   if (!out_ok(q.y, q.ldy, q.out, q.out_dtype)) return bad("y must be aligned to its type with a row stride of at least `out`");
   if (q.residual && !out_ok(q.residual, q.ldr, q.out, q.out_dtype))
     return bad("residual must be aligned to its type with a row stride of at least `out`");
@@ -96,6 +97,7 @@ static const char* ffn_shape(int64_t rows, int32_t E, int32_t k, int32_t d, int3
   if (rows < 0 || rows * k > MAX_PAIRS) return "rows * top_k must be in [0, 2^24]";
   if (d < 1 || d > 32768 || F < 1 || F > 32768) return "d_model and ffn must be in [1, 32768]";
   if (d % ks(dtype) || F % ks(dtype)) return "d_model and ffn must be multiples of 32 (bf16) / 16 (f32)";
+  if ((int64_t)2 * F * d * esz(dtype) >= int64_t(1) << 31) return "an expert's gate and up weights must stay below 2 GiB";
   if (rows * k * ((d > F ? d : F) / 16) > MAX_BLOCKS) return "too many output tiles";
   return nullptr;
 }
@@ -117,7 +119,7 @@ int32_t ee_moe_ffn(const ee_moe_ffn_args* p, void* stream) {
   if (q.rows == 0) return EE_OK;
   if (!q.x || !q.w_gate_up || !q.w_down || !q.ids || !q.weights || !q.out || !q.workspace)
     return bad("x, w_gate_up, w_down, ids, weights, out and workspace must be non-NULL");
-  if (!rows_ok(q.x, q.ldx, q.d_model, q.dtype)) return bad("x must be 16-byte aligned with a row stride of at least d_model and a multiple of 16 bytes");
+  if (!rows_ok(q.x, q.ldx, q.d_model, q.dtype)) return bad("x must be 16-byte aligned with a row stride of at least d_model, at most 2^21, and a multiple of 16 bytes");
   if (!aligned(q.w_gate_up, 16) || !aligned(q.w_down, 16)) return bad("w_gate_up and w_down must be 16-byte aligned");
   if (!aligned(q.ids, 4) || !aligned(q.weights, 4)) return bad("ids and weights must be aligned to their type");
   if (!out_ok(q.out, q.ldo, q.d_model, q.out_dtype)) return bad("out must be aligned to its type with a row stride of at least d_model");

@@ -5,7 +5,9 @@
 // Arithmetic (independent of the number of rows and of the kernel that runs,
 // so a row's result never depends on the other rows of a call):
 //   * every product element is one fp32 accumulator that takes the reduction's
-//     super-steps (32 columns in bf16, 16 in fp32: one fragment) in order;
+//     super-steps (32 columns in bf16, 16 in fp32: one fragment) in order; a
+//     linear of at most NARROW outputs (a router) instead sums eight such
+//     chains, in order, whatever the number of rows;
 //   * an experts' row is sum_j fma(w_j, y_j) over its slots in order, in fp32.
 
 #include "operators.h"
@@ -55,6 +57,15 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wp)[NT], cons
   }
 }
 
+// Four consecutive values, rounded to the type, from an aligned element index.
+template <int DT> __device__ __forceinline__ void store4(void* base, size_t i, f32x4 v) {
+  if constexpr (DT == DT_BF16)
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(base) + i) =
+        make_uint2(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]));
+  else
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(base) + i) = v;
+}
+
 __device__ __forceinline__ float silu(float v) { return v / (1.0f + expf(-v)); }
 
 __device__ __forceinline__ float activate(float v, int act) {
@@ -67,27 +78,346 @@ __device__ __forceinline__ float activate(float v, int act) {
   }
 }
 
-// ------------------------------------------------------------------- linear --
+// ----------------------------------------------------------------- epilogues --
+
+__device__ __forceinline__ f32x4 activate4(f32x4 v, int act) {
+  if (act == ACT_NONE) return v;
+  f32x4 u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = activate(v[i], act);
+  return u;
+}
 
 // Bias, activation and residual of features n .. n + 3 of row t, and the store.
-template <int ODT>
-__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v) {
-  if (t >= a.T) return;
+// vec: rows of y and residual are aligned for four values at a time.
+__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v, f32x4 bias, bool vec) {
+  if (t >= a.T || n >= a.N) return;
+  v = activate4(v + bias, a.act);
   const size_t yo = (size_t)t * a.ldy + n, ro = (size_t)t * a.ldr + n;
+  if (a.odt == DT_BF16) {
+    const uint16_t* res = reinterpret_cast<const uint16_t*>(a.res);
+    uint16_t* y = reinterpret_cast<uint16_t*>(a.y);
+    if (vec) {
+      if (res) {
+        const uint2 r = *reinterpret_cast<const uint2*>(res + ro);
+        v += f32x4{bf2f(r.x & 0xffff), bf2f(r.x >> 16), bf2f(r.y & 0xffff), bf2f(r.y >> 16)};
+      }
+      *reinterpret_cast<uint2*>(y + yo) = make_uint2(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]));
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (n + i >= a.N) return;
-    float u = v[i];
-    if (a.bias) u += a.bias[n + i];
-    u = activate(u, a.act);
-    if (a.res) u += load_elt<ODT>(a.res, ro + i);
-    store_elt<ODT>(a.y, yo + i, u);
+      for (int i = 0; i < 4; ++i)
+        if (n + i < a.N) y[yo + i] = (uint16_t)f2bf_bits(res ? v[i] + bf2f(res[ro + i]) : v[i]);
+    }
+  } else {
+    const float* res = reinterpret_cast<const float*>(a.res);
+    float* y = reinterpret_cast<float*>(a.y);
+    if (vec) {
+      if (res) v += *reinterpret_cast<const f32x4*>(res + ro);
+      *reinterpret_cast<f32x4*>(y + yo) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n + i < a.N) y[yo + i] = res ? v[i] + res[ro + i] : v[i];
+    }
+  }
+}
+__device__ __forceinline__ bool linear_vec(const LinearArgs& a) {
+  const uintptr_t need = a.odt == DT_BF16 ? 8 : 16;
+  return a.N % 4 == 0 && a.ldy % 4 == 0 && (!a.res || a.ldr % 4 == 0) && reinterpret_cast<uintptr_t>(a.y) % need == 0 &&
+         reinterpret_cast<uintptr_t>(a.res) % need == 0;
+}
+__device__ __forceinline__ f32x4 linear_bias(const LinearArgs& a, int n) {
+  f32x4 b = {0.f, 0.f, 0.f, 0.f};
+  if (a.bias)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = a.bias[min(n + i, a.N - 1)];
+  return b;
+}
+
+// -------------------------------------------------------------- tile products --
+
+// Waits until at most N of the wave's vector memory operations are outstanding.
+template <int N> __device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+// Workgroup barrier that waits for no memory operation (the callers wait for
+// what they need), and that the compiler moves no access across.
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+enum TileMode { TM_LINEAR, TM_UP, TM_DOWN };
+
+// A run of at most BM rows of one expert, rows p0 .. p0 + n - 1 of the sorted order.
+struct ExpertTile {
+  int e, p0, n;
+};
+
+// What one call's experts kernels share (device memory in the workspace).
+struct FfnPlan {
+  int* ntile;          // row tiles in use
+  ExpertTile* tile;    // [ntile]
+  int* order;          // [pairs] pairs (row * k + slot) sorted by expert; skipped ones are not in it
+  void* z;             // [pairs][F] dt, rows in sorted order
+  float* y;            // [pairs][d], rows by pair
+};
+
+struct TileArgs {
+  LinearArgs l;        // TM_LINEAR
+  FfnArgs f;           // the others
+  FfnPlan p;
+  int nrt, nft;        // row tiles (at most), feature tiles
+};
+
+// Products of BM rows with BN rows of weights, both streamed through LDS in
+// stages of 128 bytes of a row (two super-steps), NST stages deep.  What bounds
+// a large product is that every wave reads its fragments from LDS while the
+// matrix cores run: a wave of RF x FF fragments reads RF + FF per RF FF matrix
+// instructions, so the largest tile (256 x 256, eight waves of 64 x 128) takes
+// all of the registers of two waves per SIMD.
+//   * Stages arrive by direct loads to LDS; each load takes eight rows of 128
+//     bytes (whole lines), the 16-byte pieces of row r at place piece ^ (r / 2
+//     % 8), so that the 16 rows that a fragment read touches fall on all banks.
+//   * A stage's two super-steps are read one ahead of the matrix instructions
+//     that use them, across the stage's barrier too.
+// Rows past the end repeat the last one; their results are not stored.
+template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST>
+__global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
+  constexpr int ESZ = Geo<DT>::ESZ, WAVES = WR * WF, RF = BM / WR / 16, FF = BN / WF / 16;
+  constexpr int LPW = (BM + BN) / 8 / WAVES;   // loads per wave and stage
+  constexpr int STAGE = (BM + BN) * 8;         // 16-byte pieces of a stage
+  static_assert((BM + BN) / 8 % WAVES == 0, "every wave loads as much");
+  static_assert(MODE != TM_UP || FF % 2 == 0, "a wave owns gate and up tiles of the same features");
+  static_assert((NST - 1) * LPW < 64, "outstanding loads are counted in six bits");
+  // (arrays of their own: the compiler then knows that a request into one does not touch the others)
+  __shared__ uint4 b0[STAGE], b1[STAGE], b2[NST > 2 ? STAGE : 1], b3[NST > 3 ? STAGE : 1];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  const int wr = wv / WF, wf = wv % WF;
+
+  // Workgroups are dealt to the eight XCDs in turn: each XCD takes a run of the
+  // tiles, GR row tiles side by side under one feature tile after another, so
+  // that what they share stays in its L2.
+  const int nrt = MODE == TM_LINEAR ? a.nrt : *a.p.ntile;
+  const int ntile = nrt * a.nft, per = (ntile + 7) / 8, at = (int)(blockIdx.x >> 3);
+  const int tile = (int)(blockIdx.x & 7) * per + at;
+  if (at >= per || tile >= ntile) return;
+  constexpr int GR = 8;
+  const int gsz = GR * a.nft, gi = tile / gsz, gr0 = gi * GR, gh = min(GR, nrt - gr0), gj = tile - gi * gsz;
+  const int rt = gr0 + gj % gh, ft = gj / gh;
+
+  const unsigned char *xb, *wb;   // the operands' tiles
+  unsigned ldx, ldw;              // bytes between their rows
+  int S, t0 = 0, rows;            // super-steps, first row, rows
+  int f0;                         // first feature
+  ExpertTile et{};
+  if constexpr (MODE == TM_LINEAR) {
+    S = a.l.K / Geo<DT>::KS;
+    t0 = rt * BM;
+    rows = min(BM, a.l.T - t0);
+    f0 = ft * BN;
+    ldx = (unsigned)a.l.ldx * ESZ;
+    ldw = (unsigned)a.l.ldw * ESZ;
+    xb = reinterpret_cast<const unsigned char*>(a.l.x) + (size_t)t0 * ldx;
+    wb = reinterpret_cast<const unsigned char*>(a.l.w) + (size_t)f0 * ldw;
+  } else {
+    et = a.p.tile[rt];
+    rows = et.n;
+    const int K = MODE == TM_UP ? a.f.d : a.f.F;
+    S = K / Geo<DT>::KS;
+    ldw = (unsigned)K * ESZ;
+    if constexpr (MODE == TM_UP) {
+      f0 = ft * (BN / 2);
+      ldx = (unsigned)a.f.ldx * ESZ;
+      xb = reinterpret_cast<const unsigned char*>(a.f.x);
+      wb = reinterpret_cast<const unsigned char*>(a.f.wgu) + (size_t)et.e * 2 * a.f.F * ldw;
+    } else {
+      f0 = ft * BN;
+      ldx = (unsigned)a.f.F * ESZ;
+      xb = reinterpret_cast<const unsigned char*>(a.p.z) + (size_t)et.p0 * ldx;
+      wb = reinterpret_cast<const unsigned char*>(a.f.wd) + ((size_t)et.e * a.f.d + f0) * ldw;
+    }
+  }
+  const int stages = (S + 1) / 2;
+
+  // this lane's piece of each of the wave's loads
+  unsigned off[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int inst = wv * LPW + i;
+    int r = inst * 8 + (lane >> 3);
+    const unsigned piece = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
+    if (inst < BM / 8) {
+      r = min(r, rows - 1);
+      if constexpr (MODE == TM_UP) r = a.p.order[et.p0 + r] / a.f.k;
+      off[i] = (unsigned)r * ldx + piece;
+    } else {
+      r -= BM;
+      if constexpr (MODE == TM_LINEAR) r = min(r, a.l.N - 1 - f0);
+      if constexpr (MODE == TM_DOWN) r = min(r, a.f.d - 1 - f0);
+      if constexpr (MODE == TM_UP) {   // a wave's first FF / 2 tiles are gate features, then up of the same
+        const int w = r / (FF * 16), j = r % (FF * 16), up = j >= FF * 8;
+        r = min(f0 + w * (FF * 8) + (up ? j - FF * 8 : j), a.f.F - 1) + (up ? a.f.F : 0);
+      }
+      off[i] = (unsigned)r * ldw + piece;
+    }
+  }
+  // Requests the next stage (past the last one: that one again, unused).  The
+  // second half of an odd reduction's last stage is the first half again.
+  int next = 0;
+  auto fetch = [&](uint4* buf) {
+    const bool half = 2 * next + 1 == S;
+    const size_t col = (size_t)next * 128;
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int inst = wv * LPW + i;
+      const unsigned over = half && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
+      const unsigned char* src = (inst < BM / 8 ? xb : wb) + col;
+      __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
+    }
+    if (next < stages - 1) ++next;
+  };
+
+  f32x4 acc[FF][RF];
+#pragma unroll
+  for (int f = 0; f < FF; ++f)
+#pragma unroll
+    for (int r = 0; r < RF; ++r) acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int q = grp ^ ((c >> 1) & 7);
+  const int xo = (wr * RF * 16 + c) * 8 + q, wo = (BM + wf * FF * 16 + c) * 8 + q;
+  uint4 xa[RF], wa[FF], xc[RF], wc[FF];   // the first and second super-step of a stage
+  auto read = [&](uint4 (&xf)[RF], uint4 (&wfr)[FF], const uint4* buf, int s) {
+#pragma unroll
+    for (int r = 0; r < RF; ++r) xf[r] = buf[(xo ^ (s * 4)) + r * 128];
+#pragma unroll
+    for (int f = 0; f < FF; ++f) wfr[f] = buf[(wo ^ (s * 4)) + f * 128];
+  };
+  auto mul = [&](const uint4 (&xf)[RF], const uint4 (&wfr)[FF]) {
+#pragma unroll
+    for (int f = 0; f < FF; ++f)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) acc[f][r] = mma<DT>(wfr[f], xf[r], acc[f][r]);
+  };
+  int left = stages;
+  auto second = [&](const uint4* cur) {
+    read(xc, wc, cur, 1);
+    if (--left == 0 && (S & 1))   // (an odd reduction ends with half a stage: zeros)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) xc[r] = make_uint4(0, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(xa, wa);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // The stage in `cur`: the products of the stage before, in `prev`, are finished
+  // while its first fragments are read; `prev`, which every wave has read by
+  // now, takes the stage NST - 1 on.
+  auto stage = [&](uint4* prev, uint4* cur) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): this wave's reads of `prev` are done
+    wait_vm<(NST - 2) * LPW>();           // its part of `cur` has arrived
+    barrier_only();
+    fetch(prev);
+    read(xa, wa, cur, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    mul(xc, wc);
+    __builtin_amdgcn_sched_barrier(0);
+    second(cur);
+  };
+  fetch(b0);
+  fetch(b1);
+  if (NST > 2) fetch(b2);
+  if (NST > 3) fetch(b3);
+  wait_vm<(NST - 1) * LPW>();
+  barrier_only();
+  read(xa, wa, b0, 0);
+  second(b0);
+  if constexpr (NST == 2) {
+    while (left) {
+      stage(b0, b1);
+      if (!left) break;
+      stage(b1, b0);
+    }
+  } else {
+    // (whole turns of the buffers without an exit between them, so that the
+    // compiler sees which request each read follows and adds no wait of its
+    // own; then the rest)
+    const int rest = (stages - 1) % NST;
+    for (int g = (stages - 1) / NST; g > 0; --g) {
+      stage(b0, b1);
+      stage(b1, b2);
+      if constexpr (NST == 3) stage(b2, b0);
+      if constexpr (NST == 4) { stage(b2, b3); stage(b3, b0); }
+    }
+    if (rest > 0) {
+      stage(b0, b1);
+      if (rest > 1) {
+        stage(b1, b2);
+        if constexpr (NST > 3)
+          if (rest > 2) stage(b2, b3);
+      }
+    }
+  }
+  mul(xc, wc);
+  wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
+
+  if constexpr (MODE == TM_LINEAR) {
+    const bool vec = linear_vec(a.l);
+#pragma unroll
+    for (int f = 0; f < FF; ++f) {
+      const int n = f0 + (wf * FF + f) * 16 + 4 * grp;
+      const f32x4 bias = linear_bias(a.l, n);
+#pragma unroll
+      for (int r = 0; r < RF; ++r) linear_out(a.l, t0 + (wr * RF + r) * 16 + c, n, acc[f][r], bias, vec);
+    }
+  } else if constexpr (MODE == TM_UP) {
+#pragma unroll
+    for (int f = 0; f < FF / 2; ++f) {
+      const int n = f0 + (wf * (FF / 2) + f) * 16 + 4 * grp;
+      if (n >= a.f.F) continue;
+#pragma unroll
+      for (int r = 0; r < RF; ++r) {
+        const int row = (wr * RF + r) * 16 + c;
+        if (row >= rows) continue;
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = silu(acc[f][r][i]) * acc[f + FF / 2][r][i];
+        store4<DT>(a.p.z, (size_t)(et.p0 + row) * a.f.F + n, v);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < RF; ++r) {
+      const int row = (wr * RF + r) * 16 + c;
+      if (row >= rows) continue;
+      float* y = a.p.y + (size_t)a.p.order[et.p0 + row] * a.f.d;
+#pragma unroll
+      for (int f = 0; f < FF; ++f) {
+        const int n = f0 + (wf * FF + f) * 16 + 4 * grp;
+        if (n < a.f.d) *reinterpret_cast<f32x4*>(y + n) = acc[f][r];
+      }
+    }
   }
 }
 
+template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST>
+static hipError_t launch_tile(TileArgs a, hipStream_t st) {
+  if (MODE == TM_LINEAR) a.nrt = (a.l.T + BM - 1) / BM;
+  const int cols = MODE == TM_LINEAR ? a.l.N : MODE == TM_UP ? 2 * a.f.F : a.f.d;
+  a.nft = (cols + BN - 1) / BN;
+  const int64_t n = (int64_t)a.nrt * a.nft;
+  hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------- linear --
+
 // One 16-feature tile per wave and 16 rows per workgroup.
-template <int DT, int ODT>
-__global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, int nblk) {
+template <int DT>
+__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, int nblk) {
   constexpr int ESZ = Geo<DT>::ESZ;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, grp = lane >> 4;
   const int nb = blockIdx.x % nblk, t0 = blockIdx.x / nblk * 16, n0 = (nb * 4 + wv) * 16;
@@ -98,17 +428,100 @@ __global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, int nblk) {
       reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + c, a.T - 1) * a.ldx * ESZ + grp * 16;
   f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
   chain<DT, 1, 8>(wp, xp, a.K / Geo<DT>::KS, acc);
-  linear_out<ODT>(a, t0 + c, n0 + 4 * grp, acc[0]);
+  linear_out(a, t0 + c, n0 + 4 * grp, acc[0], linear_bias(a, n0 + 4 * grp), linear_vec(a));
+}
+
+// Products of few outputs (a router): a workgroup's eight waves each sum the
+// 128-byte stages w, w + 8, ... of the reduction for MT x NT tiles, and the
+// eight sums are added in wave order.
+constexpr int NARROW = 512, CHAINS = 8;
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(CHAINS * 64) void linear_narrow_kernel(LinearArgs a, int nblk) {
+  constexpr int ESZ = Geo<DT>::ESZ, D = MT * NT > 4 ? 2 : 4;   // stages requested ahead
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  const int n0 = blockIdx.x % nblk * (NT * 16), t0 = blockIdx.x / nblk * (MT * 16);
+  const int S = a.K / Geo<DT>::KS;
+  const unsigned char *wp[NT], *xp[MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+    wp[n] = reinterpret_cast<const unsigned char*>(a.w) + (size_t)min(n0 + n * 16 + c, a.N - 1) * a.ldw * ESZ + grp * 16;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+    xp[m] = reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + m * 16 + c, a.T - 1) * a.ldx * ESZ + grp * 16;
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int j = wv; 2 * j < S; j += CHAINS * D) {
+    uint4 wq[D][2][NT], xq[D][2][MT];
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const size_t o = (size_t)min(2 * (j + CHAINS * i) + h, S - 1) * STEP;   // (past the end: unused)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wq[i][h][n] = *reinterpret_cast<const uint4*>(wp[n] + o);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xq[i][h][m] = *reinterpret_cast<const uint4*>(xp[m] + o);
+      }
+#pragma unroll
+    for (int i = 0; i < D; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (2 * (j + CHAINS * i) + h < S)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[n][m] = mma<DT>(wq[i][h][n], xq[i][h][m], acc[n][m]);
+  }
+  __shared__ f32x4 red[CHAINS][NT * MT][64];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) red[wv][n * MT + m][lane] = acc[n][m];
+  __syncthreads();
+  for (int i = wv; i < NT * MT; i += CHAINS) {
+    f32x4 v = red[0][i][lane];
+#pragma unroll
+    for (int w = 1; w < CHAINS; ++w) v += red[w][i][lane];
+    const int n = n0 + i / MT * 16 + 4 * grp;
+    linear_out(a, t0 + i % MT * 16 + c, n, v, linear_bias(a, n), linear_vec(a));
+  }
+}
+
+template <int DT, int MT, int NT>
+static hipError_t launch_narrow(const LinearArgs& a, hipStream_t st) {
+  const int nblk = (a.N + NT * 16 - 1) / (NT * 16);
+  hipLaunchKernelGGL((linear_narrow_kernel<DT, MT, NT>), dim3((unsigned)nblk * ((a.T + MT * 16 - 1) / (MT * 16))),
+                     dim3(CHAINS * 64), 0, st, a, nblk);
+  return hipGetLastError();
+}
+
+template <int DT>
+static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
+  const int64_t rt = (a.T + 15) / 16, nt = (a.N + 15) / 16;
+  if (a.N <= NARROW)
+    // small tiles until they fill the chip, then those that read the rows less often
+    return rt * nt <= 2048 ? launch_narrow<DT, 1, 1>(a, st) : launch_narrow<DT, 2, 4>(a, st);
+  if (a.T <= 16) {
+    const int nblk = (a.N + 63) / 64;
+    hipLaunchKernelGGL((linear_rows_kernel<DT>), dim3((unsigned)nblk * (unsigned)rt), dim3(256), 0, st, a, nblk);
+    return hipGetLastError();
+  }
+  TileArgs t{};
+  t.l = a;
+  auto tiles = [&](int64_t m, int64_t n) { return ((a.T + m - 1) / m) * ((a.N + n - 1) / n); };
+  if constexpr (DT == DT_BF16)
+    if (tiles(256, 256) >= 256) return launch_tile<DT, TM_LINEAR, 256, 256, 4, 2, 2>(t, st);
+  if (tiles(128, 128) >= 512) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 2, 2>(t, st);
+  if (tiles(64, 64) >= 256) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 2>(t, st);
+  return launch_tile<DT, TM_LINEAR, 32, 64, 1, 4, 4>(t, st);
 }
 
 hipError_t run_linear(const LinearArgs& a, hipStream_t st) {
   if (a.T == 0) return hipSuccess;
-  const int nblk = (a.N + 63) / 64;
-  const dim3 grid((unsigned)nblk * ((a.T + 15) / 16)), block(256);
-  if (a.dt == DT_F32) hipLaunchKernelGGL((linear_kernel<DT_F32, DT_F32>), grid, block, 0, st, a, nblk);
-  else if (a.odt == DT_F32) hipLaunchKernelGGL((linear_kernel<DT_BF16, DT_F32>), grid, block, 0, st, a, nblk);
-  else hipLaunchKernelGGL((linear_kernel<DT_BF16, DT_BF16>), grid, block, 0, st, a, nblk);
-  return hipGetLastError();
+  return a.dt == DT_F32 ? linear_t<DT_F32>(a, st) : linear_t<DT_BF16>(a, st);
 }
 
 // -------------------------------------------------------------------- route --
@@ -293,26 +706,166 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void ffn_down_kernel(FfnArgs a, co
   }
 }
 
+// ------------------------------------------------------- experts, many rows --
+
+// Sorts the pairs by expert and cuts every expert's run into row tiles of BM.
+// One workgroup: counts in LDS, offsets by a scan over the experts, places by
+// LDS counters again.  (The order of the pairs within an expert may differ from
+// run to run; every row's arithmetic is its own, so the results do not.)
+constexpr int PLAN_THREADS = 1024;
+static_assert(PLAN_THREADS >= ROUTE_MAX_E, "a thread per expert");
+__global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __restrict__ ids, int P, int E, int BM, FfnPlan p) {
+  __shared__ int cnt[ROUTE_MAX_E], first[ROUTE_MAX_E], tiles[ROUTE_MAX_E];
+  const int t = threadIdx.x;
+  for (int e = t; e < E; e += PLAN_THREADS) cnt[e] = 0;
+  __syncthreads();
+  for (int i = t; i < P; i += PLAN_THREADS) {
+    const int e = ids[i];
+    if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
+  }
+  __syncthreads();
+  // inclusive scans of the counts and of the tiles
+  int n = 0, own = 0;
+  if (t < E) {
+    n = cnt[t];
+    own = (n + BM - 1) / BM;
+    first[t] = n;
+    tiles[t] = own;
+  }
+  __syncthreads();
+  for (int o = 1; o < E; o <<= 1) {
+    int a = 0, b = 0;
+    if (t >= o && t < E) { a = first[t - o]; b = tiles[t - o]; }
+    __syncthreads();
+    if (t >= o && t < E) { first[t] += a; tiles[t] += b; }
+    __syncthreads();
+  }
+  if (t < E) {
+    const int p0 = first[t] - n, t0 = tiles[t] - own;
+    for (int i = 0; i < own; ++i) p.tile[t0 + i] = ExpertTile{t, p0 + i * BM, min(BM, n - i * BM)};
+    cnt[t] = p0;
+    if (t == E - 1) *p.ntile = tiles[t];
+  }
+  __syncthreads();
+  for (int i = t; i < P; i += PLAN_THREADS) {
+    const int e = ids[i];
+    if (e >= 0 && e < E) p.order[atomicAdd(&cnt[e], 1)] = i;
+  }
+}
+
+// out[t] = sum_j w_j y[t k + j] + res, slots in order, four columns per thread.
+template <int ODT>
+__global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a, const float* __restrict__ y) {
+  const int per = (a.d / 4 + 255) / 256, t = blockIdx.x / per, n = (blockIdx.x % per * 256 + threadIdx.x) * 4;
+  if (n >= a.d) return;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < a.k; ++j) {
+    const size_t p = (size_t)t * a.k + j;
+    const int e = a.ids[p];
+    if (e < 0 || e >= a.E) continue;
+    const f32x4 v = *reinterpret_cast<const f32x4*>(y + p * a.d + n);
+    const float w = a.weights[p];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = fmaf(w, v[i], o[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float u = o[i];
+    if (a.res) u += load_elt<ODT>(a.res, (size_t)t * a.ldr + n + i);
+    store_elt<ODT>(a.out, (size_t)t * a.ldo + n + i, u);
+  }
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+// (row tiles of 16 rows at least: what the smallest tile needs holds for all)
+size_t ffn_tiles(int64_t P, int E, int BM) { return (size_t)(P / BM + std::min<int64_t>(P, E)); }
+constexpr int MIN_BM = 32;
+
 size_t ffn_workspace(int T, int E, int k, int d, int F, int dt) {
-  (void)E; (void)d;
-  return ((size_t)T * k * F * esz_of(dt) + 255) / 256 * 256;
+  const size_t P = (size_t)T * k;
+  return align256(4) + align256(ffn_tiles(P, E, MIN_BM) * sizeof(ExpertTile)) + align256(P * 4) +
+         align256(P * F * esz_of(dt)) + align256(P * d * 4);
+}
+
+static FfnPlan ffn_plan(const FfnArgs& a) {
+  const size_t P = (size_t)a.T * a.k;
+  unsigned char* ws = a.ws;
+  FfnPlan p;
+  p.ntile = reinterpret_cast<int*>(ws); ws += align256(4);
+  p.tile = reinterpret_cast<ExpertTile*>(ws); ws += align256(ffn_tiles(P, a.E, MIN_BM) * sizeof(ExpertTile));
+  p.order = reinterpret_cast<int*>(ws); ws += align256(P * 4);
+  p.z = ws; ws += align256(P * a.F * esz_of(a.dt));
+  p.y = reinterpret_cast<float*>(ws);
+  return p;
+}
+
+template <int DT, int BM>
+static hipError_t ffn_tiles_t(const TileArgs& t, hipStream_t st) {
+  hipError_t e;
+  if constexpr (BM == 32) {
+    if ((e = launch_tile<DT, TM_UP, 32, 128, 1, 4, 4>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 32, 128, 1, 4, 4>(t, st);
+  } else if constexpr (BM == 64) {
+    if ((e = launch_tile<DT, TM_UP, 64, 128, 2, 2, 3>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 64, 128, 2, 2, 3>(t, st);
+  } else if constexpr (BM == 128) {
+    if ((e = launch_tile<DT, TM_UP, 128, 128, 2, 2, 2>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 128, 128, 2, 2, 2>(t, st);
+  } else {
+    if ((e = launch_tile<DT, TM_UP, 256, 256, 4, 2, 2>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 256, 256, 4, 2, 2>(t, st);
+  }
 }
 
 template <int DT, int ODT>
 static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
-  void* z = a.ws;
-  const int ub = (a.F + 63) / 64, db = a.d / 16;
-  hipLaunchKernelGGL((ffn_up_kernel<DT>), dim3((unsigned)ub * a.T * a.k), dim3(256), 0, st, a, z, ub);
-  hipError_t e = hipGetLastError();
+  const int64_t P = (int64_t)a.T * a.k;
+  hipError_t e;
+  FfnPlan pl = ffn_plan(a);
+  if (P <= 64) {
+    const int ub = (a.F + 63) / 64, db = a.d / 16;
+    hipLaunchKernelGGL((ffn_up_kernel<DT>), dim3((unsigned)ub * P), dim3(256), 0, st, a, pl.z, ub);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL((ffn_down_kernel<DT, ODT>), dim3((unsigned)db * a.T), dim3(DOWN_WAVES * 64), 0, st, a, (const void*)pl.z, db);
+    return hipGetLastError();
+  }
+  const int64_t avg = P / a.E;
+  const int BM = avg < 24 ? 32 : avg < 96 ? 64 : (avg < 256 || DT == DT_F32) ? 128 : 256;
+  TileArgs t{};
+  t.f = a;
+  t.p = pl;
+  t.nrt = (int)ffn_tiles(P, a.E, BM);
+  hipLaunchKernelGGL(ffn_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (BM == 32) e = ffn_tiles_t<DT, 32>(t, st);
+  else if (BM == 64) e = ffn_tiles_t<DT, 64>(t, st);
+  else if (BM == 128) e = ffn_tiles_t<DT, 128>(t, st);
+  else if constexpr (DT == DT_BF16) e = ffn_tiles_t<DT, 256>(t, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((ffn_down_kernel<DT, ODT>), dim3((unsigned)db * a.T), dim3(DOWN_WAVES * 64), 0, st, a, (const void*)z, db);
+  hipLaunchKernelGGL((ffn_sum_kernel<ODT>), dim3((unsigned)((a.d / 4 + 255) / 256) * a.T), dim3(256), 0, st, a, (const float*)pl.y);
   return hipGetLastError();
 }
 
 hipError_t run_ffn(const FfnArgs& a, hipStream_t st) {
-  if (a.T == 0) return hipSuccess;
-  if (a.dt == DT_F32) return ffn_t<DT_F32, DT_F32>(a, st);
-  return a.odt == DT_F32 ? ffn_t<DT_BF16, DT_F32>(a, st) : ffn_t<DT_BF16, DT_BF16>(a, st);
+  // The tile kernels gather rows of x at 32-bit offsets: inputs of 4 GiB and
+  // more run in parts (on the same workspace, one after another).
+  const int64_t row = a.ldx * esz_of(a.dt);
+  const int most = (int)std::min<int64_t>(a.T, (int64_t(1) << 32) / row - 1);
+  for (int t = 0; t < a.T; t += most) {
+    FfnArgs b = a;
+    b.T = std::min(most, a.T - t);
+    b.x = reinterpret_cast<const unsigned char*>(a.x) + (size_t)t * row;
+    b.ids = a.ids + (size_t)t * a.k;
+    b.weights = a.weights + (size_t)t * a.k;
+    b.out = reinterpret_cast<unsigned char*>(a.out) + (size_t)t * a.ldo * esz_of(a.odt);
+    if (a.res) b.res = reinterpret_cast<const unsigned char*>(a.res) + (size_t)t * a.ldr * esz_of(a.odt);
+    const hipError_t e = a.dt == DT_F32     ? ffn_t<DT_F32, DT_F32>(b, st)
+                         : a.odt == DT_F32 ? ffn_t<DT_BF16, DT_F32>(b, st)
+                                           : ffn_t<DT_BF16, DT_BF16>(b, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ee

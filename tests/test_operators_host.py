@@ -57,6 +57,7 @@ def test_zero_rows_are_no_work(ee):
     (dict(x=None, rows=1), "non-NULL"), (dict(w=None, rows=1), "non-NULL"), (dict(y=None, rows=1), "non-NULL"),
     (dict(x=P + 8, rows=1), "16-byte"), (dict(w=P + 2, rows=1), "16-byte"), (dict(ldx=63, rows=1), "16-byte"),
     (dict(ldw=56, rows=1), "16-byte"), (dict(ldx=68, rows=1), "16-byte"), (dict(ldx=-64, rows=1), "16-byte"),
+    (dict(ldx=(1 << 21) + 64, rows=1), "16-byte"), (dict(ldw=(1 << 21) + 64, rows=1), "16-byte"),
     (dict(y=P + 1, rows=1), "y must"), (dict(ldy=47, rows=1), "y must"), (dict(ldr=47, rows=1), "residual"),
     (dict(residual=P + 1, rows=1), "residual"), (dict(bias=P + 2, rows=1), "bias"),
     (dict(rows=1 << 22, out=1 << 20, ldy=1 << 20, ldr=1 << 20), "tiles"),
@@ -88,7 +89,7 @@ def test_route_refusals(ee, kw, word):
     (dict(dtype=0, out_dtype=1), "out_dtype"), (dict(x=None, rows=1), "non-NULL"), (dict(w_gate_up=None, rows=1), "non-NULL"),
     (dict(w_down=None, rows=1), "non-NULL"), (dict(ids=None, rows=1), "non-NULL"), (dict(weights=None, rows=1), "non-NULL"),
     (dict(out=None, rows=1), "non-NULL"), (dict(workspace=None, rows=1), "non-NULL"), (dict(x=P + 2, rows=1), "x must"),
-    (dict(ldx=65, rows=1), "x must"), (dict(ldx=56, rows=1), "x must"), (dict(w_gate_up=P + 2, rows=1), "w_gate_up"),
+    (dict(d_model=32768, ffn=16384), "2 GiB"), (dict(ldx=(1 << 21) + 64, rows=1), "x must"), (dict(ldx=65, rows=1), "x must"), (dict(ldx=56, rows=1), "x must"), (dict(w_gate_up=P + 2, rows=1), "w_gate_up"),
     (dict(w_down=P + 8, rows=1), "w_down"), (dict(ids=P + 2, rows=1), "ids"), (dict(ldo=63, rows=1), "out must"),
     (dict(out=P + 1, rows=1), "out must"), (dict(ldr=63, rows=1), "residual"), (dict(workspace=P + 128, rows=1), "workspace"),
 ])
