@@ -66,13 +66,21 @@ template <int DT> __device__ __forceinline__ void store4(void* base, size_t i, f
     *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(base) + i) = v;
 }
 
-__device__ __forceinline__ float silu(float v) { return v / (1.0f + expf(-v)); }
+// 1 / (1 + e^-v) on the hardware's exp2 and reciprocal.  The exponent's product is
+// rounded once (|v| log2(e) 2^-24 of e^-v), so the result is off by at most a few
+// 2^-24 where it matters (|v| e^-v / (1 + e^-v) < 0.3) and its product with v by a
+// few 2^-24 |v| everywhere.  (expf and a division: the activation of an 8192 x
+// 11008 output took 110 us, now 16.)
+__device__ __forceinline__ float logistic(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
+}
+__device__ __forceinline__ float silu(float v) { return v * logistic(v); }
 
 __device__ __forceinline__ float activate(float v, int act) {
   switch (act) {
     case ACT_SILU: return silu(v);
     case ACT_GELU: return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-    case ACT_GELU_TANH: return v / (1.0f + expf(-1.5957691216057308f * (v + 0.044715f * v * v * v)));
+    case ACT_GELU_TANH: return v * logistic(1.5957691216057308f * (v + 0.044715f * v * v * v));
     case ACT_RELU: return v < 0.0f ? 0.0f : v;   // (NaN stays NaN)
     default: return v;
   }
@@ -266,20 +274,23 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       off[i] = (unsigned)r * ldw + piece;
     }
   }
-  // Requests the next stage (past the last one: that one again, unused).  The
-  // second half of an odd reduction's last stage is the first half again.
+  // Requests load i of the next stage (past the last one: that one again,
+  // unused).  The second half of an odd reduction's last stage is the first half
+  // again.
   int next = 0;
-  auto fetch = [&](uint4* buf) {
-    const bool half = 2 * next + 1 == S;
-    const size_t col = (size_t)next * 128;
-#pragma unroll
-    for (int i = 0; i < LPW; ++i) {
-      const int inst = wv * LPW + i;
-      const unsigned over = half && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
-      const unsigned char* src = (inst < BM / 8 ? xb : wb) + col;
-      __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
-    }
+  auto fetch_one = [&](uint4* buf, int i) {
+    const int inst = wv * LPW + i;
+    const unsigned over = 2 * next + 1 == S && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
+    const unsigned char* src = (inst < BM / 8 ? xb : wb) + (size_t)next * 128;
+    __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
+  };
+  auto fetched = [&]() {
     if (next < stages - 1) ++next;
+  };
+  auto fetch = [&](uint4* buf) {
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) fetch_one(buf, i);
+    fetched();
   };
 
   f32x4 acc[FF][RF];
@@ -290,27 +301,35 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   const int q = grp ^ ((c >> 1) & 7);
   const int xo = (wr * RF * 16 + c) * 8 + q, wo = (BM + wf * FF * 16 + c) * 8 + q;
   uint4 xa[RF], wa[FF], xc[RF], wc[FF];   // the first and second super-step of a stage
+  // fragment i of a super-step: weights first, then rows
+  auto read_one = [&](uint4 (&xf)[RF], uint4 (&wfr)[FF], const uint4* buf, int s, int i) {
+    if (i < FF) wfr[i] = buf[(wo ^ (s * 4)) + i * 128];
+    else xf[i - FF] = buf[(xo ^ (s * 4)) + (i - FF) * 128];
+  };
   auto read = [&](uint4 (&xf)[RF], uint4 (&wfr)[FF], const uint4* buf, int s) {
 #pragma unroll
-    for (int r = 0; r < RF; ++r) xf[r] = buf[(xo ^ (s * 4)) + r * 128];
-#pragma unroll
-    for (int f = 0; f < FF; ++f) wfr[f] = buf[(wo ^ (s * 4)) + f * 128];
+    for (int i = 0; i < FF + RF; ++i) read_one(xf, wfr, buf, s, i);
   };
-  auto mul = [&](const uint4 (&xf)[RF], const uint4 (&wfr)[FF]) {
+  auto mul = [&](const uint4 (&xf)[RF], const uint4 (&wfr)[FF], int j0, int j1) {
 #pragma unroll
-    for (int f = 0; f < FF; ++f)
-#pragma unroll
-      for (int r = 0; r < RF; ++r) acc[f][r] = mma<DT>(wfr[f], xf[r], acc[f][r]);
+    for (int j = j0; j < j1; ++j) acc[j / RF][j % RF] = mma<DT>(wfr[j / RF], xf[j % RF], acc[j / RF][j % RF]);
   };
+  // A super-step's matrix instructions in PARTS parts, between which the next
+  // super-step's fragments are read and (buf not null) the requests for a later
+  // stage go out: all at once, either would hold up the wave's matrix
+  // instructions for as long as all eight waves' reads or requests take.
+  constexpr int MN = FF * RF, PARTS = MN < 8 ? MN : 8;
   int left = stages;
   auto second = [&](const uint4* cur) {
-    read(xc, wc, cur, 1);
-    if (--left == 0 && (S & 1))   // (an odd reduction ends with half a stage: zeros)
+    --left;
 #pragma unroll
-      for (int r = 0; r < RF; ++r) xc[r] = make_uint4(0, 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    mul(xa, wa);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int j = 0; j < PARTS; ++j) {
+#pragma unroll
+      for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(xc, wc, cur, 1, i);
+      __builtin_amdgcn_sched_barrier(0);
+      mul(xa, wa, j * MN / PARTS, (j + 1) * MN / PARTS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // The stage in `cur`: the products of the stage before, in `prev`, are finished
   // while its first fragments are read; `prev`, which every wave has read by
@@ -319,11 +338,17 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): this wave's reads of `prev` are done
     wait_vm<(NST - 2) * LPW>();           // its part of `cur` has arrived
     barrier_only();
-    fetch(prev);
-    read(xa, wa, cur, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    mul(xc, wc);
-    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) {
+#pragma unroll
+      for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(xa, wa, cur, 0, i);
+#pragma unroll
+      for (int i = j * LPW / PARTS; i < (j + 1) * LPW / PARTS; ++i) fetch_one(prev, i);
+      __builtin_amdgcn_sched_barrier(0);
+      mul(xc, wc, j * MN / PARTS, (j + 1) * MN / PARTS);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    fetched();
     second(cur);
   };
   fetch(b0);
@@ -360,7 +385,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       }
     }
   }
-  mul(xc, wc);
+  if (S % 2 == 0) mul(xc, wc, 0, MN);   // (an odd reduction ends with half a stage)
   wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
 
   if constexpr (MODE == TM_LINEAR) {
@@ -511,12 +536,19 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   }
   TileArgs t{};
   t.l = a;
-  auto tiles = [&](int64_t m, int64_t n) { return ((a.T + m - 1) / m) * ((a.N + n - 1) / n); };
-  if constexpr (DT == DT_BF16)
-    if (tiles(256, 256) >= 256) return launch_tile<DT, TM_LINEAR, 256, 256, 4, 2, 2>(t, st);
-  if (tiles(128, 128) >= 512) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 2, 2>(t, st);
-  if (tiles(64, 64) >= 256) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 2>(t, st);
-  return launch_tile<DT, TM_LINEAR, 32, 64, 1, 4, 4>(t, st);
+  // The tile that finishes first: turns of the 256 CUs times what a turn costs
+  // (us over 4096 bf16 columns with every CU at work; one turn alone: 64 x 32 12
+  // us, 64 x 64 14, 128 x 128 26, 256 x 128 43).  33 rows x 6144: 64 x 32 11.8
+  // us, 64 x 64 13.4; 256 x 4096: 19.4, 14.4, 128 x 128 25.6; 513 x 4096: 64 x 64
+  // 35, 128 x 128 26, 256 x 128 43; 8192 x 11008: 128 x 128 780, 256 x 128 659,
+  // 256 x 256 (two turns fewer, but only one stage ahead) 689.
+  auto turns = [&](int64_t m, int64_t n) { return (((a.T + m - 1) / m) * ((a.N + n - 1) / n) + 255) / 256; };
+  const int64_t c1 = 10 * turns(64, 32), c2 = 13 * turns(64, 64), c3 = 27 * turns(128, 128), c4 = 46 * turns(256, 128);
+  const int64_t best = std::min(std::min(c1, c2), std::min(c3, c4));
+  if (best == c4) return launch_tile<DT, TM_LINEAR, 256, 128, 4, 2, 3>(t, st);
+  if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
+  if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 4>(t, st);
+  return launch_tile<DT, TM_LINEAR, 64, 32, 2, 2, 4>(t, st);
 }
 
 hipError_t run_linear(const LinearArgs& a, hipStream_t st) {
@@ -709,21 +741,33 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void ffn_down_kernel(FfnArgs a, co
 // ------------------------------------------------------- experts, many rows --
 
 // Sorts the pairs by expert and cuts every expert's run into row tiles of BM.
-// One workgroup: counts in LDS, offsets by a scan over the experts, places by
-// LDS counters again.  (The order of the pairs within an expert may differ from
-// run to run; every row's arithmetic is its own, so the results do not.)
-constexpr int PLAN_THREADS = 1024;
+// Workgroup b places the pairs of chunk b.  It needs the counts of all pairs and
+// of those before its chunk, and counts them itself (every workgroup reads all
+// ids, from L2): one launch and no wait between workgroups.  (65536 pairs: 61 us
+// in a single workgroup.)  The order of the pairs within an expert may differ
+// from run to run; every row's arithmetic is its own, so the results do not.
+constexpr int PLAN_THREADS = 1024, PLAN_CHUNK = 2048;
 static_assert(PLAN_THREADS >= ROUTE_MAX_E, "a thread per expert");
 __global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __restrict__ ids, int P, int E, int BM, FfnPlan p) {
   __shared__ int cnt[ROUTE_MAX_E], first[ROUTE_MAX_E], tiles[ROUTE_MAX_E];
-  const int t = threadIdx.x;
-  for (int e = t; e < E; e += PLAN_THREADS) cnt[e] = 0;
+  const int t = threadIdx.x, lo = blockIdx.x * PLAN_CHUNK, hi = min(P, lo + PLAN_CHUNK);
+  if (t < E) cnt[t] = 0;
   __syncthreads();
-  for (int i = t; i < P; i += PLAN_THREADS) {
-    const int e = ids[i];
-    if (e >= 0 && e < E) atomicAdd(&cnt[e], 1);
-  }
+  auto count = [&](int from, int to) {
+    for (int i = from + t; i < to; i += 4 * PLAN_THREADS) {
+      int e[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[j] = i + j * PLAN_THREADS < to ? ids[i + j * PLAN_THREADS] : -1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e[j] >= 0 && e[j] < E) atomicAdd(&cnt[e[j]], 1);
+    }
+    __syncthreads();
+  };
+  count(0, lo);
+  const int before = t < E ? cnt[t] : 0;
   __syncthreads();
+  count(lo, P);
   // inclusive scans of the counts and of the tiles
   int n = 0, own = 0;
   if (t < E) {
@@ -742,12 +786,14 @@ __global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __res
   }
   if (t < E) {
     const int p0 = first[t] - n, t0 = tiles[t] - own;
-    for (int i = 0; i < own; ++i) p.tile[t0 + i] = ExpertTile{t, p0 + i * BM, min(BM, n - i * BM)};
-    cnt[t] = p0;
-    if (t == E - 1) *p.ntile = tiles[t];
+    if (blockIdx.x == 0) {
+      for (int i = 0; i < own; ++i) p.tile[t0 + i] = ExpertTile{t, p0 + i * BM, min(BM, n - i * BM)};
+      if (t == E - 1) *p.ntile = tiles[t];
+    }
+    cnt[t] = p0 + before;
   }
   __syncthreads();
-  for (int i = t; i < P; i += PLAN_THREADS) {
+  for (int i = lo + t; i < hi; i += PLAN_THREADS) {
     const int e = ids[i];
     if (e >= 0 && e < E) p.order[atomicAdd(&cnt[e], 1)] = i;
   }
@@ -807,14 +853,11 @@ static hipError_t ffn_tiles_t(const TileArgs& t, hipStream_t st) {
     if ((e = launch_tile<DT, TM_UP, 32, 128, 1, 4, 4>(t, st)) != hipSuccess) return e;
     return launch_tile<DT, TM_DOWN, 32, 128, 1, 4, 4>(t, st);
   } else if constexpr (BM == 64) {
-    if ((e = launch_tile<DT, TM_UP, 64, 128, 2, 2, 3>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 64, 128, 2, 2, 3>(t, st);
-  } else if constexpr (BM == 128) {
-    if ((e = launch_tile<DT, TM_UP, 128, 128, 2, 2, 2>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 128, 128, 2, 2, 2>(t, st);
+    if ((e = launch_tile<DT, TM_UP, 64, 128, 2, 4, 4>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 64, 128, 2, 4, 4>(t, st);
   } else {
-    if ((e = launch_tile<DT, TM_UP, 256, 256, 4, 2, 2>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 256, 256, 4, 2, 2>(t, st);
+    if ((e = launch_tile<DT, TM_UP, 128, 256, 2, 4, 3>(t, st)) != hipSuccess) return e;
+    return launch_tile<DT, TM_DOWN, 128, 256, 2, 4, 3>(t, st);
   }
 }
 
@@ -831,17 +874,16 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   const int64_t avg = P / a.E;
-  const int BM = avg < 24 ? 32 : avg < 96 ? 64 : (avg < 256 || DT == DT_F32) ? 128 : 256;
+  const int BM = avg < 24 ? 32 : avg < 96 ? 64 : 128;
   TileArgs t{};
   t.f = a;
   t.p = pl;
   t.nrt = (int)ffn_tiles(P, a.E, BM);
-  hipLaunchKernelGGL(ffn_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
+  hipLaunchKernelGGL(ffn_plan_kernel, dim3((unsigned)((P + PLAN_CHUNK - 1) / PLAN_CHUNK)), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (BM == 32) e = ffn_tiles_t<DT, 32>(t, st);
   else if (BM == 64) e = ffn_tiles_t<DT, 64>(t, st);
-  else if (BM == 128) e = ffn_tiles_t<DT, 128>(t, st);
-  else if constexpr (DT == DT_BF16) e = ffn_tiles_t<DT, 256>(t, st);
+  else e = ffn_tiles_t<DT, 128>(t, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((ffn_sum_kernel<ODT>), dim3((unsigned)((a.d / 4 + 255) / 256) * a.T), dim3(256), 0, st, a, (const float*)pl.y);
   return hipGetLastError();
