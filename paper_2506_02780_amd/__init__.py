@@ -11,6 +11,7 @@ been built, importing this package raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -186,80 +187,90 @@ def make_moe_config(shape) -> EEMoeConfig:
 # stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given.
 
 _TYPES = {torch.float32: EE_F32, torch.bfloat16: EE_BF16}
+_ACT_OF = {a: i for i, a in enumerate(ACTIVATIONS)}
+_SCORE_OF = {a: i for i, a in enumerate(SCORES)}
+# (the plain call where the raw one is missing: it is 1.8 us slower, a seventh of a small call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _type(t: torch.Tensor, what: str) -> int:
-    try:
-        return _TYPES[t.dtype]
-    except KeyError:
-        raise EEError(EE_EINVAL, f"{what} must be float32 or bfloat16") from None
+def _refuse(what: str, shape, dtype, dev, t):
+    got = f"{list(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+    raise EEError(EE_EINVAL, f"{what} must be {list(shape)} {dtype} on cuda:{dev} (rows of unit column stride), not {got}")
 
 
-def _matrix(t: torch.Tensor, what: str, shape, dtype, dev) -> torch.Tensor:
-    """Checks a [rows, cols] operand of unit column stride; returns it."""
-    if t.dim() != 2 or tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev:
-        raise EEError(EE_EINVAL, f"{what} must be {list(shape)} {dtype} on {dev}, "
-                                 f"not {list(t.shape)} {t.dtype} on {t.device}")
-    if t.stride(1) != 1 and t.shape[1] > 1:
-        raise EEError(EE_EINVAL, f"{what} must have unit column stride")
-    return t
-
-
-def _whole(t: torch.Tensor, what: str, shape, dtype, dev) -> torch.Tensor:
-    """Checks a contiguous operand; returns it."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != dev or not t.is_contiguous():
-        raise EEError(EE_EINVAL, f"{what} must be contiguous {list(shape)} {dtype} on {dev}")
-    return t
-
-
-def _ld(t: torch.Tensor) -> int:
+def _rows_of(t, what: str, shape, dtype, dev) -> int:
+    """Checks a [rows, cols] operand of unit column stride; returns its row stride."""
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        _refuse(what, shape, dtype, dev, t)
+    rs, cs = t.stride()
+    if cs != 1 and shape[1] > 1:
+        _refuse(what, shape, dtype, dev, t)
     # (a single row may carry any stride)
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return rs if shape[0] > 1 or rs > shape[1] else shape[1]
 
 
-def _operator(fn, args, dev):
-    """Calls an operator on ``dev`` and its current stream."""
-    if dev.index == torch.cuda.current_device():
-        rc = fn(ctypes.byref(args), torch.cuda.current_stream(dev).cuda_stream)
+def _whole(t, what: str, shape, dtype, dev):
+    """Checks a contiguous operand."""
+    if (not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.get_device() != dev
+            or not t.is_contiguous()):
+        _refuse(what, shape, dtype, dev, t)
+
+
+def _operand(x, what: str):
+    """Device index and EE_* type of a call's first operand."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda:
+        raise EEError(EE_EINVAL, f"{what} must be a two-dimensional tensor on a GPU")
+    dt = _TYPES.get(x.dtype)
+    if dt is None:
+        raise EEError(EE_EINVAL, f"{what} must be float32 or bfloat16")
+    return x.get_device(), dt
+
+
+def _out_type(out_dtype, out, x):
+    odt = out_dtype or (x.dtype if out is None else out.dtype)
+    if odt not in _TYPES:
+        raise EEError(EE_EINVAL, "out_dtype must be float32 or bfloat16")
+    return odt
+
+
+def _operator(fn, args, dev: int):
+    """Calls an operator on GPU ``dev`` and its current stream."""
+    if dev == torch.cuda.current_device():
+        rc = fn(ctypes.byref(args), _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(ctypes.byref(args), torch.cuda.current_stream(dev).cuda_stream)
-    _check(rc)
-
-
-def _operand(x: torch.Tensor, what: str):
-    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.device.type != "cuda":
-        raise EEError(EE_EINVAL, f"{what} must be a two-dimensional tensor on a GPU")
-    return x.device
+            rc = fn(ctypes.byref(args), _raw_stream(dev))
+    if rc != EE_OK:
+        _check(rc)
 
 
 def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtype=None):
     """act(x w^T + bias) + residual (ee_linear).  x [rows, in] and w [out, in]
     in float32 or bfloat16, bias [out] float32, residual [rows, out] in the
     output's dtype (``out_dtype``: x's, or float32).  ``out`` may be the residual."""
-    dev = _operand(x, "x")
-    dt = _type(x, "x")
-    if act not in ACTIVATIONS:
+    dev, dt = _operand(x, "x")
+    code = _ACT_OF.get(act)
+    if code is None:
         raise EEError(EE_EINVAL, f"act must be one of {ACTIVATIONS}")
     if not isinstance(w, torch.Tensor) or w.dim() != 2:
         raise EEError(EE_EINVAL, "w must be [out, in]")
-    rows, cols, n = x.shape[0], x.shape[1], w.shape[0]
-    _matrix(x, "x", (rows, cols), x.dtype, dev)
-    _matrix(w, "w", (n, cols), x.dtype, dev)
-    odt = out_dtype or (out.dtype if out is not None else x.dtype)
+    rows, cols = x.shape
+    n = w.shape[0]
+    ldx = _rows_of(x, "x", (rows, cols), x.dtype, dev)
+    ldw = _rows_of(w, "w", (n, cols), x.dtype, dev)
+    odt = _out_type(out_dtype, out, x)
+    shape = (rows, n)
     if out is None:
-        out = torch.empty((rows, n), dtype=odt, device=dev)
+        out, ldy = x.new_empty(shape, dtype=odt), n
     else:
-        _matrix(out, "out", (rows, n), odt, dev)
+        ldy = _rows_of(out, "out", shape, odt, dev)
     if bias is not None:
         _whole(bias, "bias", (n,), torch.float32, dev)
-    if residual is not None:
-        _matrix(residual, "residual", (rows, n), odt, dev)
-    a = EELinearArgs(x.data_ptr(), w.data_ptr(), bias.data_ptr() if bias is not None else None,
-                     residual.data_ptr() if residual is not None else None, out.data_ptr(), _ld(x), _ld(w),
-                     _ld(residual) if residual is not None else 0, _ld(out), rows, cols, n, dt, _type(out, "out"),
-                     ACTIVATIONS.index(act))
-    _operator(ee_linear, a, dev)
+    ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
+    _operator(ee_linear, EELinearArgs(x.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+                                      None if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr,
+                                      ldy, rows, cols, n, dt, _TYPES[odt], code), dev)
     return out
 
 
@@ -267,22 +278,25 @@ def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize
               n_groups: int = 1, top_groups: int = 1, group_top: int = 1):
     """Experts and weights of every row of the router's logits [rows, experts]
     (ee_moe_route): (ids int32, weights float32), both [rows, top_k]."""
-    dev = _operand(logits, "logits")
-    dt = _type(logits, "logits")
-    if score not in SCORES:
+    dev, dt = _operand(logits, "logits")
+    code = _SCORE_OF.get(score)
+    if code is None:
         raise EEError(EE_EINVAL, f"score must be one of {SCORES}")
     rows, n = logits.shape
-    _matrix(logits, "logits", (rows, n), logits.dtype, dev)
+    ld = _rows_of(logits, "logits", (rows, n), logits.dtype, dev)
     if bias is not None:
         _whole(bias, "bias", (n,), torch.float32, dev)
     k = int(top_k)
-    ids = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
-    weights = torch.empty((rows, max(k, 0)), dtype=torch.float32, device=dev)
-    a = EEMoeRouteArgs(logits.data_ptr(), bias.data_ptr() if bias is not None else None, ids.data_ptr(),
-                       weights.data_ptr(), _ld(logits), rows, n, k, dt, SCORES.index(score), int(bool(renormalize)),
-                       int(n_groups), int(top_groups), int(group_top), float(scale))
-    _operator(ee_moe_route, a, dev)
+    shape = (rows, k if k > 0 else 0)
+    ids = logits.new_empty(shape, dtype=torch.int32)
+    weights = logits.new_empty(shape, dtype=torch.float32)
+    _operator(ee_moe_route, EEMoeRouteArgs(logits.data_ptr(), None if bias is None else bias.data_ptr(), ids.data_ptr(),
+                                           weights.data_ptr(), ld, rows, n, k, dt, code, 1 if renormalize else 0,
+                                           int(n_groups), int(top_groups), int(group_top), scale), dev)
     return ids, weights
+
+
+_ffn_workspace = functools.lru_cache(maxsize=1024)(ee_moe_ffn_workspace_bytes)   # (a function of its arguments)
 
 
 def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dtype=None, workspace=None):
@@ -292,33 +306,33 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     weights float32 [rows, top_k] as from ``moe_route``; residual and out
     [rows, d] in ``out_dtype`` (x's, or float32).  ``workspace``: a uint8 tensor
     of at least ee_moe_ffn_workspace_bytes, else one is allocated."""
-    dev = _operand(x, "x")
-    dt = _type(x, "x")
-    if not (isinstance(w_gate_up, torch.Tensor) and isinstance(w_down, torch.Tensor)
-            and w_gate_up.dim() == 3 and w_down.dim() == 3 and isinstance(ids, torch.Tensor) and ids.dim() == 2):
-        raise EEError(EE_EINVAL, "w_gate_up and w_down must be three-dimensional, ids [rows, top_k]")
-    (rows, d), (E, _, f), k = x.shape, w_down.shape, ids.shape[1]
-    _matrix(x, "x", (rows, d), x.dtype, dev)
+    dev, dt = _operand(x, "x")
+    if not (isinstance(w_down, torch.Tensor) and w_down.dim() == 3 and isinstance(ids, torch.Tensor) and ids.dim() == 2):
+        raise EEError(EE_EINVAL, "w_down must be [experts, d, ffn], ids [rows, top_k]")
+    rows, d = x.shape
+    E, _, f = w_down.shape
+    k = ids.shape[1]
+    ldx = _rows_of(x, "x", (rows, d), x.dtype, dev)
     _whole(w_gate_up, "w_gate_up", (E, 2 * f, d), x.dtype, dev)
     _whole(w_down, "w_down", (E, d, f), x.dtype, dev)
     _whole(ids, "ids", (rows, k), torch.int32, dev)
     _whole(weights, "weights", (rows, k), torch.float32, dev)
-    odt = out_dtype or (out.dtype if out is not None else x.dtype)
+    odt = _out_type(out_dtype, out, x)
+    shape = (rows, d)
     if out is None:
-        out = torch.empty((rows, d), dtype=odt, device=dev)
+        out, ldo = x.new_empty(shape, dtype=odt), d
     else:
-        _matrix(out, "out", (rows, d), odt, dev)
-    if residual is not None:
-        _matrix(residual, "residual", (rows, d), odt, dev)
+        ldo = _rows_of(out, "out", shape, odt, dev)
+    ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
     if workspace is None:
-        workspace = torch.empty(ee_moe_ffn_workspace_bytes(rows, E, k, d, f, dt), dtype=torch.uint8, device=dev)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-        raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on {dev}")
-    a = EEMoeFfnArgs(x.data_ptr(), w_gate_up.data_ptr(), w_down.data_ptr(), ids.data_ptr(), weights.data_ptr(),
-                     residual.data_ptr() if residual is not None else None, out.data_ptr(), workspace.data_ptr(),
-                     workspace.numel(), _ld(x), _ld(residual) if residual is not None else 0, _ld(out),
-                     rows, E, k, d, f, dt, _type(out, "out"))
-    _operator(ee_moe_ffn, a, dev)
+        workspace = x.new_empty(_ffn_workspace(rows, E, k, d, f, dt), dtype=torch.uint8)
+    elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or workspace.get_device() != dev
+          or not workspace.is_contiguous()):
+        raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")
+    _operator(ee_moe_ffn, EEMoeFfnArgs(x.data_ptr(), w_gate_up.data_ptr(), w_down.data_ptr(), ids.data_ptr(),
+                                       weights.data_ptr(), None if residual is None else residual.data_ptr(),
+                                       out.data_ptr(), workspace.data_ptr(), workspace.numel(), ldx, ldr, ldo, rows, E, k,
+                                       d, f, dt, _TYPES[odt]), dev)
     return out
 
 

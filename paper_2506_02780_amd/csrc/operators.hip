@@ -26,35 +26,65 @@ namespace ee {
 constexpr int STEP = 64;
 
 // acc[n] += (16 features of wp[n]) x (16 rows of xp) over S super-steps.  wp and
-// xp point to the lane's own 16 bytes of step 0.  Two buffers of D steps: the next
-// D steps are requested before the current ones are multiplied.
+// xp point to the lane's own 16 bytes of step 0.  D steps are in flight: a step's
+// registers are requested again as soon as it is multiplied.  Bound by the bytes
+// in flight (a wave's share of the weights is one chain: nothing else may be
+// multiplied meanwhile), so D is what the registers hold; whole turns of D
+// have no branch between their steps, where the compiler would wait for more
+// than the step needs (one decoded token through 8 experts, 2048 x 768: 25 us
+// with a test per step and two alternating sets of 8, 13 us).
+typedef const __attribute__((address_space(1))) unsigned char global_bytes;
+typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
 template <int DT, int NT, int D>
-__device__ __forceinline__ void chain(const unsigned char* const (&wp)[NT], const unsigned char* xp, int S,
+__device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], const unsigned char* xptr, int S,
                                       f32x4 (&acc)[NT]) {
-  uint4 wa[D][NT], xa[D], wb[D][NT], xb[D];
-  auto load = [&](uint4 (&w)[D][NT], uint4 (&x)[D], int s0) {
+  // (global pointers by type: through the loop the compiler loses that they
+  // are, and a flat load's wait drains all of them)
+  global_bytes *wp[NT], *xp = (global_bytes*)xptr;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) wp[n] = (global_bytes*)wptr[n];
+  uint4 w[D][NT], x[D];
+  auto load = [&](int i) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) w[i][n] = __builtin_bit_cast(uint4, *(global_u32x4*)(wp[n] + i * STEP));
+    x[i] = __builtin_bit_cast(uint4, *(global_u32x4*)(xp + i * STEP));
+    __builtin_amdgcn_sched_barrier(0);   // (requests in the order of their use: a wait then leaves the later ones out)
+  };
+  auto mul = [&](int i) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = mma<DT>(w[i][n], x[i], acc[n]);
+  };
+  auto next = [&]() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) wp[n] += D * STEP;
+    xp += D * STEP;
+  };
+  const int turns = S / D, rest = S % D;
+  if (turns) {
+#pragma unroll
+    for (int i = 0; i < D; ++i) load(i);
+    next();
+    for (int g = 1; g < turns; ++g) {
+#pragma unroll
+      for (int i = 0; i < D; ++i) {
+        mul(i);
+        load(i);
+      }
+      next();
+    }
 #pragma unroll
     for (int i = 0; i < D; ++i) {
-      const int s = min(s0 + i, S - 1);   // (past the end: the last step again, unused)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) w[i][n] = *reinterpret_cast<const uint4*>(wp[n] + (size_t)s * STEP);
-      x[i] = *reinterpret_cast<const uint4*>(xp + (size_t)s * STEP);
+      mul(i);
+      if (i < rest) load(i);
     }
-  };
-  auto mul = [&](const uint4 (&w)[D][NT], const uint4 (&x)[D], int s0) {
+  } else {
 #pragma unroll
     for (int i = 0; i < D; ++i)
-      if (s0 + i < S)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = mma<DT>(w[i][n], x[i], acc[n]);
-  };
-  load(wa, xa, 0);
-  for (int s = 0; s < S; s += 2 * D) {
-    load(wb, xb, s + D);
-    mul(wa, xa, s);
-    load(wa, xa, s + 2 * D);
-    mul(wb, xb, s + D);
+      if (i < rest) load(i);
   }
+#pragma unroll
+  for (int i = 0; i < D; ++i)
+    if (i < rest) mul(i);
 }
 
 // Four consecutive values, rounded to the type, from an aligned element index.
@@ -172,7 +202,8 @@ struct FfnPlan {
   ExpertTile* tile;    // [ntile]
   int* order;          // [pairs] pairs (row * k + slot) sorted by expert; skipped ones are not in it
   void* z;             // [pairs][F] dt, rows in sorted order
-  float* y;            // [pairs][d], rows by pair
+  float* y;            // [pairs][nc]: columns c0 .. c0 + nc - 1 of the down products, rows by pair
+  int c0, nc;
 };
 
 struct TileArgs {
@@ -244,7 +275,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       xb = reinterpret_cast<const unsigned char*>(a.f.x);
       wb = reinterpret_cast<const unsigned char*>(a.f.wgu) + (size_t)et.e * 2 * a.f.F * ldw;
     } else {
-      f0 = ft * BN;
+      f0 = a.p.c0 + ft * BN;
       ldx = (unsigned)a.f.F * ESZ;
       xb = reinterpret_cast<const unsigned char*>(a.p.z) + (size_t)et.p0 * ldx;
       wb = reinterpret_cast<const unsigned char*>(a.f.wd) + ((size_t)et.e * a.f.d + f0) * ldw;
@@ -417,11 +448,11 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     for (int r = 0; r < RF; ++r) {
       const int row = (wr * RF + r) * 16 + c;
       if (row >= rows) continue;
-      float* y = a.p.y + (size_t)a.p.order[et.p0 + row] * a.f.d;
+      float* y = a.p.y + (size_t)a.p.order[et.p0 + row] * a.p.nc;
 #pragma unroll
       for (int f = 0; f < FF; ++f) {
-        const int n = f0 + (wf * FF + f) * 16 + 4 * grp;
-        if (n < a.f.d) *reinterpret_cast<f32x4*>(y + n) = acc[f][r];
+        const int n = f0 - a.p.c0 + (wf * FF + f) * 16 + 4 * grp;
+        if (n < a.p.nc) *reinterpret_cast<f32x4*>(y + n) = acc[f][r];
       }
     }
   }
@@ -430,7 +461,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST>
 static hipError_t launch_tile(TileArgs a, hipStream_t st) {
   if (MODE == TM_LINEAR) a.nrt = (a.l.T + BM - 1) / BM;
-  const int cols = MODE == TM_LINEAR ? a.l.N : MODE == TM_UP ? 2 * a.f.F : a.f.d;
+  const int cols = MODE == TM_LINEAR ? a.l.N : MODE == TM_UP ? 2 * a.f.F : a.p.nc;
   a.nft = (cols + BN - 1) / BN;
   const int64_t n = (int64_t)a.nrt * a.nft;
   hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
@@ -440,20 +471,19 @@ static hipError_t launch_tile(TileArgs a, hipStream_t st) {
 
 // ------------------------------------------------------------------- linear --
 
-// One 16-feature tile per wave and 16 rows per workgroup.
+// At most 16 rows: one 16-feature tile per wave, a wave per workgroup (they
+// spread over more CUs than as four).
 template <int DT>
-__global__ __launch_bounds__(256) void linear_rows_kernel(LinearArgs a, int nblk) {
+__global__ __launch_bounds__(64, 2) void linear_rows_kernel(LinearArgs a) {
   constexpr int ESZ = Geo<DT>::ESZ;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, grp = lane >> 4;
-  const int nb = blockIdx.x % nblk, t0 = blockIdx.x / nblk * 16, n0 = (nb * 4 + wv) * 16;
-  if (n0 >= a.N) return;
+  const int lane = threadIdx.x, c = lane & 15, grp = lane >> 4, n0 = blockIdx.x * 16;
   const unsigned char* wp[1] = {reinterpret_cast<const unsigned char*>(a.w) +
                                 (size_t)min(n0 + c, a.N - 1) * a.ldw * ESZ + grp * 16};
   const unsigned char* xp =
-      reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + c, a.T - 1) * a.ldx * ESZ + grp * 16;
+      reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(c, a.T - 1) * a.ldx * ESZ + grp * 16;
   f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
-  chain<DT, 1, 8>(wp, xp, a.K / Geo<DT>::KS, acc);
-  linear_out(a, t0 + c, n0 + 4 * grp, acc[0], linear_bias(a, n0 + 4 * grp), linear_vec(a));
+  chain<DT, 1, 24>(wp, xp, a.K / Geo<DT>::KS, acc);
+  linear_out(a, c, n0 + 4 * grp, acc[0], linear_bias(a, n0 + 4 * grp), linear_vec(a));
 }
 
 // Products of few outputs (a router): a workgroup's eight waves each sum the
@@ -530,8 +560,7 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
     // small tiles until they fill the chip, then those that read the rows less often
     return rt * nt <= 2048 ? launch_narrow<DT, 1, 1>(a, st) : launch_narrow<DT, 2, 4>(a, st);
   if (a.T <= 16) {
-    const int nblk = (a.N + 63) / 64;
-    hipLaunchKernelGGL((linear_rows_kernel<DT>), dim3((unsigned)nblk * (unsigned)rt), dim3(256), 0, st, a, nblk);
+    hipLaunchKernelGGL((linear_rows_kernel<DT>), dim3((unsigned)nt), dim3(64), 0, st, a);
     return hipGetLastError();
   }
   TileArgs t{};
@@ -560,102 +589,169 @@ hipError_t run_linear(const LinearArgs& a, hipStream_t st) {
 
 constexpr int ROUTE_ROWS = 4;   // rows (waves) per workgroup
 
+// x of the lane n places on in its row of 16 (a rotation), as DPP: no LDS.
+template <int N> __device__ __forceinline__ uint32_t ror16(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xf, 0xf, false);
+}
+template <int N> __device__ __forceinline__ double ror16d(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)ror16<N>((uint32_t)(b >> 32)) << 32 | ror16<N>((uint32_t)b));
+}
+// f over the wave's 64 values of x, in every lane: rotations within the rows of
+// 16, then swaps of rows and of halves (both of a swap's results, in the same
+// order in every lane).
+template <class F> __device__ __forceinline__ uint32_t wave_all(uint32_t x, F f) {
+  x = f(x, ror16<1>(x));
+  x = f(x, ror16<2>(x));
+  x = f(x, ror16<4>(x));
+  x = f(x, ror16<8>(x));
+  const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(p[0], p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(q[0], q[1]);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  return wave_all(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ double lane_value(double x, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t hi = __builtin_amdgcn_readlane((int)(b >> 32), lane), lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// (rotations add in another order in every lane: lane 0's sum serves all, or equal
+// scores would differ in their last bit)
+__device__ __forceinline__ double wave_sum(double x) {
+  x += ror16d<1>(x);
+  x += ror16d<2>(x);
+  x += ror16d<4>(x);
+  x += ror16d<8>(x);
+  return ((lane_value(x, 0) + lane_value(x, 16)) + lane_value(x, 32)) + lane_value(x, 48);
+}
+// Unsigned integers in the order of the values (of which none is -0 or NaN).
+__device__ __forceinline__ uint64_t ordered(double x) {
+  const int64_t b = __builtin_bit_cast(int64_t, x);
+  return (uint64_t)(b ^ ((b >> 63) | INT64_MIN));
+}
+
 // One wave per row, experts e = 64 i + lane in registers.  Scores, biased
 // scores and the selection are float64 values of the logits, so which experts
 // a row gets never hangs on a float32 rounding.  The k experts are taken one
-// after another: a lane's best, then the wave's, the lowest index among equal
-// ones.
+// after another: every lane's best (the first of equal ones), then the wave's by
+// the upper halves of the ordered keys, by the lower halves and by the
+// index where those before leave several.  Bound by the instructions
+// of these steps (16384 rows of 256 sigmoid scores in 8 groups: 62 us with
+// shuffles through LDS and a lane per group, 32 us).
 template <int DT, int EPL>
 __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, t = blockIdx.x * ROUTE_ROWS + wv;
   __shared__ double gkey[ROUTE_ROWS][EPL * 64];
   const bool row = t < a.T;
   constexpr double NONE = -INFINITY;
+  float l[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = i * 64 + lane;
+    l[i] = row && e < a.E ? load_elt<DT>(a.logits, (size_t)t * a.ld + e) : -INFINITY;
+  }
   double s[EPL], key[EPL];
-  double mx = NONE;
+  float mx = -FLT_MAX;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    float l = row && e < a.E ? load_elt<DT>(a.logits, (size_t)t * a.ld + e) : -INFINITY;
-    if (!(l > -INFINITY)) l = -INFINITY;   // (NaN)
-    s[i] = (double)fminf(l, FLT_MAX);
-    mx = fmax(mx, s[i]);
+    l[i] = l[i] > -INFINITY ? fminf(l[i], FLT_MAX) : -INFINITY;   // (NaN: not selectable)
+    mx = fmaxf(mx, l[i]);
   }
-  for (int o = 32; o; o >>= 1) mx = fmax(mx, __shfl_xor(mx, o));
-  double sum = 0.0;
+  if (a.score == SCORE_SOFTMAX) {
+    mx = __uint_as_float(wave_all(__float_as_uint(mx), [](uint32_t x, uint32_t y) {
+      return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
+    }));
+    double sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const bool dead = s[i] == NONE;
-    key[i] = dead ? NONE : 0.0;
-    s[i] = dead ? 0.0 : a.score == SCORE_SOFTMAX ? exp(s[i] - mx) : 1.0 / (1.0 + exp(-s[i]));
-    sum += s[i];
-  }
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    if (a.score == SCORE_SOFTMAX && sum > 0.0) s[i] /= sum;
-    if (key[i] == NONE) continue;
-    double b = 0.0;
-    if (a.bias) {
-      const float f = a.bias[e];
-      b = f > -INFINITY ? (double)fminf(f, FLT_MAX) : NONE;   // (NaN: not selectable)
+    for (int i = 0; i < EPL; ++i) {
+      s[i] = l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)mx);
+      sum += s[i];
     }
-    key[i] = s[i] + b;
+    sum = wave_sum(sum);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) s[i] = sum > 0.0 ? s[i] / sum : 0.0;
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) s[i] = l[i] == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-(double)l[i]));
+  }
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = i * 64 + lane;
+    key[i] = l[i] == -INFINITY ? NONE : s[i];
+    if (a.bias && e < a.E) {
+      const float f = a.bias[e];
+      key[i] = f > -INFINITY ? key[i] + (double)fminf(f, FLT_MAX) : NONE;   // (NaN: not selectable)
+    }
   }
   if (a.groups > 1) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) gkey[wv][i * 64 + lane] = key[i];
     __syncthreads();
     const int per = a.E / a.groups;
-    double gs = NONE;   // lane g: the score of group g
-    if (lane < a.groups) {
-      double b1 = NONE, b2 = NONE;
-      for (int i = 0; i < per; ++i) {
-        const double v = gkey[wv][lane * per + i];
-        if (v > b1) { b2 = b1; b1 = v; }
-        else if (v > b2) b2 = v;
+    int lanes = 1;   // lanes per group
+    while (2 * lanes * a.groups <= 64) lanes *= 2;
+    const int g = lane / lanes;
+    double b1 = NONE, b2 = NONE;   // the group's best two keys
+    if (g < a.groups)
+      for (int i = lane % lanes; i < per; i += lanes) {
+        const double v = gkey[wv][g * per + i];
+        b2 = fmax(b2, fmin(b1, v));
+        b1 = fmax(b1, v);
       }
-      gs = a.group_top == 2 && b2 > NONE ? b1 + b2 : b1;
+    for (int o = 1; o < lanes; o <<= 1) {
+      const double c1 = __shfl_xor(b1, o), c2 = __shfl_xor(b2, o);
+      b2 = fmax(fmin(b1, c1), fmax(b2, c2));
+      b1 = fmax(b1, c1);
     }
+    const double gs = a.group_top == 2 && b2 > NONE ? b1 + b2 : b1;
     // groups that come before this one: better, or equal with a lower index
     int before = 0;
-    for (int g = 0; g < a.groups; ++g) {
-      const double o = __shfl(gs, g);
-      before += o > gs || (o == gs && g < lane);
+    for (int h = 0; h < a.groups; ++h) {
+      const double o = lane_value(gs, h * lanes);
+      before += o > gs || (o == gs && h < g);
     }
-    const unsigned long long keep = __ballot(lane < a.groups && before < a.top_groups);
+    const unsigned long long keep = __ballot(g < a.groups && before < a.top_groups);
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       const int e = i * 64 + lane;
-      if (e < a.E && !((keep >> (e / per)) & 1ull)) key[i] = NONE;
+      if (e < a.E && !((keep >> (e / per * lanes)) & 1ull)) key[i] = NONE;
     }
   }
   int id = -1;        // lane j: the expert of slot j and its score
-  double w = 0.0;
+  double w = 0.0, tot = 0.0;
   for (int j = 0; j < a.k; ++j) {
-    double best = NONE;
-    int at = 0x7fffffff;
-    double sc = 0.0;
+    double best = key[0], sc = s[0];
+    int at = lane;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i)
+    for (int i = 1; i < EPL; ++i)
       if (key[i] > best) { best = key[i]; at = i * 64 + lane; sc = s[i]; }
-    for (int o = 32; o; o >>= 1) {
-      const double b = __shfl_xor(best, o), bs = __shfl_xor(sc, o);
-      const int ba = __shfl_xor(at, o);
-      if (b > best || (b == best && ba < at)) { best = b; at = ba; sc = bs; }
+    const uint64_t o = ordered(best);
+    const uint32_t hi = (uint32_t)(o >> 32), lo = (uint32_t)o;
+    const uint32_t top = wave_max(hi);
+    unsigned long long m = __ballot(hi == top);
+    if (m & (m - 1)) {
+      const uint32_t low = wave_max(hi == top ? lo : 0u);
+      m = __ballot(hi == top && lo == low);
+      if (m & (m - 1)) {   // equal keys: the lowest index
+        const bool in = (m >> lane) & 1ull;
+        const uint32_t inv = wave_max(in ? ~(uint32_t)at : 0u);
+        m = __ballot(in && ~(uint32_t)at == inv);
+      }
     }
-    if (best == NONE) break;
-    if (lane == j) { id = at; w = sc; }
+    const int win = __ffsll(m) - 1;
+    if (lane_value(best, win) == NONE) break;   // none left
+    const int e = __builtin_amdgcn_readlane(at, win);
+    const double v = lane_value(sc, win);
+    tot += v;
+    if (lane == j) { id = e; w = v; }
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
-      if (at == i * 64 + lane) key[i] = NONE;
+      if (e == i * 64 + lane) key[i] = NONE;
   }
-  if (a.renorm) {
-    double tot = 0.0;
-    for (int j = 0; j < a.k; ++j) tot += __shfl(w, j);
-    w = tot > 0.0 ? w / tot : 0.0;
-  }
+  if (a.renorm) w = tot > 0.0 ? w / tot : 0.0;
   if (row && lane < a.k) {
     a.ids[(size_t)t * a.k + lane] = id;
     a.weights[(size_t)t * a.k + lane] = (float)(w * (double)a.scale);
@@ -684,21 +780,22 @@ hipError_t run_route(const RouteArgs& a, hipStream_t st) {
 // dtype: it is the down product's operand.  One 16-feature tile of gate and of
 // up per wave; all 16 columns of the product hold the pair's row.
 template <int DT>
-__global__ __launch_bounds__(256) void ffn_up_kernel(FfnArgs a, void* z, int nblk) {
+__global__ __launch_bounds__(64, 2) void ffn_up_kernel(FfnArgs a, void* z, int nblk) {
   constexpr int ESZ = Geo<DT>::ESZ;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, grp = lane >> 4;
-  const int p = blockIdx.x / nblk, f0 = (blockIdx.x % nblk * 4 + wv) * 16;
+  const int lane = threadIdx.x, c = lane & 15, grp = lane >> 4;
+  const int p = blockIdx.x / nblk, f0 = blockIdx.x % nblk * 16;
   const int e = a.ids[p];
-  if (f0 >= a.F || e < 0 || e >= a.E) return;
+  if (e < 0 || e >= a.E) return;
   const size_t rb = (size_t)a.d * ESZ;
   const unsigned char* w = reinterpret_cast<const unsigned char*>(a.wgu) + ((size_t)e * 2 * a.F + f0 + c) * rb + grp * 16;
   const unsigned char* wp[2] = {w, w + (size_t)a.F * rb};
   const unsigned char* xp = reinterpret_cast<const unsigned char*>(a.x) + (size_t)(p / a.k) * a.ldx * ESZ + grp * 16;
   f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-  chain<DT, 2, 8>(wp, xp, a.d / Geo<DT>::KS, acc);
-  if (c == 0)
+  chain<DT, 2, 16>(wp, xp, a.d / Geo<DT>::KS, acc);
+  f32x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_elt<DT>(z, (size_t)p * a.F + f0 + 4 * grp + i, silu(acc[0][i]) * acc[1][i]);
+  for (int i = 0; i < 4; ++i) v[i] = silu(acc[0][i]) * acc[1][i];
+  if (c == 0) store4<DT>(z, (size_t)p * a.F + f0 + 4 * grp, v);
 }
 
 constexpr int DOWN_WAVES = 8;
@@ -706,7 +803,7 @@ constexpr int DOWN_WAVES = 8;
 // out[t] = sum_j w_j (z_j Wd^T) + res of 16 features of one row: a wave per
 // slot, the slots' products joined in slot order.
 template <int DT, int ODT>
-__global__ __launch_bounds__(DOWN_WAVES * 64) void ffn_down_kernel(FfnArgs a, const void* z, int nblk) {
+__global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a, const void* z, int nblk) {
   constexpr int ESZ = Geo<DT>::ESZ;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, grp = lane >> 4;
   const int t = blockIdx.x / nblk, n0 = blockIdx.x % nblk * 16;
@@ -719,7 +816,7 @@ __global__ __launch_bounds__(DOWN_WAVES * 64) void ffn_down_kernel(FfnArgs a, co
     const unsigned char* wp[1] = {reinterpret_cast<const unsigned char*>(a.wd) + ((size_t)e * a.d + n0 + c) * rb + grp * 16};
     const unsigned char* zp = reinterpret_cast<const unsigned char*>(z) + p * rb + grp * 16;
     f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
-    chain<DT, 1, 8>(wp, zp, a.F / Geo<DT>::KS, acc);
+    chain<DT, 1, 24>(wp, zp, a.F / Geo<DT>::KS, acc);
     if (c == 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[j][4 * grp + i] = acc[0][i];
@@ -799,26 +896,37 @@ __global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __res
   }
 }
 
-// out[t] = sum_j w_j y[t k + j] + res, slots in order, four columns per thread.
+// out[t] = sum_j w_j y[t k + j] + res, slots in order, of columns c0 .. c0 + nc - 1,
+// four per thread.  Eight slots are requested at once.
 template <int ODT>
-__global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a, const float* __restrict__ y) {
-  const int per = (a.d / 4 + 255) / 256, t = blockIdx.x / per, n = (blockIdx.x % per * 256 + threadIdx.x) * 4;
-  if (n >= a.d) return;
+__global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a, FfnPlan p) {
+  const int per = (p.nc / 4 + 255) / 256, t = blockIdx.x / per, n = (blockIdx.x % per * 256 + threadIdx.x) * 4;
+  if (n >= p.nc || t >= a.T) return;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < a.k; ++j) {
-    const size_t p = (size_t)t * a.k + j;
-    const int e = a.ids[p];
-    if (e < 0 || e >= a.E) continue;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(y + p * a.d + n);
-    const float w = a.weights[p];
+  for (int j0 = 0; j0 < a.k; j0 += 8) {
+    f32x4 v[8];
+    float w[8];
+    bool on[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = fmaf(w, v[i], o[i]);
+    for (int j = 0; j < 8; ++j) {
+      const size_t q = (size_t)t * a.k + min(j0 + j, a.k - 1);
+      const int e = a.ids[q];
+      on[j] = j0 + j < a.k && e >= 0 && e < a.E;
+      w[j] = a.weights[q];
+      if (on[j]) v[j] = *reinterpret_cast<const f32x4*>(p.y + q * p.nc + n);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (on[j])
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(w[j], v[j][i], o[i]);
   }
+  const size_t c = p.c0 + n;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float u = o[i];
-    if (a.res) u += load_elt<ODT>(a.res, (size_t)t * a.ldr + n + i);
-    store_elt<ODT>(a.out, (size_t)t * a.ldo + n + i, u);
+    if (a.res) u += load_elt<ODT>(a.res, (size_t)t * a.ldr + c + i);
+    store_elt<ODT>(a.out, (size_t)t * a.ldo + c + i, u);
   }
 }
 
@@ -828,10 +936,18 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 size_t ffn_tiles(int64_t P, int E, int BM) { return (size_t)(P / BM + std::min<int64_t>(P, E)); }
 constexpr int MIN_BM = 32;
 
+// Columns of the down products that are held at once: what stays in the 256 MB
+// Infinity Cache between the product and its sum, in whole tiles.
+constexpr size_t Y_BYTES = size_t(256) << 20;
+int ffn_columns(int64_t P, int d) {
+  const int64_t n = (int64_t)(Y_BYTES / 4) / P / 256 * 256;
+  return (int)std::min<int64_t>(d, std::max<int64_t>(256, n));
+}
+
 size_t ffn_workspace(int T, int E, int k, int d, int F, int dt) {
   const size_t P = (size_t)T * k;
   return align256(4) + align256(ffn_tiles(P, E, MIN_BM) * sizeof(ExpertTile)) + align256(P * 4) +
-         align256(P * F * esz_of(dt)) + align256(P * d * 4);
+         align256(P * F * esz_of(dt)) + align256(P * (P ? ffn_columns(P, d) : 0) * 4);
 }
 
 static FfnPlan ffn_plan(const FfnArgs& a) {
@@ -843,22 +959,22 @@ static FfnPlan ffn_plan(const FfnArgs& a) {
   p.order = reinterpret_cast<int*>(ws); ws += align256(P * 4);
   p.z = ws; ws += align256(P * a.F * esz_of(a.dt));
   p.y = reinterpret_cast<float*>(ws);
+  p.c0 = 0;
+  p.nc = ffn_columns(P, a.d);
   return p;
 }
 
-template <int DT, int BM>
-static hipError_t ffn_tiles_t(const TileArgs& t, hipStream_t st) {
-  hipError_t e;
-  if constexpr (BM == 32) {
-    if ((e = launch_tile<DT, TM_UP, 32, 128, 1, 4, 4>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 32, 128, 1, 4, 4>(t, st);
-  } else if constexpr (BM == 64) {
-    if ((e = launch_tile<DT, TM_UP, 64, 128, 2, 4, 4>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 64, 128, 2, 4, 4>(t, st);
-  } else {
-    if ((e = launch_tile<DT, TM_UP, 128, 256, 2, 4, 3>(t, st)) != hipSuccess) return e;
-    return launch_tile<DT, TM_DOWN, 128, 256, 2, 4, 3>(t, st);
+template <int DT, int ODT, int BM, int BN, int WR, int WF, int NST>
+static hipError_t ffn_tiles_t(TileArgs t, hipStream_t st) {
+  hipError_t e = launch_tile<DT, TM_UP, BM, BN, WR, WF, NST>(t, st);
+  const int nc = t.p.nc;
+  for (t.p.c0 = 0; t.p.c0 < t.f.d && e == hipSuccess; t.p.c0 += nc) {
+    t.p.nc = std::min(nc, t.f.d - t.p.c0);
+    if ((e = launch_tile<DT, TM_DOWN, BM, BN, WR, WF, NST>(t, st)) != hipSuccess) break;
+    hipLaunchKernelGGL((ffn_sum_kernel<ODT>), dim3((unsigned)((t.p.nc / 4 + 255) / 256) * t.f.T), dim3(256), 0, st, t.f, t.p);
+    e = hipGetLastError();
   }
+  return e;
 }
 
 template <int DT, int ODT>
@@ -867,8 +983,8 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
   hipError_t e;
   FfnPlan pl = ffn_plan(a);
   if (P <= 64) {
-    const int ub = (a.F + 63) / 64, db = a.d / 16;
-    hipLaunchKernelGGL((ffn_up_kernel<DT>), dim3((unsigned)ub * P), dim3(256), 0, st, a, pl.z, ub);
+    const int ub = a.F / 16, db = a.d / 16;
+    hipLaunchKernelGGL((ffn_up_kernel<DT>), dim3((unsigned)ub * P), dim3(64), 0, st, a, pl.z, ub);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((ffn_down_kernel<DT, ODT>), dim3((unsigned)db * a.T), dim3(DOWN_WAVES * 64), 0, st, a, (const void*)pl.z, db);
     return hipGetLastError();
@@ -881,12 +997,9 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
   t.nrt = (int)ffn_tiles(P, a.E, BM);
   hipLaunchKernelGGL(ffn_plan_kernel, dim3((unsigned)((P + PLAN_CHUNK - 1) / PLAN_CHUNK)), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (BM == 32) e = ffn_tiles_t<DT, 32>(t, st);
-  else if (BM == 64) e = ffn_tiles_t<DT, 64>(t, st);
-  else e = ffn_tiles_t<DT, 128>(t, st);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((ffn_sum_kernel<ODT>), dim3((unsigned)((a.d / 4 + 255) / 256) * a.T), dim3(256), 0, st, a, (const float*)pl.y);
-  return hipGetLastError();
+  if (BM == 32) return ffn_tiles_t<DT, ODT, 32, 128, 1, 4, 4>(t, st);
+  if (BM == 64) return ffn_tiles_t<DT, ODT, 64, 128, 2, 4, 4>(t, st);
+  return ffn_tiles_t<DT, ODT, 128, 256, 2, 4, 3>(t, st);
 }
 
 hipError_t run_ffn(const FfnArgs& a, hipStream_t st) {
