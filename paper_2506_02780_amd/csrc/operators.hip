@@ -217,8 +217,10 @@ struct TileArgs {
 // stages of 128 bytes of a row (two super-steps), NST stages deep.  What bounds
 // a large product is that every wave reads its fragments from LDS while the
 // matrix cores run: a wave of RF x FF fragments reads RF + FF per RF FF matrix
-// instructions, so the largest tile (256 x 256, eight waves of 64 x 128) takes
-// all of the registers of two waves per SIMD.
+// instructions.  The largest tile, 128 x 256 with eight waves of 64 x 64, keeps two
+// stages in flight and the matrix cores busy two thirds of the clocks; with
+// all CUs at work the clock itself falls to about 1.9 GHz (the same tile alone:
+// 0.75 of the time).
 //   * Stages arrive by direct loads to LDS; each load takes eight rows of 128
 //     bytes (whole lines), the 16-byte pieces of row r at place piece ^ (r / 2
 //     % 8), so that the 16 rows that a fragment read touches fall on all banks.
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   const int ntile = nrt * a.nft, per = (ntile + 7) / 8, at = (int)(blockIdx.x >> 3);
   const int tile = (int)(blockIdx.x & 7) * per + at;
   if (at >= per || tile >= ntile) return;
-  constexpr int GR = 8;
+  constexpr int GR = BN > BM ? 4 : 8;   // (8192 x 11008, 128 x 256 tiles: 608 us with 4, 670 with 8, 680 with 32)
   const int gsz = GR * a.nft, gi = tile / gsz, gr0 = gi * GR, gh = min(GR, nrt - gr0), gj = tile - gi * gsz;
   const int rt = gr0 + gj % gh, ft = gj / gh;
 
@@ -567,14 +569,14 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   t.l = a;
   // The tile that finishes first: turns of the 256 CUs times what a turn costs
   // (us over 4096 bf16 columns with every CU at work; one turn alone: 64 x 32 12
-  // us, 64 x 64 14, 128 x 128 26, 256 x 128 43).  33 rows x 6144: 64 x 32 11.8
+  // us, 64 x 64 14, 128 x 128 26, 128 x 256 43).  33 rows x 6144: 64 x 32 11.8
   // us, 64 x 64 13.4; 256 x 4096: 19.4, 14.4, 128 x 128 25.6; 513 x 4096: 64 x 64
-  // 35, 128 x 128 26, 256 x 128 43; 8192 x 11008: 128 x 128 780, 256 x 128 659,
-  // 256 x 256 (two turns fewer, but only one stage ahead) 689.
+  // 35, 128 x 128 26, 128 x 256 43; 8192 x 11008: 128 x 128 780, 128 x 256 608,
+  // 256 x 256 (half as many turns, one stage ahead instead of two) 690.
   auto turns = [&](int64_t m, int64_t n) { return (((a.T + m - 1) / m) * ((a.N + n - 1) / n) + 255) / 256; };
-  const int64_t c1 = 10 * turns(64, 32), c2 = 13 * turns(64, 64), c3 = 27 * turns(128, 128), c4 = 46 * turns(256, 128);
+  const int64_t c1 = 10 * turns(64, 32), c2 = 13 * turns(64, 64), c3 = 27 * turns(128, 128), c4 = 46 * turns(128, 256);
   const int64_t best = std::min(std::min(c1, c2), std::min(c3, c4));
-  if (best == c4) return launch_tile<DT, TM_LINEAR, 256, 128, 4, 2, 3>(t, st);
+  if (best == c4) return launch_tile<DT, TM_LINEAR, 128, 256, 2, 4, 3>(t, st);
   if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
   if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 4>(t, st);
   return launch_tile<DT, TM_LINEAR, 64, 32, 2, 2, 4>(t, st);
