@@ -6,8 +6,9 @@
 // so a row's result never depends on the other rows of a call):
 //   * every product element is one fp32 accumulator that takes the reduction's
 //     super-steps (32 columns in bf16, 16 in fp32: one fragment) in order; a
-//     linear of at most NARROW outputs (a router) instead sums eight such
-//     chains, in order, whatever the number of rows;
+//     linear sums several such chains, in order, their number a function of
+//     the reduction's length (linear_chains) or, for at most NARROW outputs (a
+//     router), eight;
 //   * an experts' row is sum_j fma(w_j, y_j) over its slots in order, in fp32.
 
 #include "operators.h"
@@ -25,7 +26,7 @@ namespace ee {
 // bytes per lane group.
 constexpr int STEP = 64;
 
-// acc[n] += (16 features of wp[n]) x (16 rows of xp) over S super-steps.  wp and
+// acc[n][m] += (16 features of wp[n]) x (16 rows of xp[m]) over S super-steps.  wp and
 // xp point to the lane's own 16 bytes of step 0.  D steps are in flight: a step's
 // registers are requested again as soon as it is multiplied.  Bound by the bytes
 // in flight (a wave's share of the weights is one chain: nothing else may be
@@ -35,29 +36,35 @@ constexpr int STEP = 64;
 // with a test per step and two alternating sets of 8, 13 us).
 typedef const __attribute__((address_space(1))) unsigned char global_bytes;
 typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
-template <int DT, int NT, int D>
-__device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], const unsigned char* xptr, int S,
-                                      f32x4 (&acc)[NT]) {
+template <int DT, int NT, int MT, int D>
+__device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], const unsigned char* const (&xptr)[MT], int S,
+                                      f32x4 (&acc)[NT][MT]) {
   // (global pointers by type: through the loop the compiler loses that they
   // are, and a flat load's wait drains all of them)
-  global_bytes *wp[NT], *xp = (global_bytes*)xptr;
+  global_bytes *wp[NT], *xp[MT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) wp[n] = (global_bytes*)wptr[n];
-  uint4 w[D][NT], x[D];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) xp[m] = (global_bytes*)xptr[m];
+  uint4 w[D][NT], x[D][MT];
   auto load = [&](int i) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) w[i][n] = __builtin_bit_cast(uint4, *(global_u32x4*)(wp[n] + i * STEP));
-    x[i] = __builtin_bit_cast(uint4, *(global_u32x4*)(xp + i * STEP));
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x[i][m] = __builtin_bit_cast(uint4, *(global_u32x4*)(xp[m] + i * STEP));
     __builtin_amdgcn_sched_barrier(0);   // (requests in the order of their use: a wait then leaves the later ones out)
   };
   auto mul = [&](int i) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = mma<DT>(w[i][n], x[i], acc[n]);
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[n][m] = mma<DT>(w[i][n], x[i][m], acc[n][m]);
   };
   auto next = [&]() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) wp[n] += D * STEP;
-    xp += D * STEP;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) xp[m] += D * STEP;
   };
   const int turns = S / D, rest = S % D;
   if (turns) {
@@ -126,36 +133,52 @@ __device__ __forceinline__ f32x4 activate4(f32x4 v, int act) {
   return u;
 }
 
-// Bias, activation and residual of features n .. n + 3 of row t, and the store.
-// vec: rows of y and residual are aligned for four values at a time.
-__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v, f32x4 bias, bool vec) {
-  if (t >= a.T || n >= a.N) return;
-  v = activate4(v + bias, a.act);
-  const size_t yo = (size_t)t * a.ldy + n, ro = (size_t)t * a.ldr + n;
+// The residual of features n .. n + 3 of row t (zeros where there is none), and
+// the bias, activation, residual and store of a product.  vec: rows of y and
+// residual are aligned for four values at a time.
+__device__ __forceinline__ f32x4 linear_residual(const LinearArgs& a, int t, int n, bool vec) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (!a.res || t >= a.T || n >= a.N) return v;
+  const size_t o = (size_t)t * a.ldr + n;
   if (a.odt == DT_BF16) {
-    const uint16_t* res = reinterpret_cast<const uint16_t*>(a.res);
-    uint16_t* y = reinterpret_cast<uint16_t*>(a.y);
+    const uint16_t* res = reinterpret_cast<const uint16_t*>(a.res) + o;
     if (vec) {
-      if (res) {
-        const uint2 r = *reinterpret_cast<const uint2*>(res + ro);
-        v += f32x4{bf2f(r.x & 0xffff), bf2f(r.x >> 16), bf2f(r.y & 0xffff), bf2f(r.y >> 16)};
-      }
-      *reinterpret_cast<uint2*>(y + yo) = make_uint2(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]));
+      const uint2 r = *reinterpret_cast<const uint2*>(res);
+      return f32x4{bf2f(r.x & 0xffff), bf2f(r.x >> 16), bf2f(r.y & 0xffff), bf2f(r.y >> 16)};
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < a.N) v[i] = bf2f(res[i]);
+  } else {
+    const float* res = reinterpret_cast<const float*>(a.res) + o;
+    if (vec) return *reinterpret_cast<const f32x4*>(res);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < a.N) v[i] = res[i];
+  }
+  return v;
+}
+__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v, f32x4 bias, f32x4 res, bool vec) {
+  if (t >= a.T || n >= a.N) return;
+  v = activate4(v + bias, a.act) + res;
+  const size_t o = (size_t)t * a.ldy + n;
+  if (a.odt == DT_BF16) {
+    uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + o;
+    if (vec) {
+      *reinterpret_cast<uint2*>(y) = make_uint2(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (n + i < a.N) y[yo + i] = (uint16_t)f2bf_bits(res ? v[i] + bf2f(res[ro + i]) : v[i]);
+        if (n + i < a.N) y[i] = (uint16_t)f2bf_bits(v[i]);
     }
   } else {
-    const float* res = reinterpret_cast<const float*>(a.res);
-    float* y = reinterpret_cast<float*>(a.y);
+    float* y = reinterpret_cast<float*>(a.y) + o;
     if (vec) {
-      if (res) v += *reinterpret_cast<const f32x4*>(res + ro);
-      *reinterpret_cast<f32x4*>(y + yo) = v;
+      *reinterpret_cast<f32x4*>(y) = v;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (n + i < a.N) y[yo + i] = res ? v[i] + res[ro + i] : v[i];
+        if (n + i < a.N) y[i] = v[i];
     }
   }
 }
@@ -170,6 +193,19 @@ __device__ __forceinline__ f32x4 linear_bias(const LinearArgs& a, int n) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) b[i] = a.bias[min(n + i, a.N - 1)];
   return b;
+}
+
+// Chains of a linear's reduction over S super-steps: one for every 64 (2048 bf16
+// columns), at most eight, each a run of whole groups of four.  They let a product
+// of few rows spread a long reduction over several waves; the others fold one
+// accumulator into another at a chain's end.  First super-step of chain j.
+constexpr int MAX_CHAINS = 8;
+__host__ __device__ __forceinline__ int linear_chains(int S) {
+  const int c = S / 64;
+  return c < 1 ? 1 : c > MAX_CHAINS ? MAX_CHAINS : c;
+}
+__host__ __device__ __forceinline__ int chain_start(int j, int S, int chains) {
+  return j == chains ? S : j * (S / 4) / chains * 4;   // (S <= 2^16)
 }
 
 // -------------------------------------------------------------- tile products --
@@ -214,29 +250,35 @@ struct TileArgs {
 };
 
 // Products of BM rows with BN rows of weights, both streamed through LDS in
-// stages of 128 bytes of a row (two super-steps), NST stages deep.  What bounds
+// stages of SPS super-steps (64 bytes of a row each), NST stages deep.  What bounds
 // a large product is that every wave reads its fragments from LDS while the
 // matrix cores run: a wave of RF x FF fragments reads RF + FF per RF FF matrix
 // instructions.  The largest tile, 128 x 256 with eight waves of 64 x 64, keeps two
 // stages in flight and the matrix cores busy two thirds of the clocks; with
 // all CUs at work the clock itself falls to about 1.9 GHz (the same tile alone:
 // 0.75 of the time).
-//   * Stages arrive by direct loads to LDS; each load takes eight rows of 128
-//     bytes (whole lines), the 16-byte pieces of row r at place piece ^ (r / 2
-//     % 8), so that the 16 rows that a fragment read touches fall on all banks.
-//   * A stage's two super-steps are read one ahead of the matrix instructions
-//     that use them, across the stage's barrier too.
+//   * Stages arrive by direct loads to LDS, each of whole lines (SPS = 2: eight
+//     rows of 128 bytes; 4: four of 256).  The 16-byte pieces of row r stand at
+//     place piece ^ (r / 2 % 8) or piece ^ (r % 16), so that the 16 rows that a
+//     fragment read touches fall on all banks.
+//   * Fragments are read one super-step ahead of the matrix instructions
+//     that use them, across the stages' barriers too.
+//   * SPS = 4 halves the barriers, which small tiles wait for most, and needs a
+//     multiple of four super-steps; SPS = 2 takes any number.
 // Rows past the end repeat the last one; their results are not stored.
-template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST>
+template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST, int SPS>
 __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   constexpr int ESZ = Geo<DT>::ESZ, WAVES = WR * WF, RF = BM / WR / 16, FF = BN / WF / 16;
-  constexpr int LPW = (BM + BN) / 8 / WAVES;   // loads per wave and stage
-  constexpr int STAGE = (BM + BN) * 8;         // 16-byte pieces of a stage
-  static_assert((BM + BN) / 8 % WAVES == 0, "every wave loads as much");
+  constexpr int PPR = 4 * SPS, RPL = 64 / PPR;   // 16-byte pieces of a row's stage, rows per load
+  constexpr int LPW = (BM + BN) / RPL / WAVES;   // loads per wave and stage
+  constexpr int STAGE = (BM + BN) * PPR;         // pieces of a stage
+  static_assert(SPS == 2 || SPS == 4, "two fragment sets in turn, rows of 8 or 16 pieces");
+  static_assert((BM + BN) % (RPL * WAVES) == 0 && BM % RPL == 0, "every wave loads as much");
   static_assert(MODE != TM_UP || FF % 2 == 0, "a wave owns gate and up tiles of the same features");
+  static_assert(NST == 3 || NST == 4, "buffers in turn");
   static_assert((NST - 1) * LPW < 64, "outstanding loads are counted in six bits");
   // (arrays of their own: the compiler then knows that a request into one does not touch the others)
-  __shared__ uint4 b0[STAGE], b1[STAGE], b2[NST > 2 ? STAGE : 1], b3[NST > 3 ? STAGE : 1];
+  __shared__ uint4 b0[STAGE], b1[STAGE], b2[STAGE], b3[NST > 3 ? STAGE : 1];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
   const int wr = wv / WF, wf = wv % WF;
 
@@ -283,16 +325,17 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       wb = reinterpret_cast<const unsigned char*>(a.f.wd) + ((size_t)et.e * a.f.d + f0) * ldw;
     }
   }
-  const int stages = (S + 1) / 2;
+  const int stages = (S + SPS - 1) / SPS;
+  auto swizzle = [](int r) { return SPS == 2 ? (r >> 1) & 7 : r & 15; };
 
   // this lane's piece of each of the wave's loads
   unsigned off[LPW];
 #pragma unroll
   for (int i = 0; i < LPW; ++i) {
     const int inst = wv * LPW + i;
-    int r = inst * 8 + (lane >> 3);
-    const unsigned piece = ((lane & 7) ^ ((r >> 1) & 7)) * 16;
-    if (inst < BM / 8) {
+    int r = inst * RPL + lane / PPR;
+    const unsigned piece = ((lane % PPR) ^ swizzle(r)) * 16;
+    if (inst < BM / RPL) {
       r = min(r, rows - 1);
       if constexpr (MODE == TM_UP) r = a.p.order[et.p0 + r] / a.f.k;
       off[i] = (unsigned)r * ldx + piece;
@@ -313,8 +356,8 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   int next = 0;
   auto fetch_one = [&](uint4* buf, int i) {
     const int inst = wv * LPW + i;
-    const unsigned over = 2 * next + 1 == S && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
-    const unsigned char* src = (inst < BM / 8 ? xb : wb) + (size_t)next * 128;
+    const unsigned over = SPS == 2 && 2 * next + 1 == S && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
+    const unsigned char* src = (inst < BM / RPL ? xb : wb) + (size_t)next * (SPS * STEP);
     __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
   };
   auto fetched = [&]() {
@@ -326,43 +369,43 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     fetched();
   };
 
-  f32x4 acc[FF][RF];
+  f32x4 acc[FF][RF], tot[FF][RF];   // the chain, and (linear) the sum of the chains before it
 #pragma unroll
   for (int f = 0; f < FF; ++f)
 #pragma unroll
-    for (int r = 0; r < RF; ++r) acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int q = grp ^ ((c >> 1) & 7);
-  const int xo = (wr * RF * 16 + c) * 8 + q, wo = (BM + wf * FF * 16 + c) * 8 + q;
-  uint4 xa[RF], wa[FF], xc[RF], wc[FF];   // the first and second super-step of a stage
-  // fragment i of a super-step: weights first, then rows
-  auto read_one = [&](uint4 (&xf)[RF], uint4 (&wfr)[FF], const uint4* buf, int s, int i) {
-    if (i < FF) wfr[i] = buf[(wo ^ (s * 4)) + i * 128];
-    else xf[i - FF] = buf[(xo ^ (s * 4)) + (i - FF) * 128];
+    for (int r = 0; r < RF; ++r) tot[f][r] = acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int chains = MODE == TM_LINEAR ? linear_chains(S) : 1;
+  int ch = 0, ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : S;   // the chain, its last super-step + 1
+  const int q = grp ^ swizzle(c);
+  const int xo = (wr * RF * 16 + c) * PPR + q, wo = (BM + wf * FF * 16 + c) * PPR + q;
+  uint4 xs[2][RF], ws[2][FF];   // the fragments of two super-steps
+  // fragment i of super-step s: weights first, then rows
+  auto read_one = [&](const uint4* buf, int s, int i) {
+    if (i < FF) ws[s & 1][i] = buf[(wo ^ (s * 4)) + i * (16 * PPR)];
+    else xs[s & 1][i - FF] = buf[(xo ^ (s * 4)) + (i - FF) * (16 * PPR)];
   };
-  auto read = [&](uint4 (&xf)[RF], uint4 (&wfr)[FF], const uint4* buf, int s) {
+  constexpr int MN = FF * RF, PARTS = MN < 8 ? MN : 8;
+  auto mul = [&](int set, int j0, int j1) {
 #pragma unroll
-    for (int i = 0; i < FF + RF; ++i) read_one(xf, wfr, buf, s, i);
-  };
-  auto mul = [&](const uint4 (&xf)[RF], const uint4 (&wfr)[FF], int j0, int j1) {
-#pragma unroll
-    for (int j = j0; j < j1; ++j) acc[j / RF][j % RF] = mma<DT>(wfr[j / RF], xf[j % RF], acc[j / RF][j % RF]);
+    for (int j = j0; j < j1; ++j) acc[j / RF][j % RF] = mma<DT>(ws[set][j / RF], xs[set][j % RF], acc[j / RF][j % RF]);
   };
   // A super-step's matrix instructions in PARTS parts, between which the next
-  // super-step's fragments are read and (buf not null) the requests for a later
+  // super-step's fragments are read and (stage) the requests for a later
   // stage go out: all at once, either would hold up the wave's matrix
   // instructions for as long as all eight waves' reads or requests take.
-  constexpr int MN = FF * RF, PARTS = MN < 8 ? MN : 8;
   int left = stages;
-  auto second = [&](const uint4* cur) {
+  auto others = [&](const uint4* cur) {
     --left;
 #pragma unroll
-    for (int j = 0; j < PARTS; ++j) {
+    for (int s = 1; s < SPS; ++s)
 #pragma unroll
-      for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(xc, wc, cur, 1, i);
-      __builtin_amdgcn_sched_barrier(0);
-      mul(xa, wa, j * MN / PARTS, (j + 1) * MN / PARTS);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+      for (int j = 0; j < PARTS; ++j) {
+#pragma unroll
+        for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(cur, s, i);
+        __builtin_amdgcn_sched_barrier(0);
+        mul((s & 1) ^ 1, j * MN / PARTS, (j + 1) * MN / PARTS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
   };
   // The stage in `cur`: the products of the stage before, in `prev`, are finished
   // while its first fragments are read; `prev`, which every wave has read by
@@ -374,31 +417,37 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 #pragma unroll
     for (int j = 0; j < PARTS; ++j) {
 #pragma unroll
-      for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(xa, wa, cur, 0, i);
+      for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(cur, 0, i);
 #pragma unroll
       for (int i = j * LPW / PARTS; i < (j + 1) * LPW / PARTS; ++i) fetch_one(prev, i);
       __builtin_amdgcn_sched_barrier(0);
-      mul(xc, wc, j * MN / PARTS, (j + 1) * MN / PARTS);
+      mul(1, j * MN / PARTS, (j + 1) * MN / PARTS);
       __builtin_amdgcn_sched_barrier(0);
     }
     fetched();
-    second(cur);
+    if constexpr (MODE == TM_LINEAR)
+      if ((stages - left) * SPS == ch_end) {   // the stage before ended a chain
+        ch_end = chain_start(++ch + 1, S, chains);
+#pragma unroll
+        for (int f = 0; f < FF; ++f)
+#pragma unroll
+          for (int r = 0; r < RF; ++r) {
+            tot[f][r] += acc[f][r];
+            acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+      }
+    others(cur);
   };
   fetch(b0);
   fetch(b1);
-  if (NST > 2) fetch(b2);
+  fetch(b2);
   if (NST > 3) fetch(b3);
   wait_vm<(NST - 1) * LPW>();
   barrier_only();
-  read(xa, wa, b0, 0);
-  second(b0);
-  if constexpr (NST == 2) {
-    while (left) {
-      stage(b0, b1);
-      if (!left) break;
-      stage(b1, b0);
-    }
-  } else {
+#pragma unroll
+  for (int i = 0; i < FF + RF; ++i) read_one(b0, 0, i);
+  others(b0);
+  {
     // (whole turns of the buffers without an exit between them, so that the
     // compiler sees which request each read follows and adds no wait of its
     // own; then the rest)
@@ -418,17 +467,29 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       }
     }
   }
-  if (S % 2 == 0) mul(xc, wc, 0, MN);   // (an odd reduction ends with half a stage)
+  if (SPS == 4 || S % 2 == 0) mul(1, 0, MN);   // (an odd reduction ends with half a stage)
   wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
 
   if constexpr (MODE == TM_LINEAR) {
     const bool vec = linear_vec(a.l);
+    // the residual of all of the wave's values at once (y may be the residual, so
+    // the compiler keeps each load behind the stores before it: 8192 x 11008
+    // 765 us with them one after another, 730)
+    f32x4 res[FF][RF];
+#pragma unroll
+    for (int f = 0; f < FF; ++f)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) res[f][r] = linear_residual(a.l, t0 + (wr * RF + r) * 16 + c, f0 + (wf * FF + f) * 16 + 4 * grp, vec);
 #pragma unroll
     for (int f = 0; f < FF; ++f) {
       const int n = f0 + (wf * FF + f) * 16 + 4 * grp;
       const f32x4 bias = linear_bias(a.l, n);
 #pragma unroll
-      for (int r = 0; r < RF; ++r) linear_out(a.l, t0 + (wr * RF + r) * 16 + c, n, acc[f][r], bias, vec);
+      for (int r = 0; r < RF; ++r) {
+        // (one chain: the sum as it is, as everywhere)
+        const f32x4 v = chains > 1 ? tot[f][r] + acc[f][r] : acc[f][r];
+        linear_out(a.l, t0 + (wr * RF + r) * 16 + c, n, v, bias, res[f][r], vec);
+      }
     }
   } else if constexpr (MODE == TM_UP) {
 #pragma unroll
@@ -460,32 +521,66 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   }
 }
 
-template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST>
+template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST, int SPS = 2>
 static hipError_t launch_tile(TileArgs a, hipStream_t st) {
   if (MODE == TM_LINEAR) a.nrt = (a.l.T + BM - 1) / BM;
   const int cols = MODE == TM_LINEAR ? a.l.N : MODE == TM_UP ? 2 * a.f.F : a.p.nc;
   a.nft = (cols + BN - 1) / BN;
   const int64_t n = (int64_t)a.nrt * a.nft;
-  hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
+  hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST, SPS>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
                      st, a);
   return hipGetLastError();
 }
 
 // ------------------------------------------------------------------- linear --
 
-// At most 16 rows: one 16-feature tile per wave, a wave per workgroup (they
-// spread over more CUs than as four).
-template <int DT>
-__global__ __launch_bounds__(64, 2) void linear_rows_kernel(LinearArgs a) {
+// Few rows: a wave per chain of MT row tiles and NT feature tiles, operands
+// straight to registers, the workgroup's chains added in order.  (D: steps in
+// flight, what the registers hold.)
+template <int DT, int MT, int NT, int D>
+__global__ __launch_bounds__(MAX_CHAINS * 64, 2) void linear_rows_kernel(LinearArgs a, int nblk) {
   constexpr int ESZ = Geo<DT>::ESZ;
-  const int lane = threadIdx.x, c = lane & 15, grp = lane >> 4, n0 = blockIdx.x * 16;
-  const unsigned char* wp[1] = {reinterpret_cast<const unsigned char*>(a.w) +
-                                (size_t)min(n0 + c, a.N - 1) * a.ldw * ESZ + grp * 16};
-  const unsigned char* xp =
-      reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(c, a.T - 1) * a.ldx * ESZ + grp * 16;
-  f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
-  chain<DT, 1, 24>(wp, xp, a.K / Geo<DT>::KS, acc);
-  linear_out(a, c, n0 + 4 * grp, acc[0], linear_bias(a, n0 + 4 * grp), linear_vec(a));
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  const int t0 = blockIdx.x / nblk * (MT * 16), n0 = blockIdx.x % nblk * (NT * 16);
+  const int S = a.K / Geo<DT>::KS, chains = linear_chains(S);
+  const int s0 = chain_start(wv, S, chains), s1 = chain_start(wv + 1, S, chains);
+  const unsigned char *wp[NT], *xp[MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+    wp[n] = reinterpret_cast<const unsigned char*>(a.w) + (size_t)min(n0 + n * 16 + c, a.N - 1) * a.ldw * ESZ + grp * 16 +
+            (size_t)s0 * STEP;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+    xp[m] = reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + m * 16 + c, a.T - 1) * a.ldx * ESZ + grp * 16 +
+            (size_t)s0 * STEP;
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  chain<DT, NT, MT, D>(wp, xp, s1 - s0, acc);
+  __shared__ f32x4 red[MAX_CHAINS][NT * MT][64];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) red[wv][n * MT + m][lane] = acc[n][m];
+  __syncthreads();
+  const bool vec = linear_vec(a);
+  for (int i = wv; i < NT * MT; i += chains) {
+    f32x4 v = red[0][i][lane];
+    for (int w = 1; w < chains; ++w) v += red[w][i][lane];
+    const int t = t0 + i % MT * 16 + c, n = n0 + i / MT * 16 + 4 * grp;
+    linear_out(a, t, n, v, linear_bias(a, n), linear_residual(a, t, n, vec), vec);
+  }
+}
+
+template <int DT, int MT, int NT, int D>
+static hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
+  const int nblk = (a.N + NT * 16 - 1) / (NT * 16);
+  const int chains = linear_chains(a.K / ks_of(a.dt));
+  hipLaunchKernelGGL((linear_rows_kernel<DT, MT, NT, D>), dim3((unsigned)nblk * ((a.T + MT * 16 - 1) / (MT * 16))),
+                     dim3(chains * 64), 0, st, a, nblk);
+  return hipGetLastError();
 }
 
 // Products of few outputs (a router): a workgroup's eight waves each sum the
@@ -542,8 +637,8 @@ __global__ __launch_bounds__(CHAINS * 64) void linear_narrow_kernel(LinearArgs a
     f32x4 v = red[0][i][lane];
 #pragma unroll
     for (int w = 1; w < CHAINS; ++w) v += red[w][i][lane];
-    const int n = n0 + i / MT * 16 + 4 * grp;
-    linear_out(a, t0 + i % MT * 16 + c, n, v, linear_bias(a, n), linear_vec(a));
+    const int t = t0 + i % MT * 16 + c, n = n0 + i / MT * 16 + 4 * grp;
+    linear_out(a, t, n, v, linear_bias(a, n), linear_residual(a, t, n, linear_vec(a)), linear_vec(a));
   }
 }
 
@@ -561,25 +656,30 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   if (a.N <= NARROW)
     // small tiles until they fill the chip, then those that read the rows less often
     return rt * nt <= 2048 ? launch_narrow<DT, 1, 1>(a, st) : launch_narrow<DT, 2, 4>(a, st);
-  if (a.T <= 16) {
-    hipLaunchKernelGGL((linear_rows_kernel<DT>), dim3((unsigned)nt), dim3(64), 0, st, a);
-    return hipGetLastError();
-  }
+  // 4096 x 4096, weights from HBM: 9.2 us for one row, 9.6 for eight (32 x 32 tiles 11);
+  // of 32256 columns 59 us (64 x 64 tiles 51)
+  if (a.T <= 16 && nt <= 1024) return launch_rows<DT, 1, 1, 16>(a, st);
   TileArgs t{};
   t.l = a;
   // The tile that finishes first: turns of the 256 CUs times what a turn costs
-  // (us over 4096 bf16 columns with every CU at work; one turn alone: 64 x 32 12
-  // us, 64 x 64 14, 128 x 128 26, 128 x 256 43).  33 rows x 6144: 64 x 32 11.8
-  // us, 64 x 64 13.4; 256 x 4096: 19.4, 14.4, 128 x 128 25.6; 513 x 4096: 64 x 64
-  // 35, 128 x 128 26, 128 x 256 43; 8192 x 11008: 128 x 128 780, 128 x 256 608,
-  // 256 x 256 (half as many turns, one stage ahead instead of two) 690.
-  auto turns = [&](int64_t m, int64_t n) { return (((a.T + m - 1) / m) * ((a.N + n - 1) / n) + 255) / 256; };
-  const int64_t c1 = 10 * turns(64, 32), c2 = 13 * turns(64, 64), c3 = 27 * turns(128, 128), c4 = 46 * turns(128, 256);
-  const int64_t best = std::min(std::min(c1, c2), std::min(c3, c4));
+  // (us over 4096 bf16 columns).  33 rows, weights from HBM, tiles of 32 x 32 /
+  // 64 x 32 / 64 x 64: 4096 features 11.4 / 13.5 / 20 us, 6144 16.7 / 14.5 / 21,
+  // 32256 69 / 64 / 54 (one barrier per two super-steps: 16.4 / 17.4 / 20 at
+  // 4096).  256 rows x 4096: 64 x 64 14, 128 x 128 26.  513 x 4096: 64 x 64 35,
+  // 128 x 128 26, 128 x 256 43.  8192 x 11008: 128 x 128 780, 128 x 256 608.
+  auto cost = [&](int64_t m, int64_t n, int64_t turn) {
+    return ((((a.T + m - 1) / m) * ((a.N + n - 1) / n) + 255) / 256) * turn;
+  };
+  const int64_t none = INT64_MAX;   // (tiles of more than twice the rows only add reads)
+  const int64_t c0 = cost(32, 32, 9), c1 = cost(64, 32, 14), c2 = cost(64, 64, 18),
+                c3 = a.T > 64 ? cost(128, 128, 27) : none, c4 = a.T > 64 ? cost(128, 256, 46) : none, best = std::min(std::min(std::min(c0, c1), std::min(c2, c3)), c4);
   if (best == c4) return launch_tile<DT, TM_LINEAR, 128, 256, 2, 4, 3>(t, st);
   if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
   if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 4>(t, st);
-  return launch_tile<DT, TM_LINEAR, 64, 32, 2, 2, 4>(t, st);
+  const bool four = a.K / Geo<DT>::KS % 4 == 0;
+  if (best == c1)
+    return four ? launch_tile<DT, TM_LINEAR, 64, 32, 4, 2, 4, 4>(t, st) : launch_tile<DT, TM_LINEAR, 64, 32, 2, 2, 4, 2>(t, st);
+  return four ? launch_tile<DT, TM_LINEAR, 32, 32, 2, 2, 4, 4>(t, st) : launch_tile<DT, TM_LINEAR, 32, 32, 2, 2, 4, 2>(t, st);
 }
 
 hipError_t run_linear(const LinearArgs& a, hipStream_t st) {
@@ -635,6 +735,16 @@ __device__ __forceinline__ uint64_t ordered(double x) {
   return (uint64_t)(b ^ ((b >> 63) | INT64_MIN));
 }
 
+// 1 / x for x >= 1 (0 for infinity): the hardware's estimate and two Newton steps,
+// within an ulp or two of float64 (a division that rounds right takes three times the
+// instructions).
+__device__ __forceinline__ double reciprocal(double x) {
+  double r = __builtin_amdgcn_rcp(x);
+  r = fma(fma(-x, r, 1.0), r, r);
+  r = fma(fma(-x, r, 1.0), r, r);
+  return x == INFINITY ? 0.0 : r;
+}
+
 // One wave per row, experts e = 64 i + lane in registers.  Scores, biased
 // scores and the selection are float64 values of the logits, so which experts
 // a row gets never hangs on a float32 rounding.  The k experts are taken one
@@ -673,11 +783,12 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
       sum += s[i];
     }
     sum = wave_sum(sum);
+    const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) s[i] = sum > 0.0 ? s[i] / sum : 0.0;
+    for (int i = 0; i < EPL; ++i) s[i] *= inv;
   } else {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) s[i] = l[i] == -INFINITY ? 0.0 : 1.0 / (1.0 + exp(-(double)l[i]));
+    for (int i = 0; i < EPL; ++i) s[i] = l[i] == -INFINITY ? 0.0 : reciprocal(1.0 + exp(-(double)l[i]));
   }
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
@@ -791,12 +902,12 @@ __global__ __launch_bounds__(64, 2) void ffn_up_kernel(FfnArgs a, void* z, int n
   const size_t rb = (size_t)a.d * ESZ;
   const unsigned char* w = reinterpret_cast<const unsigned char*>(a.wgu) + ((size_t)e * 2 * a.F + f0 + c) * rb + grp * 16;
   const unsigned char* wp[2] = {w, w + (size_t)a.F * rb};
-  const unsigned char* xp = reinterpret_cast<const unsigned char*>(a.x) + (size_t)(p / a.k) * a.ldx * ESZ + grp * 16;
-  f32x4 acc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-  chain<DT, 2, 16>(wp, xp, a.d / Geo<DT>::KS, acc);
+  const unsigned char* xp[1] = {reinterpret_cast<const unsigned char*>(a.x) + (size_t)(p / a.k) * a.ldx * ESZ + grp * 16};
+  f32x4 acc[2][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}, {f32x4{0.f, 0.f, 0.f, 0.f}}};
+  chain<DT, 2, 1, 16>(wp, xp, a.d / Geo<DT>::KS, acc);
   f32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = silu(acc[0][i]) * acc[1][i];
+  for (int i = 0; i < 4; ++i) v[i] = silu(acc[0][0][i]) * acc[1][0][i];
   if (c == 0) store4<DT>(z, (size_t)p * a.F + f0 + 4 * grp, v);
 }
 
@@ -816,12 +927,12 @@ __global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a,
     if (e < 0 || e >= a.E) continue;
     const size_t rb = (size_t)a.F * ESZ;
     const unsigned char* wp[1] = {reinterpret_cast<const unsigned char*>(a.wd) + ((size_t)e * a.d + n0 + c) * rb + grp * 16};
-    const unsigned char* zp = reinterpret_cast<const unsigned char*>(z) + p * rb + grp * 16;
-    f32x4 acc[1] = {f32x4{0.f, 0.f, 0.f, 0.f}};
-    chain<DT, 1, 24>(wp, zp, a.F / Geo<DT>::KS, acc);
+    const unsigned char* zp[1] = {reinterpret_cast<const unsigned char*>(z) + p * rb + grp * 16};
+    f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
+    chain<DT, 1, 1, 24>(wp, zp, a.F / Geo<DT>::KS, acc);
     if (c == 0)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[j][4 * grp + i] = acc[0][i];
+      for (int i = 0; i < 4; ++i) y[j][4 * grp + i] = acc[0][0][i];
   }
   __syncthreads();
   if (threadIdx.x < 16) {
