@@ -750,15 +750,17 @@ __device__ __forceinline__ double reciprocal(double x) {
 // a row gets never hangs on a float32 rounding.  The k experts are taken one
 // after another: every lane's best (the first of equal ones), then the wave's by
 // the upper halves of the ordered keys, by the lower halves and by the
-// index where those before leave several.  Bound by the instructions
-// of these steps (16384 rows of 256 sigmoid scores in 8 groups: 62 us with
-// shuffles through LDS and a lane per group, 32 us).
+// index where those before leave several.  Bound by the vector instructions: 16384
+// rows of 256 sigmoid scores in 8 groups 62 us with shuffles through LDS and a
+// lane per group, 32 with 1120 instructions per row, 25 us with 830
+// (keys as ordered integers and sorted per lane, scores looked up at the end).
 template <int DT, int EPL>
 __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, t = blockIdx.x * ROUTE_ROWS + wv;
-  __shared__ double gkey[ROUTE_ROWS][EPL * 64];
+  __shared__ double lds[ROUTE_ROWS][EPL * 64];   // the row's keys (groups), then its scores
   const bool row = t < a.T;
   constexpr double NONE = -INFINITY;
+  constexpr uint64_t ONONE = 0x000fffffffffffffull;   // ordered(NONE); no key's upper half is as small
   float l[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
@@ -779,7 +781,7 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      s[i] = l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)mx);
+      s[i] = exp((double)l[i] - (double)mx);   // (mx is finite: 0 for -inf)
       sum += s[i];
     }
     sum = wave_sum(sum);
@@ -788,7 +790,7 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
     for (int i = 0; i < EPL; ++i) s[i] *= inv;
   } else {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) s[i] = l[i] == -INFINITY ? 0.0 : reciprocal(1.0 + exp(-(double)l[i]));
+    for (int i = 0; i < EPL; ++i) s[i] = reciprocal(1.0 + exp(-(double)l[i]));   // (0 for -inf)
   }
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
@@ -801,7 +803,7 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
   }
   if (a.groups > 1) {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) gkey[wv][i * 64 + lane] = key[i];
+    for (int i = 0; i < EPL; ++i) lds[wv][i * 64 + lane] = key[i];
     __syncthreads();
     const int per = a.E / a.groups;
     int lanes = 1;   // lanes per group
@@ -810,14 +812,15 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
     double b1 = NONE, b2 = NONE;   // the group's best two keys
     if (g < a.groups)
       for (int i = lane % lanes; i < per; i += lanes) {
-        const double v = gkey[wv][g * per + i];
-        b2 = fmax(b2, fmin(b1, v));
-        b1 = fmax(b1, v);
+        const double v = lds[wv][g * per + i], low = v > b1 ? b1 : v;
+        b2 = low > b2 ? low : b2;
+        b1 = v > b1 ? v : b1;
       }
     for (int o = 1; o < lanes; o <<= 1) {
       const double c1 = __shfl_xor(b1, o), c2 = __shfl_xor(b2, o);
-      b2 = fmax(fmin(b1, c1), fmax(b2, c2));
-      b1 = fmax(b1, c1);
+      const double low = c1 > b1 ? b1 : c1, two = c2 > b2 ? c2 : b2;
+      b2 = low > two ? low : two;
+      b1 = c1 > b1 ? c1 : b1;
     }
     const double gs = a.group_top == 2 && b2 > NONE ? b1 + b2 : b1;
     // groups that come before this one: better, or equal with a lower index
@@ -827,44 +830,81 @@ __global__ __launch_bounds__(ROUTE_ROWS * 64) void route_kernel(RouteArgs a) {
       before += o > gs || (o == gs && h < g);
     }
     const unsigned long long keep = __ballot(g < a.groups && before < a.top_groups);
+    const unsigned inv = ((1u << 20) + per - 1) / per;   // e / per = e inv / 2^20 for e, per <= 1024
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
       const int e = i * 64 + lane;
-      if (e < a.E && !((keep >> (e / per * lanes)) & 1ull)) key[i] = NONE;
+      if (e < a.E && !((keep >> ((e * inv >> 20) * lanes)) & 1ull)) key[i] = NONE;
     }
+    __syncthreads();
   }
-  int id = -1;        // lane j: the expert of slot j and its score
-  double w = 0.0, tot = 0.0;
-  for (int j = 0; j < a.k; ++j) {
-    double best = key[0], sc = s[0];
-    int at = lane;
+  uint64_t o[EPL];
 #pragma unroll
-    for (int i = 1; i < EPL; ++i)
-      if (key[i] > best) { best = key[i]; at = i * 64 + lane; sc = s[i]; }
-    const uint64_t o = ordered(best);
-    const uint32_t hi = (uint32_t)(o >> 32), lo = (uint32_t)o;
+  for (int i = 0; i < EPL; ++i) {
+    lds[wv][i * 64 + lane] = s[i];
+    o[i] = ordered(key[i]);
+  }
+  // up to four keys per lane are sorted first (neighbours only, so equal ones keep
+  // their order), and a winner's list moves up; more are searched every time
+  constexpr bool SORTED = EPL <= 4;
+  int at[SORTED ? EPL : 1];   // expert / 64 of the sorted keys
+  if constexpr (SORTED) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) at[i] = i;
+#pragma unroll
+    for (int n = EPL - 1; n > 0; --n)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const bool sw = o[i + 1] > o[i];
+        const uint64_t x = o[i], y = o[i + 1];
+        const int u = at[i], v = at[i + 1];
+        o[i] = sw ? y : x; o[i + 1] = sw ? x : y;
+        at[i] = sw ? v : u; at[i + 1] = sw ? u : v;
+      }
+  }
+  int id = -1;   // lane j: the expert of slot j
+  for (int j = 0; j < a.k; ++j) {
+    uint64_t best = o[0];
+    if constexpr (!SORTED) {
+      at[0] = 0;
+#pragma unroll
+      for (int i = 1; i < EPL; ++i)
+        if (o[i] > best) { best = o[i]; at[0] = i; }
+    }
+    const uint32_t hi = (uint32_t)(best >> 32), lo = (uint32_t)best;
     const uint32_t top = wave_max(hi);
+    if (top == (uint32_t)(ONONE >> 32)) break;   // none left
     unsigned long long m = __ballot(hi == top);
     if (m & (m - 1)) {
       const uint32_t low = wave_max(hi == top ? lo : 0u);
       m = __ballot(hi == top && lo == low);
       if (m & (m - 1)) {   // equal keys: the lowest index
         const bool in = (m >> lane) & 1ull;
-        const uint32_t inv = wave_max(in ? ~(uint32_t)at : 0u);
-        m = __ballot(in && ~(uint32_t)at == inv);
+        const uint32_t inv = ~(uint32_t)(at[0] * 64 + lane), last = wave_max(in ? inv : 0u);
+        m = __ballot(in && inv == last);
       }
     }
-    const int win = __ffsll(m) - 1;
-    if (lane_value(best, win) == NONE) break;   // none left
-    const int e = __builtin_amdgcn_readlane(at, win);
-    const double v = lane_value(sc, win);
-    tot += v;
-    if (lane == j) { id = e; w = v; }
+    const int win = __builtin_amdgcn_readfirstlane(__ffsll(m) - 1), wi = __builtin_amdgcn_readlane(at[0], win);
+    if (lane == j) id = wi * 64 + win;
+    if constexpr (SORTED) {
+      if (lane == win) {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (e == i * 64 + lane) key[i] = NONE;
+        for (int i = 0; i + 1 < EPL; ++i) { o[i] = o[i + 1]; at[i] = at[i + 1]; }
+        o[EPL - 1] = ONONE;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (i == wi && lane == win) o[i] = ONONE;
+    }
   }
-  if (a.renorm) w = tot > 0.0 ? w / tot : 0.0;
+  __syncthreads();
+  double w = id >= 0 ? lds[wv][id] : 0.0;
+  if (a.renorm) {
+    double tot = 0.0;
+    for (int j = 0; j < a.k; ++j) tot += lane_value(w, j);
+    w = tot > 0.0 ? w / tot : 0.0;
+  }
   if (row && lane < a.k) {
     a.ids[(size_t)t * a.k + lane] = id;
     a.weights[(size_t)t * a.k + lane] = (float)(w * (double)a.scale);
