@@ -201,20 +201,20 @@ def _refuse(what: str, shape, dtype, dev, t):
 
 def _rows_of(t, what: str, shape, dtype, dev) -> int:
     """Checks a [rows, cols] operand of unit column stride; returns its row stride."""
-    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.get_device() != dev:
-        _refuse(what, shape, dtype, dev, t)
-    rs, cs = t.stride()
-    if cs != 1 and shape[1] > 1:
-        _refuse(what, shape, dtype, dev, t)
-    # (a single row may carry any stride)
-    return rs if shape[0] > 1 or rs > shape[1] else shape[1]
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+        rs, cs = t.stride()
+        if cs == 1 or shape[1] <= 1:
+            # (a single row may carry any stride)
+            return rs if shape[0] > 1 or rs > shape[1] else shape[1]
+    _refuse(what, shape, dtype, dev, t)
 
 
-def _whole(t, what: str, shape, dtype, dev):
-    """Checks a contiguous operand."""
-    if (not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.get_device() != dev
-            or not t.is_contiguous()):
-        _refuse(what, shape, dtype, dev, t)
+def _whole(t, what: str, shape, dtype, dev) -> int:
+    """Checks a contiguous operand; returns its address."""
+    if (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _refuse(what, shape, dtype, dev, t)
 
 
 def _operand(x, what: str):
@@ -234,9 +234,12 @@ def _out_type(out_dtype, out, x):
     return odt
 
 
+_current_device = torch.cuda.current_device
+
+
 def _operator(fn, args, dev: int):
     """Calls an operator on GPU ``dev`` and its current stream."""
-    if dev == torch.cuda.current_device():
+    if dev == _current_device():
         rc = fn(ctypes.byref(args), _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
@@ -265,10 +268,9 @@ def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtyp
         out, ldy = x.new_empty(shape, dtype=odt), n
     else:
         ldy = _rows_of(out, "out", shape, odt, dev)
-    if bias is not None:
-        _whole(bias, "bias", (n,), torch.float32, dev)
     ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
-    _operator(ee_linear, EELinearArgs(x.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+    _operator(ee_linear, EELinearArgs(x.data_ptr(), w.data_ptr(),
+                                      None if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
                                       None if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr,
                                       ldy, rows, cols, n, dt, _TYPES[odt], code), dev)
     return out
@@ -284,13 +286,12 @@ def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize
         raise EEError(EE_EINVAL, f"score must be one of {SCORES}")
     rows, n = logits.shape
     ld = _rows_of(logits, "logits", (rows, n), logits.dtype, dev)
-    if bias is not None:
-        _whole(bias, "bias", (n,), torch.float32, dev)
     k = int(top_k)
     shape = (rows, k if k > 0 else 0)
     ids = logits.new_empty(shape, dtype=torch.int32)
     weights = logits.new_empty(shape, dtype=torch.float32)
-    _operator(ee_moe_route, EEMoeRouteArgs(logits.data_ptr(), None if bias is None else bias.data_ptr(), ids.data_ptr(),
+    _operator(ee_moe_route, EEMoeRouteArgs(logits.data_ptr(),
+                                           None if bias is None else _whole(bias, "bias", (n,), torch.float32, dev), ids.data_ptr(),
                                            weights.data_ptr(), ld, rows, n, k, dt, code, 1 if renormalize else 0,
                                            int(n_groups), int(top_groups), int(group_top), scale), dev)
     return ids, weights
@@ -313,10 +314,9 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     E, _, f = w_down.shape
     k = ids.shape[1]
     ldx = _rows_of(x, "x", (rows, d), x.dtype, dev)
-    _whole(w_gate_up, "w_gate_up", (E, 2 * f, d), x.dtype, dev)
-    _whole(w_down, "w_down", (E, d, f), x.dtype, dev)
-    _whole(ids, "ids", (rows, k), torch.int32, dev)
-    _whole(weights, "weights", (rows, k), torch.float32, dev)
+    pointers = (x.data_ptr(), _whole(w_gate_up, "w_gate_up", (E, 2 * f, d), x.dtype, dev),
+                _whole(w_down, "w_down", (E, d, f), x.dtype, dev), _whole(ids, "ids", (rows, k), torch.int32, dev),
+                _whole(weights, "weights", (rows, k), torch.float32, dev))
     odt = _out_type(out_dtype, out, x)
     shape = (rows, d)
     if out is None:
@@ -329,8 +329,7 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or workspace.get_device() != dev
           or not workspace.is_contiguous()):
         raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")
-    _operator(ee_moe_ffn, EEMoeFfnArgs(x.data_ptr(), w_gate_up.data_ptr(), w_down.data_ptr(), ids.data_ptr(),
-                                       weights.data_ptr(), None if residual is None else residual.data_ptr(),
+    _operator(ee_moe_ffn, EEMoeFfnArgs(*pointers, None if residual is None else residual.data_ptr(),
                                        out.data_ptr(), workspace.data_ptr(), workspace.numel(), ldx, ldr, ldo, rows, E, k,
                                        d, f, dt, _TYPES[odt]), dev)
     return out

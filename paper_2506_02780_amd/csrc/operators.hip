@@ -1135,23 +1135,41 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
   const int64_t P = (int64_t)a.T * a.k;
   hipError_t e;
   FfnPlan pl = ffn_plan(a);
-  if (P <= 64) {
+  // Few pairs: each streams its expert's weights for itself, which spares the
+  // sorting and one launch, some 10 us, unless the pairs share experts so
+  // far that reading those again takes longer (64 MB of them).  With every expert
+  // as likely, P pairs meet E (1 - (1 - 1 / E)^P).
+  const double distinct = a.E * (1.0 - pow(1.0 - 1.0 / a.E, (double)P));
+  const double again = ((double)P - distinct) * 3.0 * a.d * a.F * esz_of(DT);
+  if (P <= 256 && again <= double(64 << 20)) {
     const int ub = a.F / 16, db = a.d / 16;
     hipLaunchKernelGGL((ffn_up_kernel<DT>), dim3((unsigned)ub * P), dim3(64), 0, st, a, pl.z, ub);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((ffn_down_kernel<DT, ODT>), dim3((unsigned)db * a.T), dim3(DOWN_WAVES * 64), 0, st, a, (const void*)pl.z, db);
     return hipGetLastError();
   }
-  const int64_t avg = P / a.E;
-  const int BM = avg < 24 ? 32 : avg < 96 ? 64 : 128;
+  // The tile whose turns of the chip take least, as for a linear (row tiles: every
+  // expert that is met ends in half a tile on average); with fewer than eight rows
+  // per expert the weights' stream is all, and the smallest does best.  128
+  // experts of 768 over 2048, 8 per row, tiles of 32 x 64 / 64 x 256 / 128 x 256: 33
+  // rows 156 / 173 / 178 us, 257 247 / 239 / 241, 513 303 / 270 / 283, 1025 412 /
+  // 319 / 309, 8192 1845 / 1173 / 933; 8 experts of 352 over 256, 2 per row, 257
+  // rows 13.7 / 19 / 26, 8192 62 / 54 / 45.
+  auto cost = [&](int BM, int BN, double turn) {
+    const double rt = std::max(distinct, (double)P / BM + distinct / 2);
+    auto turns = [&](int cols) { return ceil(rt * ((cols + BN - 1) / BN) / 256.0); };
+    return turn * (turns(2 * a.F) * a.d + turns(a.d) * a.F);
+  };
+  const double c0 = cost(32, 64, 9), c1 = cost(64, 256, 30), c2 = cost(128, 256, 46);
+  const int BM = P < 8 * a.E || (c0 <= c1 && c0 <= c2) ? 32 : c1 <= c2 ? 64 : 128;
   TileArgs t{};
   t.f = a;
   t.p = pl;
   t.nrt = (int)ffn_tiles(P, a.E, BM);
   hipLaunchKernelGGL(ffn_plan_kernel, dim3((unsigned)((P + PLAN_CHUNK - 1) / PLAN_CHUNK)), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (BM == 32) return ffn_tiles_t<DT, ODT, 32, 128, 1, 4, 4>(t, st);
-  if (BM == 64) return ffn_tiles_t<DT, ODT, 64, 128, 2, 4, 4>(t, st);
+  if (BM == 32) return ffn_tiles_t<DT, ODT, 32, 64, 2, 2, 4>(t, st);
+  if (BM == 64) return ffn_tiles_t<DT, ODT, 64, 256, 1, 8, 3>(t, st);
   return ffn_tiles_t<DT, ODT, 128, 256, 2, 4, 3>(t, st);
 }
 
