@@ -185,6 +185,8 @@ def make_moe_config(shape) -> EEMoeConfig:
 #
 # Device tensors in, device tensors out, on the tensors' device and its current
 # stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given.
+# They have no backward pass: operands that require a gradient are refused while
+# gradients are recorded.
 
 _TYPES = {torch.float32: EE_F32, torch.bfloat16: EE_BF16}
 _ACT_OF = {a: i for i, a in enumerate(ACTIVATIONS)}
@@ -195,13 +197,16 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 
 def _refuse(what: str, shape, dtype, dev, t):
+    if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+        raise EEError(EE_EINVAL, f"{what} requires a gradient, which these operators do not have (use torch.no_grad)")
     got = f"{list(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
     raise EEError(EE_EINVAL, f"{what} must be {list(shape)} {dtype} on cuda:{dev} (rows of unit column stride), not {got}")
 
 
 def _rows_of(t, what: str, shape, dtype, dev) -> int:
     """Checks a [rows, cols] operand of unit column stride; returns its row stride."""
-    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+    if (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev
+            and not (t.requires_grad and torch.is_grad_enabled())):
         rs, cs = t.stride()
         if cs == 1 or shape[1] <= 1:
             # (a single row may carry any stride)
@@ -212,7 +217,7 @@ def _rows_of(t, what: str, shape, dtype, dev) -> int:
 def _whole(t, what: str, shape, dtype, dev) -> int:
     """Checks a contiguous operand; returns its address."""
     if (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev
-            and t.is_contiguous()):
+            and t.is_contiguous() and not (t.requires_grad and torch.is_grad_enabled())):
         return t.data_ptr()
     _refuse(what, shape, dtype, dev, t)
 

@@ -287,6 +287,8 @@ bool valid_moe(const ee_model_config* c, const ee_moe_config* q, std::string* wh
   if (q->group_top < 1 || q->group_top > 2) return bad("group_top must be 1 or 2");
   if (q->top_k > q->n_experts / q->n_groups * q->top_groups) return bad("top_k exceeds the experts of top_groups groups");
   if (!isfinite(q->scale)) return bad("scale must be finite");
+  if ((size_t)2 * c->ffn * c->d_model * (c->dtype == EE_BF16 ? 2 : 4) >= (size_t(1) << 31))
+    return bad("an expert's gate and up weights must stay below 2 GiB");
   const size_t rows = std::max<size_t>((size_t)(c->k_max + 1) * c->max_seqs, prompt_rows(*c));
   if (rows * q->top_k > (size_t(1) << 24)) return bad("max_seqs * (k_max + 1) * top_k must be at most 2^24");
   return true;

@@ -289,7 +289,7 @@ def _ffn64(x, gu, dn, ids, w, residual, dtype):
     rows, d = x.shape
     E, f = gu.shape[0], gu.shape[1] // 2
     uz = UBF if dtype == "bf16" else U32
-    out, err = torch.zeros(rows, d, dtype=torch.float64), torch.zeros(rows, d, dtype=torch.float64)
+    out, err = (torch.zeros(rows, d, dtype=torch.float64, device=x.device) for _ in range(2))
     for e in range(E):
         row, slot = torch.nonzero(ids == e, as_tuple=True)
         if not len(row):
@@ -489,6 +489,125 @@ def test_two_streams_at_once(ee):
     torch.cuda.synchronize()
     for o1, o2 in outs:
         assert torch.equal(o1, wa) and torch.equal(o2, wb)
+
+
+def test_rows_and_columns_past_the_output_stay(ee):
+    g = _gen(12)
+    for rows in (1, 20, 70, 300):
+        for n in (40, 600):
+            big = torch.full((rows + 40, n + 8), 5.0, dtype=torch.bfloat16, device="cuda")
+            ee.linear(_rand(g, rows, 64, dtype=torch.bfloat16).cuda(), _rand(g, n, 64, dtype=torch.bfloat16).cuda(),
+                      out=big[20:20 + rows, :n])
+            assert (big[:20] == 5).all() and (big[20 + rows:] == 5).all() and (big[:, n:] == 5).all()
+        a = [t.cuda() for t in _ffn_inputs(rows, 64, 64, 8, 2, "bf16", seed=rows)]
+        big = torch.full((rows + 40, 72), 5.0, dtype=torch.bfloat16, device="cuda")
+        ee.moe_ffn(*a, out=big[20:20 + rows, :64])
+        assert (big[:20] == 5).all() and (big[20 + rows:] == 5).all() and (big[:, 64:] == 5).all()
+
+
+def test_a_workspace_of_the_callers(ee):
+    """Whatever it holds, and whichever call used it before."""
+    most = ee.ee_moe_ffn_workspace_bytes(400, 16, 4, 128, 96, ee.EE_BF16)
+    ws = torch.full((most + 512,), 255, dtype=torch.uint8, device="cuda")
+    for rows in (400, 3, 90, 400):
+        a = [t.cuda() for t in _ffn_inputs(rows, 128, 96, 16, 4, "bf16", seed=rows)]
+        assert torch.equal(ee.moe_ffn(*a, workspace=ws), ee.moe_ffn(*a))
+        assert (ws[most:] == 255).all(), "written past the stated size"
+    with pytest.raises(ee.EEError) as e:
+        ee.moe_ffn(*a, workspace=ws[:most - 256])
+    assert e.value.code == ee.EE_ECAPACITY
+
+
+def test_offsets_past_32_bits(ee):
+    """Rows 2^21 elements apart: x, w, y and the residual each span more than
+    4 GiB."""
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    ld, g = 1 << 21, _gen(13)
+
+    def spread(t):
+        base = torch.empty(t.shape[0] * ld, dtype=t.dtype, device="cuda")
+        v = base.as_strided((t.shape[0], t.shape[1]), (ld, 1))
+        v.copy_(t)
+        return v
+
+    x, w = _rand(g, 1200, 96, dtype=torch.bfloat16).cuda(), _rand(g, 1100, 96, std=0.1, dtype=torch.bfloat16).cuda()
+    r = _rand(g, 1200, 1100, dtype=torch.bfloat16).cuda()
+    want = ee.linear(x, w, residual=r)
+    xs, ws, rs = spread(x), spread(w), spread(r)
+    assert torch.equal(ee.linear(xs, ws, residual=rs, out=rs), want)
+    assert torch.equal(ee.linear(xs[1190:], w), ee.linear(x[1190:], w))
+    assert torch.equal(ee.linear(xs, w[:300], out_dtype=torch.float32), ee.linear(x, w[:300], out_dtype=torch.float32))
+    del ws
+    a = [t.cuda() for t in _ffn_inputs(1200, 96, 64, 8, 2, "bf16", seed=14)]
+    want = ee.moe_ffn(*a, residual=r[:, :96].contiguous())
+    h = rs[:, :96]
+    h.copy_(r[:, :96])
+    assert torch.equal(ee.moe_ffn(spread(a[0]), *a[1:], residual=h, out=h), want)
+    ids, wt = ee.moe_route(x, 8)
+    assert all(torch.equal(p, q) for p, q in zip(ee.moe_route(xs, 8), (ids, wt)))
+
+
+def test_an_expert_bank_of_more_than_4_gib(ee):
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    E, d, f, k = 640, 2048, 1024, 4
+    g = torch.Generator(device="cuda").manual_seed(15)
+    gu = torch.empty(E, 2 * f, d, dtype=torch.bfloat16, device="cuda").normal_(0, d ** -0.5, generator=g)
+    dn = torch.empty(E, d, f, dtype=torch.bfloat16, device="cuda").normal_(0, f ** -0.5, generator=g)
+    for rows in (1, 7, 150):
+        x = torch.randn(rows, d, generator=g, device="cuda").to(torch.bfloat16)
+        ids = torch.randint(E - 40, E, (rows, k), generator=g, device="cuda", dtype=torch.int32)
+        w = torch.rand(rows, k, generator=g, device="cuda")
+        want, err = _ffn64(x, gu, dn, ids, w, None, "bf16")
+        got = ee.moe_ffn(x, gu, dn, ids, w)
+        _close(got, want.cpu(), (err + UBF * (want.abs() + err) + 2 * U32 * want.abs() + 1e-30).cpu())
+
+
+def test_many_rows(ee):
+    """Pairs sorted by many workgroups, down products in several groups of
+    columns, and long grids."""
+    a = [t.cuda() for t in _ffn_inputs(9000, 1056, 32, 16, 8, "bf16", seed=16)]
+    res = _rand(_gen(17), 9000, 1056, dtype=torch.bfloat16).cuda()
+    want, err = _ffn64(*a, res, "bf16")
+    got = ee.moe_ffn(*a, residual=res)
+    _close(got, want.cpu(), (err + UBF * (want.abs() + err) + 2 * U32 * want.abs() + 1e-30).cpu())
+    g = _gen(18)
+    l = _rand(g, 70001, 24, std=2.0).cuda()
+    ids, w = ee.moe_route(l, 3)
+    top = torch.sort(l, dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), top[1][:, :3])
+    e = torch.exp(top[0][:, :3].double() - top[0][:, :1].double())
+    assert ((w.double() - e / e.sum(1, keepdim=True)).abs() <= U32 * (1 + 1e-6)).all()
+    x, wt = _rand(g, 70001, 64).cuda(), _rand(g, 24, 64).cuda()
+    y = ee.linear(x, wt)
+    assert ((y.double() - x.double() @ wt.double().T).abs() <= 66 * U32 * (x.double().abs() @ wt.double().abs().T)).all()
+
+
+def test_python_refusals(ee):
+    x, w = torch.zeros(4, 64, device="cuda"), torch.zeros(48, 64, device="cuda")
+    ids, wt = torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+    gu, dn = torch.zeros(3, 64, 64, device="cuda"), torch.zeros(3, 64, 32, device="cuda")
+    bad = [lambda: ee.linear(x.double(), w.double()), lambda: ee.linear(x, w.bfloat16()), lambda: ee.linear(x, w[:, :32]),
+           lambda: ee.linear(x, w.cpu()), lambda: ee.linear(x, w, act="tanh"), lambda: ee.linear(x.t(), w),
+           lambda: ee.linear(x, w, bias=torch.zeros(48, device="cuda", dtype=torch.bfloat16)),
+           lambda: ee.linear(x, w, residual=torch.zeros(4, 47, device="cuda")), lambda: ee.linear(x, w, out_dtype=torch.bfloat16),
+           lambda: ee.linear(x, w, out=torch.zeros(4, 96, device="cuda")[:, ::2]), lambda: ee.linear(x[0], w),
+           lambda: ee.linear(x[:, :40].contiguous(), w[:, :40].contiguous()),
+           lambda: ee.linear(x, w.clone().requires_grad_()),
+           lambda: ee.moe_route(x, 0), lambda: ee.moe_route(x, 65), lambda: ee.moe_route(x, 4, score="tanh"),
+           lambda: ee.moe_route(x, 4, n_groups=5), lambda: ee.moe_route(x, 4, bias=torch.zeros(63, device="cuda")),
+           lambda: ee.moe_ffn(x, gu, dn, ids.long(), wt), lambda: ee.moe_ffn(x, gu, dn, ids, wt[:3]),
+           lambda: ee.moe_ffn(x, gu[:2], dn, ids, wt), lambda: ee.moe_ffn(x, gu, dn.transpose(1, 2), ids, wt),
+           lambda: ee.moe_ffn(x.bfloat16(), gu, dn, ids, wt), lambda: ee.moe_ffn(x, gu, dn, ids, wt, workspace=x)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ee.EEError) as e:
+            call()
+        assert e.value.code == ee.EE_EINVAL, i
+    with torch.no_grad():
+        ee.linear(x, w.clone().requires_grad_())
 
 
 def test_empty_calls(ee):
