@@ -158,9 +158,8 @@ __device__ __forceinline__ f32x4 linear_residual(const LinearArgs& a, int t, int
   }
   return v;
 }
-__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v, f32x4 bias, f32x4 res, bool vec) {
+__device__ __forceinline__ void linear_store(const LinearArgs& a, int t, int n, f32x4 v, bool vec) {
   if (t >= a.T || n >= a.N) return;
-  v = activate4(v + bias, a.act) + res;
   const size_t o = (size_t)t * a.ldy + n;
   if (a.odt == DT_BF16) {
     uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + o;
@@ -182,10 +181,23 @@ __device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f3
     }
   }
 }
+__device__ __forceinline__ void linear_out(const LinearArgs& a, int t, int n, f32x4 v, f32x4 bias, f32x4 res, bool vec) {
+  linear_store(a, t, n, activate4(v + bias, a.act) + res, vec);
+}
 __device__ __forceinline__ bool linear_vec(const LinearArgs& a) {
   const uintptr_t need = a.odt == DT_BF16 ? 8 : 16;
   return a.N % 4 == 0 && a.ldy % 4 == 0 && (!a.res || a.ldr % 4 == 0) && reinterpret_cast<uintptr_t>(a.y) % need == 0 &&
          reinterpret_cast<uintptr_t>(a.res) % need == 0;
+}
+// Eight bf16 values of a row at a time: rows of y and residual in 16-byte pieces.
+__device__ __forceinline__ bool linear_wide(const LinearArgs& a) {
+  return a.odt == DT_BF16 && a.N % 8 == 0 && a.ldy % 8 == 0 && (!a.res || a.ldr % 8 == 0) &&
+         (reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.res)) % 16 == 0;
+}
+__device__ __forceinline__ void linear_store8(const LinearArgs& a, int t, int n, f32x4 v, f32x4 u) {
+  if (t >= a.T || n >= a.N) return;
+  *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.y) + (size_t)t * a.ldy + n) =
+      make_uint4(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]), bf16x2_bits(u[0], u[1]), bf16x2_bits(u[2], u[3]));
 }
 __device__ __forceinline__ f32x4 linear_bias(const LinearArgs& a, int n) {
   f32x4 b = {0.f, 0.f, 0.f, 0.f};
@@ -328,6 +340,15 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   const int stages = (S + SPS - 1) / SPS;
   auto swizzle = [](int r) { return SPS == 2 ? (r >> 1) & 7 : r & 15; };
 
+  // The order of the weights' rows within a wave's tiles, where the output leaves
+  // in bf16: row m of the tiles 2h and 2h + 1 is feature 32 h + 8 (m / 4) + m % 4,
+  // and 4 more, so that a lane's values of both are eight in a row and a store
+  // instruction writes 64 bytes of each output row instead of 32.
+  constexpr int FT = MODE == TM_UP ? FF / 2 : FF;   // tiles that one store covers
+  constexpr bool PAIRS = FT % 2 == 0 && DT == DT_BF16 && MODE != TM_DOWN;
+  const bool wide = PAIRS && (MODE == TM_UP || linear_wide(a.l));
+  auto feature = [&](int f, int m) { return wide ? (f >> 1) * 32 + (m >> 2) * 8 + (f & 1) * 4 + (m & 3) : f * 16 + m; };
+
   // this lane's piece of each of the wave's loads
   unsigned off[LPW];
 #pragma unroll
@@ -341,11 +362,15 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       off[i] = (unsigned)r * ldx + piece;
     } else {
       r -= BM;
-      if constexpr (MODE == TM_LINEAR) r = min(r, a.l.N - 1 - f0);
+      if constexpr (MODE == TM_LINEAR) {
+        const int w = r / (FF * 16), j = r % (FF * 16);
+        r = min(w * (FF * 16) + feature(j / 16, j % 16), a.l.N - 1 - f0);
+      }
       if constexpr (MODE == TM_DOWN) r = min(r, a.f.d - 1 - f0);
       if constexpr (MODE == TM_UP) {   // a wave's first FF / 2 tiles are gate features, then up of the same
         const int w = r / (FF * 16), j = r % (FF * 16), up = j >= FF * 8;
-        r = min(f0 + w * (FF * 8) + (up ? j - FF * 8 : j), a.f.F - 1) + (up ? a.f.F : 0);
+        const int k = up ? j - FF * 8 : j;
+        r = min(f0 + w * (FF * 8) + feature(k / 16, k % 16), a.f.F - 1) + (up ? a.f.F : 0);
       }
       off[i] = (unsigned)r * ldw + piece;
     }
@@ -390,11 +415,11 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     for (int j = j0; j < j1; ++j) acc[j / RF][j % RF] = mma<DT>(ws[set][j / RF], xs[set][j % RF], acc[j / RF][j % RF]);
   };
   // A super-step's matrix instructions in PARTS parts, between which the next
-  // super-step's fragments are read and (stage) the requests for a later
-  // stage go out: all at once, either would hold up the wave's matrix
-  // instructions for as long as all eight waves' reads or requests take.
+  // super-step's fragments are read and the requests for a later stage go out,
+  // spread over the whole stage: all at once, either would hold up the wave's
+  // matrix instructions for as long as all waves' reads or requests take.
   int left = stages;
-  auto others = [&](const uint4* cur) {
+  auto others = [&](const uint4* cur, uint4* prev, auto ask) {
     --left;
 #pragma unroll
     for (int s = 1; s < SPS; ++s)
@@ -402,10 +427,15 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       for (int j = 0; j < PARTS; ++j) {
 #pragma unroll
         for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(cur, s, i);
+        if constexpr (decltype(ask)::value) {
+#pragma unroll
+          for (int i = (s * PARTS + j) * LPW / (PARTS * SPS); i < (s * PARTS + j + 1) * LPW / (PARTS * SPS); ++i) fetch_one(prev, i);
+        }
         __builtin_amdgcn_sched_barrier(0);
         mul((s & 1) ^ 1, j * MN / PARTS, (j + 1) * MN / PARTS);
         __builtin_amdgcn_sched_barrier(0);
       }
+    if constexpr (decltype(ask)::value) fetched();
   };
   // The stage in `cur`: the products of the stage before, in `prev`, are finished
   // while its first fragments are read; `prev`, which every wave has read by
@@ -419,12 +449,11 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 #pragma unroll
       for (int i = j * (FF + RF) / PARTS; i < (j + 1) * (FF + RF) / PARTS; ++i) read_one(cur, 0, i);
 #pragma unroll
-      for (int i = j * LPW / PARTS; i < (j + 1) * LPW / PARTS; ++i) fetch_one(prev, i);
+      for (int i = j * LPW / (PARTS * SPS); i < (j + 1) * LPW / (PARTS * SPS); ++i) fetch_one(prev, i);
       __builtin_amdgcn_sched_barrier(0);
       mul(1, j * MN / PARTS, (j + 1) * MN / PARTS);
       __builtin_amdgcn_sched_barrier(0);
     }
-    fetched();
     if constexpr (MODE == TM_LINEAR)
       if ((stages - left) * SPS == ch_end) {   // the stage before ended a chain
         ch_end = chain_start(++ch + 1, S, chains);
@@ -436,7 +465,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
             acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
           }
       }
-    others(cur);
+    others(cur, prev, std::true_type{});
   };
   fetch(b0);
   fetch(b1);
@@ -446,7 +475,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   barrier_only();
 #pragma unroll
   for (int i = 0; i < FF + RF; ++i) read_one(b0, 0, i);
-  others(b0);
+  others(b0, nullptr, std::false_type{});
   {
     // (whole turns of the buffers without an exit between them, so that the
     // compiler sees which request each read follows and adds no wait of its
@@ -471,39 +500,64 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
 
   if constexpr (MODE == TM_LINEAR) {
+    // Each step over all of the wave's values under one branch of its own: with the
+    // choices inside the loop its code was so long that fetching it bound it
+    // (128 x 256 tiles: 10400 cycles of a workgroup, 4300 so; its 64 stages take 81000).  The residual is read before the first store (y may be
+    // the residual, so the compiler keeps each load behind the stores before it).
+    auto each = [&](auto fn) {
+#pragma unroll
+      for (int f = 0; f < FF; ++f)
+#pragma unroll
+        for (int r = 0; r < RF; ++r) fn(f, r, t0 + (wr * RF + r) * 16 + c, f0 + wf * (FF * 16) + feature(f, 4 * grp));
+    };
     const bool vec = linear_vec(a.l);
-    // the residual of all of the wave's values at once (y may be the residual, so
-    // the compiler keeps each load behind the stores before it: 8192 x 11008
-    // 765 us with them one after another, 730)
     f32x4 res[FF][RF];
+    each([&](int f, int r, int t, int n) { res[f][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    if (a.l.res) each([&](int f, int r, int t, int n) { res[f][r] = linear_residual(a.l, t, n, vec); });
+    if (chains > 1) each([&](int f, int r, int, int) { acc[f][r] = tot[f][r] + acc[f][r]; });   // (one chain: the sum as it is, as everywhere)
+    f32x4 bias[FF];
 #pragma unroll
-    for (int f = 0; f < FF; ++f)
-#pragma unroll
-      for (int r = 0; r < RF; ++r) res[f][r] = linear_residual(a.l, t0 + (wr * RF + r) * 16 + c, f0 + (wf * FF + f) * 16 + 4 * grp, vec);
-#pragma unroll
-    for (int f = 0; f < FF; ++f) {
-      const int n = f0 + (wf * FF + f) * 16 + 4 * grp;
-      const f32x4 bias = linear_bias(a.l, n);
-#pragma unroll
-      for (int r = 0; r < RF; ++r) {
-        // (one chain: the sum as it is, as everywhere)
-        const f32x4 v = chains > 1 ? tot[f][r] + acc[f][r] : acc[f][r];
-        linear_out(a.l, t0 + (wr * RF + r) * 16 + c, n, v, bias, res[f][r], vec);
-      }
+    for (int f = 0; f < FF; ++f) bias[f] = linear_bias(a.l, f0 + wf * (FF * 16) + feature(f, 4 * grp));
+    each([&](int f, int r, int, int) { acc[f][r] += bias[f]; });
+    auto act = [&](auto kind) { each([&](int f, int r, int, int) { acc[f][r] = activate4(acc[f][r], decltype(kind)::value); }); };
+    switch (a.l.act) {
+      case ACT_SILU: act(std::integral_constant<int, ACT_SILU>{}); break;
+      case ACT_GELU: act(std::integral_constant<int, ACT_GELU>{}); break;
+      case ACT_GELU_TANH: act(std::integral_constant<int, ACT_GELU_TANH>{}); break;
+      case ACT_RELU: act(std::integral_constant<int, ACT_RELU>{}); break;
+      default: break;
+    }
+    each([&](int f, int r, int, int) { acc[f][r] += res[f][r]; });
+    if (wide) {
+      if constexpr (PAIRS) each([&](int f, int r, int t, int n) { if (f % 2 == 0) linear_store8(a.l, t, n, acc[f][r], acc[f + 1][r]); });
+    } else if (vec) {
+      each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], true); });
+    } else {
+      each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], false); });
     }
   } else if constexpr (MODE == TM_UP) {
 #pragma unroll
-    for (int f = 0; f < FF / 2; ++f) {
-      const int n = f0 + (wf * (FF / 2) + f) * 16 + 4 * grp;
+    for (int f = 0; f < FT; f += PAIRS ? 2 : 1) {
+      const int n = f0 + wf * (FT * 16) + feature(f, 4 * grp);
       if (n >= a.f.F) continue;
 #pragma unroll
       for (int r = 0; r < RF; ++r) {
         const int row = (wr * RF + r) * 16 + c;
         if (row >= rows) continue;
-        f32x4 v;
+        auto glu = [&](int g) {
+          f32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = silu(acc[f][r][i]) * acc[f + FF / 2][r][i];
-        store4<DT>(a.p.z, (size_t)(et.p0 + row) * a.f.F + n, v);
+          for (int i = 0; i < 4; ++i) v[i] = silu(acc[g][r][i]) * acc[g + FT][r][i];
+          return v;
+        };
+        const size_t o = (size_t)(et.p0 + row) * a.f.F + n;
+        if constexpr (PAIRS) {   // (F is a multiple of 32)
+          const f32x4 v = glu(f), u = glu(f + 1);
+          *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.p.z) + o) =
+              make_uint4(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]), bf16x2_bits(u[0], u[1]), bf16x2_bits(u[2], u[3]));
+        } else {
+          store4<DT>(a.p.z, o, glu(f));
+        }
       }
     }
   } else {
