@@ -259,6 +259,7 @@ struct TileArgs {
   FfnArgs f;           // the others
   FfnPlan p;
   int nrt, nft;        // row tiles (at most), feature tiles
+  unsigned kmul;       // TM_UP: 2^32 / k rounded up, the factor that divides a pair's number (< 2^24) by k <= 32; 0: k is 1
 };
 
 // Products of BM rows with BN rows of weights, both streamed through LDS in
@@ -278,12 +279,22 @@ struct TileArgs {
 //   * SPS = 4 halves the barriers, which small tiles wait for most, and needs a
 //     multiple of four super-steps; SPS = 2 takes any number.
 // Rows past the end repeat the last one; their results are not stored.
+// Whether a workgroup takes one tile after another, so that the next one's first
+// stages are on their way while the last one's results are stored: where only one
+// workgroup fits a CU and reductions are short (8192 rows of 128 experts, 2048 x
+// 768: 942 us without, 903 so; linears gain nothing, 8192 x 11008 606 us without, 612 so: the
+// sums of their chains leave too few registers, and their clock is lower).
+template <int MODE, int BM, int BN, int NST, int SPS> constexpr bool tile_keeps() {
+  return MODE != TM_LINEAR && (BM + BN) * SPS * 64 * NST > 80 * 1024;
+}
+
 template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST, int SPS>
 __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   constexpr int ESZ = Geo<DT>::ESZ, WAVES = WR * WF, RF = BM / WR / 16, FF = BN / WF / 16;
   constexpr int PPR = 4 * SPS, RPL = 64 / PPR;   // 16-byte pieces of a row's stage, rows per load
   constexpr int LPW = (BM + BN) / RPL / WAVES;   // loads per wave and stage
   constexpr int STAGE = (BM + BN) * PPR;         // pieces of a stage
+  constexpr bool KEEP = tile_keeps<MODE, BM, BN, NST, SPS>();
   static_assert(SPS == 2 || SPS == 4, "two fragment sets in turn, rows of 8 or 16 pieces");
   static_assert((BM + BN) % (RPL * WAVES) == 0 && BM % RPL == 0, "every wave loads as much");
   static_assert(MODE != TM_UP || FF % 2 == 0, "a wave owns gate and up tiles of the same features");
@@ -298,45 +309,14 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   // tiles, GR row tiles side by side under one feature tile after another, so
   // that what they share stays in its L2.
   const int nrt = MODE == TM_LINEAR ? a.nrt : *a.p.ntile;
-  const int ntile = nrt * a.nft, per = (ntile + 7) / 8, at = (int)(blockIdx.x >> 3);
-  const int tile = (int)(blockIdx.x & 7) * per + at;
-  if (at >= per || tile >= ntile) return;
+  const int ntile = nrt * a.nft, per = (ntile + 7) / 8, tile0 = (int)(blockIdx.x & 7) * per;
+  const int end = min(per, ntile - tile0);   // this XCD's tiles
+  int at = (int)(blockIdx.x >> 3);
+  if (at >= end) return;
   constexpr int GR = BN > BM ? 4 : 8;   // (8192 x 11008, 128 x 256 tiles: 608 us with 4, 670 with 8, 680 with 32)
-  const int gsz = GR * a.nft, gi = tile / gsz, gr0 = gi * GR, gh = min(GR, nrt - gr0), gj = tile - gi * gsz;
-  const int rt = gr0 + gj % gh, ft = gj / gh;
-
-  const unsigned char *xb, *wb;   // the operands' tiles
-  unsigned ldx, ldw;              // bytes between their rows
-  int S, t0 = 0, rows;            // super-steps, first row, rows
-  int f0;                         // first feature
-  ExpertTile et{};
-  if constexpr (MODE == TM_LINEAR) {
-    S = a.l.K / Geo<DT>::KS;
-    t0 = rt * BM;
-    rows = min(BM, a.l.T - t0);
-    f0 = ft * BN;
-    ldx = (unsigned)a.l.ldx * ESZ;
-    ldw = (unsigned)a.l.ldw * ESZ;
-    xb = reinterpret_cast<const unsigned char*>(a.l.x) + (size_t)t0 * ldx;
-    wb = reinterpret_cast<const unsigned char*>(a.l.w) + (size_t)f0 * ldw;
-  } else {
-    et = a.p.tile[rt];
-    rows = et.n;
-    const int K = MODE == TM_UP ? a.f.d : a.f.F;
-    S = K / Geo<DT>::KS;
-    ldw = (unsigned)K * ESZ;
-    if constexpr (MODE == TM_UP) {
-      f0 = ft * (BN / 2);
-      ldx = (unsigned)a.f.ldx * ESZ;
-      xb = reinterpret_cast<const unsigned char*>(a.f.x);
-      wb = reinterpret_cast<const unsigned char*>(a.f.wgu) + (size_t)et.e * 2 * a.f.F * ldw;
-    } else {
-      f0 = a.p.c0 + ft * BN;
-      ldx = (unsigned)a.f.F * ESZ;
-      xb = reinterpret_cast<const unsigned char*>(a.p.z) + (size_t)et.p0 * ldx;
-      wb = reinterpret_cast<const unsigned char*>(a.f.wd) + ((size_t)et.e * a.f.d + f0) * ldw;
-    }
-  }
+  const int S = (MODE == TM_LINEAR ? a.l.K : MODE == TM_UP ? a.f.d : a.f.F) / Geo<DT>::KS;   // super-steps
+  const unsigned ldw = (unsigned)(MODE == TM_LINEAR ? a.l.ldw : MODE == TM_UP ? a.f.d : a.f.F) * ESZ;   // bytes between rows
+  const unsigned ldx = (unsigned)(MODE == TM_LINEAR ? a.l.ldx : MODE == TM_UP ? a.f.ldx : a.f.F) * ESZ;
   const int stages = (S + SPS - 1) / SPS;
   auto swizzle = [](int r) { return SPS == 2 ? (r >> 1) & 7 : r & 15; };
 
@@ -349,36 +329,67 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   const bool wide = PAIRS && (MODE == TM_UP || linear_wide(a.l));
   auto feature = [&](int f, int m) { return wide ? (f >> 1) * 32 + (m >> 2) * 8 + (f & 1) * 4 + (m & 3) : f * 16 + m; };
 
-  // this lane's piece of each of the wave's loads
+  // The tile's place and, for each of the wave's loads, this lane's piece.
+  const unsigned char *xb, *wb;   // the operands' tiles
+  int t0 = 0, rows, f0;           // first row, rows, first feature
+  ExpertTile et{};
   unsigned off[LPW];
-#pragma unroll
-  for (int i = 0; i < LPW; ++i) {
-    const int inst = wv * LPW + i;
-    int r = inst * RPL + lane / PPR;
-    const unsigned piece = ((lane % PPR) ^ swizzle(r)) * 16;
-    if (inst < BM / RPL) {
-      r = min(r, rows - 1);
-      if constexpr (MODE == TM_UP) r = a.p.order[et.p0 + r] / a.f.k;
-      off[i] = (unsigned)r * ldx + piece;
+  auto place = [&]() {
+    const int tile = tile0 + at, gsz = GR * a.nft, gi = tile / gsz, gr0 = gi * GR, gh = min(GR, nrt - gr0), gj = tile - gi * gsz;
+    const int rt = gr0 + gj % gh, ft = gj / gh;
+    if constexpr (MODE == TM_LINEAR) {
+      t0 = rt * BM;
+      rows = min(BM, a.l.T - t0);
+      f0 = ft * BN;
+      xb = reinterpret_cast<const unsigned char*>(a.l.x) + (size_t)t0 * ldx;
+      wb = reinterpret_cast<const unsigned char*>(a.l.w) + (size_t)f0 * ldw;
     } else {
-      r -= BM;
-      if constexpr (MODE == TM_LINEAR) {
-        const int w = r / (FF * 16), j = r % (FF * 16);
-        r = min(w * (FF * 16) + feature(j / 16, j % 16), a.l.N - 1 - f0);
+      et = a.p.tile[rt];
+      rows = et.n;
+      if constexpr (MODE == TM_UP) {
+        f0 = ft * (BN / 2);
+        xb = reinterpret_cast<const unsigned char*>(a.f.x);
+        wb = reinterpret_cast<const unsigned char*>(a.f.wgu) + (size_t)et.e * 2 * a.f.F * ldw;
+      } else {
+        f0 = a.p.c0 + ft * BN;
+        xb = reinterpret_cast<const unsigned char*>(a.p.z) + (size_t)et.p0 * ldx;
+        wb = reinterpret_cast<const unsigned char*>(a.f.wd) + ((size_t)et.e * a.f.d + f0) * ldw;
       }
-      if constexpr (MODE == TM_DOWN) r = min(r, a.f.d - 1 - f0);
-      if constexpr (MODE == TM_UP) {   // a wave's first FF / 2 tiles are gate features, then up of the same
-        const int w = r / (FF * 16), j = r % (FF * 16), up = j >= FF * 8;
-        const int k = up ? j - FF * 8 : j;
-        r = min(f0 + w * (FF * 8) + feature(k / 16, k % 16), a.f.F - 1) + (up ? a.f.F : 0);
-      }
-      off[i] = (unsigned)r * ldw + piece;
     }
-  }
+    int ln = lane;
+    if constexpr (KEEP) asm volatile("" : "+v"(ln));   // (computed anew for each tile: kept, it would cost registers that the products need)
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) {
+      const int inst = wv * LPW + i;
+      int r = inst * RPL + ln / PPR;
+      const unsigned piece = ((ln % PPR) ^ swizzle(r)) * 16;
+      if (inst < BM / RPL) {
+        r = min(r, rows - 1);
+        if constexpr (MODE == TM_UP) {
+          const unsigned pair = a.p.order[et.p0 + r];
+          r = a.kmul ? __umulhi(pair, a.kmul) : pair;
+        }
+        off[i] = (unsigned)r * ldx + piece;
+      } else {
+        r -= BM;
+        if constexpr (MODE == TM_LINEAR) {
+          const int w = r / (FF * 16), j = r % (FF * 16);
+          r = min(w * (FF * 16) + feature(j / 16, j % 16), a.l.N - 1 - f0);
+        }
+        if constexpr (MODE == TM_DOWN) r = min(r, a.f.d - 1 - f0);
+        if constexpr (MODE == TM_UP) {   // a wave's first FF / 2 tiles are gate features, then up of the same
+          const int w = r / (FF * 16), j = r % (FF * 16), up = j >= FF * 8;
+          const int k = up ? j - FF * 8 : j;
+          r = min(f0 + w * (FF * 8) + feature(k / 16, k % 16), a.f.F - 1) + (up ? a.f.F : 0);
+        }
+        off[i] = (unsigned)r * ldw + piece;
+      }
+    }
+  };
   // Requests load i of the next stage (past the last one: that one again,
   // unused).  The second half of an odd reduction's last stage is the first half
   // again.
-  int next = 0;
+  int next;
   auto fetch_one = [&](uint4* buf, int i) {
     const int inst = wv * LPW + i;
     const unsigned over = SPS == 2 && 2 * next + 1 == S && (((lane >> 2) ^ inst) & 1) ? 64u : 0u;
@@ -393,14 +404,17 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     for (int i = 0; i < LPW; ++i) fetch_one(buf, i);
     fetched();
   };
+  auto first_stages = [&]() {
+    next = 0;
+    fetch(b0);
+    fetch(b1);
+    fetch(b2);
+    if constexpr (NST > 3) fetch(b3);
+  };
 
   f32x4 acc[FF][RF], tot[FF][RF];   // the chain, and (linear) the sum of the chains before it
-#pragma unroll
-  for (int f = 0; f < FF; ++f)
-#pragma unroll
-    for (int r = 0; r < RF; ++r) tot[f][r] = acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int chains = MODE == TM_LINEAR ? linear_chains(S) : 1;
-  int ch = 0, ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : S;   // the chain, its last super-step + 1
+  int ch, ch_end;   // the chain, its last super-step + 1
   const int q = grp ^ swizzle(c);
   const int xo = (wr * RF * 16 + c) * PPR + q, wo = (BM + wf * FF * 16 + c) * PPR + q;
   uint4 xs[2][RF], ws[2][FF];   // the fragments of two super-steps
@@ -418,7 +432,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   // super-step's fragments are read and the requests for a later stage go out,
   // spread over the whole stage: all at once, either would hold up the wave's
   // matrix instructions for as long as all waves' reads or requests take.
-  int left = stages;
+  int left;
   auto others = [&](const uint4* cur, uint4* prev, auto ask) {
     --left;
 #pragma unroll
@@ -467,111 +481,141 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       }
     others(cur, prev, std::true_type{});
   };
-  fetch(b0);
-  fetch(b1);
-  fetch(b2);
-  if (NST > 3) fetch(b3);
-  wait_vm<(NST - 1) * LPW>();
-  barrier_only();
-#pragma unroll
-  for (int i = 0; i < FF + RF; ++i) read_one(b0, 0, i);
-  others(b0, nullptr, std::false_type{});
-  {
-    // (whole turns of the buffers without an exit between them, so that the
-    // compiler sees which request each read follows and adds no wait of its
-    // own; then the rest)
-    const int rest = (stages - 1) % NST;
-    for (int g = (stages - 1) / NST; g > 0; --g) {
-      stage(b0, b1);
-      stage(b1, b2);
-      if constexpr (NST == 3) stage(b2, b0);
-      if constexpr (NST == 4) { stage(b2, b3); stage(b3, b0); }
-    }
-    if (rest > 0) {
-      stage(b0, b1);
-      if (rest > 1) {
-        stage(b1, b2);
-        if constexpr (NST > 3)
-          if (rest > 2) stage(b2, b3);
-      }
-    }
-  }
-  if (SPS == 4 || S % 2 == 0) mul(1, 0, MN);   // (an odd reduction ends with half a stage)
-  wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
 
-  if constexpr (MODE == TM_LINEAR) {
-    // Each step over all of the wave's values under one branch of its own: with the
-    // choices inside the loop its code was so long that fetching it bound it
-    // (128 x 256 tiles: 10400 cycles of a workgroup, 4300 so; its 64 stages take 81000).  The residual is read before the first store (y may be
-    // the residual, so the compiler keeps each load behind the stores before it).
-    auto each = [&](auto fn) {
+  // One tile after another: the next one's first stages are requested before
+  // the last one's results are stored.
+  place();
+  first_stages();
+  for (;;) {
 #pragma unroll
-      for (int f = 0; f < FF; ++f)
+    for (int f = 0; f < FF; ++f)
 #pragma unroll
-        for (int r = 0; r < RF; ++r) fn(f, r, t0 + (wr * RF + r) * 16 + c, f0 + wf * (FF * 16) + feature(f, 4 * grp));
-    };
-    const bool vec = linear_vec(a.l);
-    f32x4 res[FF][RF];
-    each([&](int f, int r, int t, int n) { res[f][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
-    if (a.l.res) each([&](int f, int r, int t, int n) { res[f][r] = linear_residual(a.l, t, n, vec); });
-    if (chains > 1) each([&](int f, int r, int, int) { acc[f][r] = tot[f][r] + acc[f][r]; });   // (one chain: the sum as it is, as everywhere)
-    f32x4 bias[FF];
+      for (int r = 0; r < RF; ++r) tot[f][r] = acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    ch = 0;
+    ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : S;
+    left = stages;
+    wait_vm<(NST - 1) * LPW>();
+    barrier_only();
 #pragma unroll
-    for (int f = 0; f < FF; ++f) bias[f] = linear_bias(a.l, f0 + wf * (FF * 16) + feature(f, 4 * grp));
-    each([&](int f, int r, int, int) { acc[f][r] += bias[f]; });
-    auto act = [&](auto kind) { each([&](int f, int r, int, int) { acc[f][r] = activate4(acc[f][r], decltype(kind)::value); }); };
-    switch (a.l.act) {
-      case ACT_SILU: act(std::integral_constant<int, ACT_SILU>{}); break;
-      case ACT_GELU: act(std::integral_constant<int, ACT_GELU>{}); break;
-      case ACT_GELU_TANH: act(std::integral_constant<int, ACT_GELU_TANH>{}); break;
-      case ACT_RELU: act(std::integral_constant<int, ACT_RELU>{}); break;
-      default: break;
-    }
-    each([&](int f, int r, int, int) { acc[f][r] += res[f][r]; });
-    if (wide) {
-      if constexpr (PAIRS) each([&](int f, int r, int t, int n) { if (f % 2 == 0) linear_store8(a.l, t, n, acc[f][r], acc[f + 1][r]); });
-    } else if (vec) {
-      each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], true); });
-    } else {
-      each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], false); });
-    }
-  } else if constexpr (MODE == TM_UP) {
-#pragma unroll
-    for (int f = 0; f < FT; f += PAIRS ? 2 : 1) {
-      const int n = f0 + wf * (FT * 16) + feature(f, 4 * grp);
-      if (n >= a.f.F) continue;
-#pragma unroll
-      for (int r = 0; r < RF; ++r) {
-        const int row = (wr * RF + r) * 16 + c;
-        if (row >= rows) continue;
-        auto glu = [&](int g) {
-          f32x4 v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = silu(acc[g][r][i]) * acc[g + FT][r][i];
-          return v;
-        };
-        const size_t o = (size_t)(et.p0 + row) * a.f.F + n;
-        if constexpr (PAIRS) {   // (F is a multiple of 32)
-          const f32x4 v = glu(f), u = glu(f + 1);
-          *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.p.z) + o) =
-              make_uint4(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]), bf16x2_bits(u[0], u[1]), bf16x2_bits(u[2], u[3]));
-        } else {
-          store4<DT>(a.p.z, o, glu(f));
+    for (int i = 0; i < FF + RF; ++i) read_one(b0, 0, i);
+    others(b0, nullptr, std::false_type{});
+    {
+      // (whole turns of the buffers without an exit between them, so that the
+      // compiler sees which request each read follows and adds no wait of its
+      // own; then the rest)
+      const int rest = (stages - 1) % NST;
+      for (int g = (stages - 1) / NST; g > 0; --g) {
+        stage(b0, b1);
+        stage(b1, b2);
+        if constexpr (NST == 3) stage(b2, b0);
+        if constexpr (NST == 4) { stage(b2, b3); stage(b3, b0); }
+      }
+      if (rest > 0) {
+        stage(b0, b1);
+        if (rest > 1) {
+          stage(b1, b2);
+          if constexpr (NST > 3)
+            if (rest > 2) stage(b2, b3);
         }
       }
     }
-  } else {
+    if (SPS == 4 || S % 2 == 0) mul(1, 0, MN);   // (an odd reduction ends with half a stage)
+    if (chains > 1) {                            // (one chain: the sum as it is, as everywhere)
 #pragma unroll
-    for (int r = 0; r < RF; ++r) {
-      const int row = (wr * RF + r) * 16 + c;
-      if (row >= rows) continue;
-      float* y = a.p.y + (size_t)a.p.order[et.p0 + row] * a.p.nc;
+      for (int f = 0; f < FF; ++f)
 #pragma unroll
-      for (int f = 0; f < FF; ++f) {
-        const int n = f0 - a.p.c0 + (wf * FF + f) * 16 + 4 * grp;
-        if (n < a.p.nc) *reinterpret_cast<f32x4*>(y + n) = acc[f][r];
+        for (int r = 0; r < RF; ++r) acc[f][r] = tot[f][r] + acc[f][r];
+    }
+    wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
+
+    const int ct0 = t0, cf0 = f0, crows = rows, cp0 = et.p0;
+    int oc = c, og = 4 * grp;
+    if constexpr (KEEP) asm volatile("" : "+v"(oc), "+v"(og));   // (as in place())
+    bool more = false;
+    if constexpr (KEEP) {
+      at += (int)(gridDim.x >> 3);
+      more = at < end;
+      if (more) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+        barrier_only();                       // every wave has read its last fragments
+        place();
+        first_stages();
       }
     }
+    if constexpr (MODE == TM_LINEAR) {
+      // Each step over all of the wave's values under one branch of its own: with the
+      // choices inside the loop its code was so long that fetching it bound it
+      // (128 x 256 tiles: 10400 cycles of a workgroup, 4300 so; its 64 stages take 81000).  The residual is read before the first store (y may be
+      // the residual, so the compiler keeps each load behind the stores before it).
+      auto each = [&](auto fn) {
+#pragma unroll
+        for (int f = 0; f < FF; ++f)
+#pragma unroll
+          for (int r = 0; r < RF; ++r) fn(f, r, ct0 + (wr * RF + r) * 16 + oc, cf0 + wf * (FF * 16) + feature(f, og));
+      };
+      const bool vec = linear_vec(a.l);
+      f32x4 res[FF][RF];
+      each([&](int f, int r, int t, int n) { res[f][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+      if (a.l.res) each([&](int f, int r, int t, int n) { res[f][r] = linear_residual(a.l, t, n, vec); });
+      f32x4 bias[FF];
+#pragma unroll
+      for (int f = 0; f < FF; ++f) bias[f] = linear_bias(a.l, cf0 + wf * (FF * 16) + feature(f, og));
+      each([&](int f, int r, int, int) { acc[f][r] += bias[f]; });
+      auto act = [&](auto kind) { each([&](int f, int r, int, int) { acc[f][r] = activate4(acc[f][r], decltype(kind)::value); }); };
+      switch (a.l.act) {
+        case ACT_SILU: act(std::integral_constant<int, ACT_SILU>{}); break;
+        case ACT_GELU: act(std::integral_constant<int, ACT_GELU>{}); break;
+        case ACT_GELU_TANH: act(std::integral_constant<int, ACT_GELU_TANH>{}); break;
+        case ACT_RELU: act(std::integral_constant<int, ACT_RELU>{}); break;
+        default: break;
+      }
+      each([&](int f, int r, int, int) { acc[f][r] += res[f][r]; });
+      if (wide) {
+        if constexpr (PAIRS) each([&](int f, int r, int t, int n) { if (f % 2 == 0) linear_store8(a.l, t, n, acc[f][r], acc[f + 1][r]); });
+      } else if (vec) {
+        each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], true); });
+      } else {
+        each([&](int f, int r, int t, int n) { linear_store(a.l, t, n, acc[f][r], false); });
+      }
+    } else if constexpr (MODE == TM_UP) {
+#pragma unroll
+      for (int f = 0; f < FT; f += PAIRS ? 2 : 1) {
+        const int n = cf0 + wf * (FT * 16) + feature(f, og);
+        if (n >= a.f.F) continue;
+#pragma unroll
+        for (int r = 0; r < RF; ++r) {
+          const int row = (wr * RF + r) * 16 + oc;
+          if (row >= crows) continue;
+          auto glu = [&](int g) {
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = silu(acc[g][r][i]) * acc[g + FT][r][i];
+            return v;
+          };
+          const size_t o = (size_t)(cp0 + row) * a.f.F + n;
+          if constexpr (PAIRS) {   // (F is a multiple of 32)
+            const f32x4 v = glu(f), u = glu(f + 1);
+            *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(a.p.z) + o) =
+                make_uint4(bf16x2_bits(v[0], v[1]), bf16x2_bits(v[2], v[3]), bf16x2_bits(u[0], u[1]), bf16x2_bits(u[2], u[3]));
+          } else {
+            store4<DT>(a.p.z, o, glu(f));
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < RF; ++r) {
+        const int row = (wr * RF + r) * 16 + oc;
+        if (row >= crows) continue;
+        float* y = a.p.y + (size_t)a.p.order[cp0 + row] * a.p.nc;
+#pragma unroll
+        for (int f = 0; f < FF; ++f) {
+          const int n = cf0 - a.p.c0 + (wf * FF + f) * 16 + og;
+          if (n < a.p.nc) *reinterpret_cast<f32x4*>(y + n) = acc[f][r];
+        }
+      }
+    }
+    if (!KEEP || !more) break;
   }
 }
 
@@ -580,7 +624,9 @@ static hipError_t launch_tile(TileArgs a, hipStream_t st) {
   if (MODE == TM_LINEAR) a.nrt = (a.l.T + BM - 1) / BM;
   const int cols = MODE == TM_LINEAR ? a.l.N : MODE == TM_UP ? 2 * a.f.F : a.p.nc;
   a.nft = (cols + BN - 1) / BN;
-  const int64_t n = (int64_t)a.nrt * a.nft;
+  if (MODE == TM_UP) a.kmul = a.f.k > 1 ? 0xffffffffu / a.f.k + 1 : 0;
+  int64_t n = (int64_t)a.nrt * a.nft;
+  if (tile_keeps<MODE, BM, BN, NST, SPS>()) n = std::min<int64_t>(n, 256);   // one for each CU
   hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST, SPS>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
                      st, a);
   return hipGetLastError();
@@ -719,14 +765,18 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   // (us over 4096 bf16 columns).  33 rows, weights from HBM, tiles of 32 x 32 /
   // 64 x 32 / 64 x 64: 4096 features 11.4 / 13.5 / 20 us, 6144 16.7 / 14.5 / 21,
   // 32256 69 / 64 / 54 (one barrier per two super-steps: 16.4 / 17.4 / 20 at
-  // 4096).  256 rows x 4096: 64 x 64 14, 128 x 128 26.  513 x 4096: 64 x 64 35,
-  // 128 x 128 26, 128 x 256 43.  8192 x 11008: 128 x 128 780, 128 x 256 608.
-  auto cost = [&](int64_t m, int64_t n, int64_t turn) {
-    return ((((a.T + m - 1) / m) * ((a.N + n - 1) / n) + 255) / 256) * turn;
+  // 4096).  256 rows x 4096: 64 x 64 14, 128 x 128 26.  513 x 4096: 64 x 64 37,
+  // 128 x 128 26, 128 x 256 41.  With all CUs at work the clock falls, and the
+  // large tiles' turns take 36 and 55: 8192 x 11008 128 x 128 740, 128 x 256 590;
+  // 1024 x 19200 over 7168 columns 331 and 288.
+  auto cost = [&](int64_t m, int64_t n, int64_t turn, int64_t full) {
+    const int64_t tiles = (a.T + m - 1) / m * ((a.N + n - 1) / n);
+    return std::max((tiles + 255) / 256 * turn * 256, tiles * full);
   };
   const int64_t none = INT64_MAX;   // (tiles of more than twice the rows only add reads)
-  const int64_t c0 = cost(32, 32, 9), c1 = cost(64, 32, 14), c2 = cost(64, 64, 18),
-                c3 = a.T > 64 ? cost(128, 128, 27) : none, c4 = a.T > 64 ? cost(128, 256, 46) : none, best = std::min(std::min(std::min(c0, c1), std::min(c2, c3)), c4);
+  const int64_t c0 = cost(32, 32, 9, 9), c1 = cost(64, 32, 14, 14), c2 = cost(64, 64, 18, 18),
+                c3 = a.T > 64 ? cost(128, 128, 27, 36) : none, c4 = a.T > 64 ? cost(128, 256, 43, 55) : none;
+  const int64_t best = std::min({c0, c1, c2, c3, c4});
   if (best == c4) return launch_tile<DT, TM_LINEAR, 128, 256, 2, 4, 3>(t, st);
   if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
   if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 4>(t, st);
