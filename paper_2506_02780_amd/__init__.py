@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import numpy as np
 import torch  # loaded first so the HIP runtime it ships is the one libee.so binds to
@@ -124,6 +125,18 @@ class EEMoeFfnArgs(ctypes.Structure):
 ee_linear = _sig("ee_linear", _i32, [ctypes.POINTER(EELinearArgs), _vp])
 ee_moe_route = _sig("ee_moe_route", _i32, [ctypes.POINTER(EEMoeRouteArgs), _vp])
 ee_moe_ffn = _sig("ee_moe_ffn", _i32, [ctypes.POINTER(EEMoeFfnArgs), _vp])
+
+
+def _packed(name: str, args):
+    """An operator's C call for arguments packed into bytes: (packer, call).  Half a
+    microsecond faster than filling ``args``, which small calls feel."""
+    layout = "@" + "".join(t._type_ for _, t in args._fields_) + "0P"   # (padded at its end as in C)
+    return struct.Struct(layout).pack, ctypes.CFUNCTYPE(_i32, ctypes.c_char_p, _vp)((name, _lib))
+
+
+_OP_LINEAR = _packed("ee_linear", EELinearArgs)
+_OP_ROUTE = _packed("ee_moe_route", EEMoeRouteArgs)
+_OP_FFN = _packed("ee_moe_ffn", EEMoeFfnArgs)
 ee_moe_ffn_workspace_bytes = _sig("ee_moe_ffn_workspace_bytes", _sz, [_i32] * 6)
 
 ACTIVATIONS = ("none", "silu", "gelu", "gelu_tanh", "relu")
@@ -242,13 +255,18 @@ def _out_type(out_dtype, out, x):
 _current_device = torch.cuda.current_device
 
 
-def _operator(fn, args, dev: int):
+def _operator(op, dev: int, *args):
     """Calls an operator on GPU ``dev`` and its current stream."""
+    pack, fn = op
+    try:
+        packed = pack(*args)
+    except (struct.error, OverflowError) as e:
+        raise EEError(EE_EINVAL, f"an argument does not fit its type: {e}") from None
     if dev == _current_device():
-        rc = fn(ctypes.byref(args), _raw_stream(dev))
+        rc = fn(packed, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            rc = fn(ctypes.byref(args), _raw_stream(dev))
+            rc = fn(packed, _raw_stream(dev))
     if rc != EE_OK:
         _check(rc)
 
@@ -274,10 +292,9 @@ def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtyp
     else:
         ldy = _rows_of(out, "out", shape, odt, dev)
     ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
-    _operator(ee_linear, EELinearArgs(x.data_ptr(), w.data_ptr(),
-                                      None if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
-                                      None if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr,
-                                      ldy, rows, cols, n, dt, _TYPES[odt], code), dev)
+    _operator(_OP_LINEAR, dev, x.data_ptr(), w.data_ptr(), 0 if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
+              0 if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr, ldy, rows, cols, n, dt,
+              _TYPES[odt], code)
     return out
 
 
@@ -292,13 +309,12 @@ def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize
     rows, n = logits.shape
     ld = _rows_of(logits, "logits", (rows, n), logits.dtype, dev)
     k = int(top_k)
-    shape = (rows, k if k > 0 else 0)
+    shape = (rows, k if 0 < k <= n else 0)   # (refused below)
     ids = logits.new_empty(shape, dtype=torch.int32)
     weights = logits.new_empty(shape, dtype=torch.float32)
-    _operator(ee_moe_route, EEMoeRouteArgs(logits.data_ptr(),
-                                           None if bias is None else _whole(bias, "bias", (n,), torch.float32, dev), ids.data_ptr(),
-                                           weights.data_ptr(), ld, rows, n, k, dt, code, 1 if renormalize else 0,
-                                           int(n_groups), int(top_groups), int(group_top), scale), dev)
+    _operator(_OP_ROUTE, dev, logits.data_ptr(), 0 if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
+              ids.data_ptr(), weights.data_ptr(), ld, rows, n, k, dt, code, 1 if renormalize else 0, int(n_groups),
+              int(top_groups), int(group_top), scale)
     return ids, weights
 
 
@@ -334,9 +350,8 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or workspace.get_device() != dev
           or not workspace.is_contiguous()):
         raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")
-    _operator(ee_moe_ffn, EEMoeFfnArgs(*pointers, None if residual is None else residual.data_ptr(),
-                                       out.data_ptr(), workspace.data_ptr(), workspace.numel(), ldx, ldr, ldo, rows, E, k,
-                                       d, f, dt, _TYPES[odt]), dev)
+    _operator(_OP_FFN, dev, *pointers, 0 if residual is None else residual.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+              workspace.numel(), ldx, ldr, ldo, rows, E, k, d, f, dt, _TYPES[odt])
     return out
 
 

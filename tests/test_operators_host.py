@@ -114,3 +114,21 @@ def test_python_refusals_without_a_gpu(ee):
         with pytest.raises(ee.EEError) as e:
             call()
         assert e.value.code == ee.EE_EINVAL
+
+
+@pytest.mark.parametrize("op,name", [("_OP_LINEAR", "EELinearArgs"), ("_OP_ROUTE", "EEMoeRouteArgs"), ("_OP_FFN", "EEMoeFfnArgs")])
+def test_packed_arguments_are_the_struct(ee, op, name):
+    # every field with a value of its own, the last byte of the struct included
+    args = getattr(ee, name)
+    values = [1 + i * (1 << 40 if ctypes.sizeof(t) == 8 else 1 << 20) for i, (_, t) in enumerate(args._fields_)]
+    packed = getattr(ee, op)[0](*values)
+    assert len(packed) == ctypes.sizeof(args)
+    back = args.from_buffer_copy(packed)
+    assert [getattr(back, n) or 0 for n, _ in args._fields_] == values
+
+
+def test_arguments_past_their_type_are_refused(ee):
+    for bad in (1 << 31, -(1 << 31) - 1):
+        with pytest.raises(ee.EEError) as e:
+            ee._operator(ee._OP_ROUTE, 0, 0, 0, 0, 0, 0, bad, 1, 1, 0, 0, 0, 1, 1, 1, 1.0)
+        assert e.value.code == ee.EE_EINVAL
