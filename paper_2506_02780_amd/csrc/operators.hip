@@ -8,7 +8,10 @@
 //     super-steps (32 columns in bf16, 16 in fp32: one fragment) in order; a
 //     linear sums several such chains, in order, their number a function of
 //     the reduction's length (linear_chains) or, for at most NARROW outputs (a
-//     router), eight;
+//     router), eight; the experts' in fp32 are chains of EXPERT_CHAIN super-steps
+//     (their results pass through two products: with one chain each over 7168
+//     columns they are 2.3e-6 off, with these 5e-7; in bf16 the rounding of z
+//     hides it, and one chain it is);
 //   * an experts' row is sum_j fma(w_j, y_j) over its slots in order, in fp32.
 
 #include "operators.h"
@@ -25,6 +28,7 @@ namespace ee {
 // Bytes of a row that one super-step covers: 32 bf16 or 16 fp32 values, 16
 // bytes per lane group.
 constexpr int STEP = 64;
+constexpr int EXPERT_CHAIN = 16;
 
 // acc[n][m] += (16 features of wp[n]) x (16 rows of xp[m]) over S super-steps.  wp and
 // xp point to the lane's own 16 bytes of step 0.  D steps are in flight: a step's
@@ -33,10 +37,11 @@ constexpr int STEP = 64;
 // multiplied meanwhile), so D is what the registers hold; whole turns of D
 // have no branch between their steps, where the compiler would wait for more
 // than the step needs (one decoded token through 8 experts, 2048 x 768: 25 us
-// with a test per step and two alternating sets of 8, 13 us).
+// with a test per step and two alternating sets of 8, 13 us).  FOLD: every D steps
+// are a chain of their own, the chains added in order.
 typedef const __attribute__((address_space(1))) unsigned char global_bytes;
 typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
-template <int DT, int NT, int MT, int D>
+template <int DT, int NT, int MT, int D, bool FOLD = false>
 __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], const unsigned char* const (&xptr)[MT], int S,
                                       f32x4 (&acc)[NT][MT]) {
   // (global pointers by type: through the loop the compiler loses that they
@@ -66,6 +71,16 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
 #pragma unroll
     for (int m = 0; m < MT; ++m) xp[m] += D * STEP;
   };
+  f32x4 tot[NT][MT];
+  auto fold = [&](bool first) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        tot[n][m] = first ? f32x4{0.f, 0.f, 0.f, 0.f} + acc[n][m] : tot[n][m] + acc[n][m];
+        acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+  };
   const int turns = S / D, rest = S % D;
   if (turns) {
 #pragma unroll
@@ -77,6 +92,7 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
         mul(i);
         load(i);
       }
+      if constexpr (FOLD) fold(g == 1);
       next();
     }
 #pragma unroll
@@ -84,6 +100,8 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
       mul(i);
       if (i < rest) load(i);
     }
+    if constexpr (FOLD)
+      if (rest) fold(turns == 1);
   } else {
 #pragma unroll
     for (int i = 0; i < D; ++i)
@@ -92,6 +110,13 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
 #pragma unroll
   for (int i = 0; i < D; ++i)
     if (i < rest) mul(i);
+  if constexpr (FOLD)
+    if (S > D) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = tot[n][m] + acc[n][m];
+    }
 }
 
 // Four consecutive values, rounded to the type, from an aligned element index.
@@ -282,10 +307,10 @@ struct TileArgs {
 // Whether a workgroup takes one tile after another, so that the next one's first
 // stages are on their way while the last one's results are stored: where only one
 // workgroup fits a CU and reductions are short (8192 rows of 128 experts, 2048 x
-// 768: 942 us without, 903 so; linears gain nothing, 8192 x 11008 606 us without, 612 so: the
-// sums of their chains leave too few registers, and their clock is lower).
-template <int MODE, int BM, int BN, int NST, int SPS> constexpr bool tile_keeps() {
-  return MODE != TM_LINEAR && (BM + BN) * SPS * 64 * NST > 80 * 1024;
+// 768: 942 us without, 903 so; linears and fp32 gain nothing, 8192 x 11008 606 us without,
+// 612 so: the sums of their chains leave too few registers).
+template <int DT, int MODE, int BM, int BN, int NST, int SPS> constexpr bool tile_keeps() {
+  return MODE != TM_LINEAR && DT != DT_F32 && (BM + BN) * SPS * 64 * NST > 80 * 1024;
 }
 
 template <int DT, int MODE, int BM, int BN, int WR, int WF, int NST, int SPS>
@@ -294,7 +319,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   constexpr int PPR = 4 * SPS, RPL = 64 / PPR;   // 16-byte pieces of a row's stage, rows per load
   constexpr int LPW = (BM + BN) / RPL / WAVES;   // loads per wave and stage
   constexpr int STAGE = (BM + BN) * PPR;         // pieces of a stage
-  constexpr bool KEEP = tile_keeps<MODE, BM, BN, NST, SPS>();
+  constexpr bool KEEP = tile_keeps<DT, MODE, BM, BN, NST, SPS>();
   static_assert(SPS == 2 || SPS == 4, "two fragment sets in turn, rows of 8 or 16 pieces");
   static_assert((BM + BN) % (RPL * WAVES) == 0 && BM % RPL == 0, "every wave loads as much");
   static_assert(MODE != TM_UP || FF % 2 == 0, "a wave owns gate and up tiles of the same features");
@@ -412,8 +437,9 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     if constexpr (NST > 3) fetch(b3);
   };
 
-  f32x4 acc[FF][RF], tot[FF][RF];   // the chain, and (linear) the sum of the chains before it
-  const int chains = MODE == TM_LINEAR ? linear_chains(S) : 1;
+  f32x4 acc[FF][RF], tot[FF][RF];   // the chain, and the sum of the chains before it
+  constexpr bool FOLD = MODE == TM_LINEAR || DT == DT_F32;
+  const int chains = MODE == TM_LINEAR ? linear_chains(S) : FOLD ? (S + EXPERT_CHAIN - 1) / EXPERT_CHAIN : 1;
   int ch, ch_end;   // the chain, its last super-step + 1
   const int q = grp ^ swizzle(c);
   const int xo = (wr * RF * 16 + c) * PPR + q, wo = (BM + wf * FF * 16 + c) * PPR + q;
@@ -468,9 +494,9 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       mul(1, j * MN / PARTS, (j + 1) * MN / PARTS);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (MODE == TM_LINEAR)
+    if constexpr (FOLD)
       if ((stages - left) * SPS == ch_end) {   // the stage before ended a chain
-        ch_end = chain_start(++ch + 1, S, chains);
+        ch_end = MODE == TM_LINEAR ? chain_start(++ch + 1, S, chains) : ch_end + EXPERT_CHAIN;
 #pragma unroll
         for (int f = 0; f < FF; ++f)
 #pragma unroll
@@ -492,7 +518,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 #pragma unroll
       for (int r = 0; r < RF; ++r) tot[f][r] = acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
     ch = 0;
-    ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : S;
+    ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : EXPERT_CHAIN;
     left = stages;
     wait_vm<(NST - 1) * LPW>();
     barrier_only();
@@ -520,7 +546,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       }
     }
     if (SPS == 4 || S % 2 == 0) mul(1, 0, MN);   // (an odd reduction ends with half a stage)
-    if (chains > 1) {                            // (one chain: the sum as it is, as everywhere)
+    if (FOLD && chains > 1) {                            // (one chain: the sum as it is, as everywhere)
 #pragma unroll
       for (int f = 0; f < FF; ++f)
 #pragma unroll
@@ -626,7 +652,7 @@ static hipError_t launch_tile(TileArgs a, hipStream_t st) {
   a.nft = (cols + BN - 1) / BN;
   if (MODE == TM_UP) a.kmul = a.f.k > 1 ? 0xffffffffu / a.f.k + 1 : 0;
   int64_t n = (int64_t)a.nrt * a.nft;
-  if (tile_keeps<MODE, BM, BN, NST, SPS>()) n = std::min<int64_t>(n, 256);   // one for each CU
+  if (tile_keeps<DT, MODE, BM, BN, NST, SPS>()) n = std::min<int64_t>(n, 256);   // one for each CU
   hipLaunchKernelGGL((tile_kernel<DT, MODE, BM, BN, WR, WF, NST, SPS>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(WR * WF * 64), 0,
                      st, a);
   return hipGetLastError();
@@ -1048,7 +1074,7 @@ __global__ __launch_bounds__(64, 2) void ffn_up_kernel(FfnArgs a, void* z, int n
   const unsigned char* wp[2] = {w, w + (size_t)a.F * rb};
   const unsigned char* xp[1] = {reinterpret_cast<const unsigned char*>(a.x) + (size_t)(p / a.k) * a.ldx * ESZ + grp * 16};
   f32x4 acc[2][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}, {f32x4{0.f, 0.f, 0.f, 0.f}}};
-  chain<DT, 2, 1, 16>(wp, xp, a.d / Geo<DT>::KS, acc);
+  chain<DT, 2, 1, EXPERT_CHAIN, DT == DT_F32>(wp, xp, a.d / Geo<DT>::KS, acc);
   f32x4 v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = silu(acc[0][0][i]) * acc[1][0][i];
@@ -1073,7 +1099,7 @@ __global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a,
     const unsigned char* wp[1] = {reinterpret_cast<const unsigned char*>(a.wd) + ((size_t)e * a.d + n0 + c) * rb + grp * 16};
     const unsigned char* zp[1] = {reinterpret_cast<const unsigned char*>(z) + p * rb + grp * 16};
     f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
-    chain<DT, 1, 1, 24>(wp, zp, a.F / Geo<DT>::KS, acc);
+    chain<DT, 1, 1, DT == DT_F32 ? EXPERT_CHAIN : 24, DT == DT_F32>(wp, zp, a.F / Geo<DT>::KS, acc);
     if (c == 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[j][4 * grp + i] = acc[0][0][i];

@@ -411,6 +411,30 @@ def test_ffn_rows_do_not_depend_on_the_others(ee, dtype, E, k):
             assert torch.equal(ee.moe_ffn(x[s], gu, dn, ids[s].contiguous(), w[s].contiguous()), whole[s]), (rows, lo)
 
 
+@pytest.mark.parametrize("d,f", [(32, 256), (240, 272), (256, 240), (272, 528), (528, 1040), (1040, 512), (2064, 784)])
+def test_ffn_fp32_chains(ee, d, f):
+    # reductions that end before, at and behind a chain of 256 columns, by the kernels
+    # of few pairs and of every tile
+    x, gu, dn, ids, w = [t.cuda() for t in _ffn_inputs(1200, d, f, 4, 2, "f32", seed=d)]
+    whole = ee.moe_ffn(x, gu, dn, ids, w)
+    for rows in (1, 7, 40, 200):
+        assert torch.equal(ee.moe_ffn(x[:rows], gu, dn, ids[:rows].contiguous(), w[:rows].contiguous()), whole[:rows]), rows
+
+
+@pytest.mark.parametrize("rows", [9, 300])
+@pytest.mark.parametrize("d,f", [(7168, 256), (256, 4096)])
+def test_ffn_fp32_long_reductions(ee, rows, d, f):
+    # A chain of 256 columns adds its four-column steps one after another: at most 256
+    # roundings of 0.29 ulp (rms, 2^-24 sqrt(1/3)) of partial sums whose rms is
+    # sqrt(1/2) of the whole: 16 * 0.58 * 0.71 * 2^-24 = 4e-7, the chains' own sum
+    # (28 of them) 1.3e-7 more; the gate's, the up's and the down's errors add as
+    # squares: below 7.3e-7.  (One chain of 7168 columns: 2.3e-6.)
+    x, gu, dn, ids, w = [t.cuda() for t in _ffn_inputs(rows, d, f, 4, 2, "f32", seed=rows)]
+    want, _ = _ffn64(x, gu, dn, ids, w, None, "f32")
+    err = (ee.moe_ffn(x, gu, dn, ids, w).double() - want).norm() / want.norm()
+    assert err < 1e-6, float(err)
+
+
 # ---------------------------------------------------------- as they are used --
 
 def _layer(ee, h, gain, router, gu, dn, k, **kw):
