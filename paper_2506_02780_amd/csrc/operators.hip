@@ -800,12 +800,20 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
     return std::max((tiles + 255) / 256 * turn * 256, tiles * full);
   };
   const int64_t none = INT64_MAX;   // (tiles of more than twice the rows only add reads)
-  const int64_t c0 = cost(32, 32, 9, 9), c1 = cost(64, 32, 14, 14), c2 = cost(64, 64, 18, 18),
-                c3 = a.T > 64 ? cost(128, 128, 27, 36) : none, c4 = a.T > 64 ? cost(128, 256, 43, 55) : none;
+  // fp32 is bound by its matrix instructions, a sixteenth as fast, and what counts
+  // is that all CUs have the same work: over 4096 columns 32 x 32 25 us, 19 with
+  // more than one on a CU, 64 x 64 67 and 62, 128 x 128 239.  513 x 4096: 32 x 32 169,
+  // 64 x 64 188, 128 x 128 243; 2000 x 2000 over 2048 columns 153, 128, 125; 64 x 64
+  // with eight waves 4 to 8 % faster than with four.
+  const bool f32 = DT == DT_F32;
+  const int64_t c0 = f32 ? cost(32, 32, 19, 19) : cost(32, 32, 9, 9), c1 = f32 ? cost(64, 32, 40, 40) : cost(64, 32, 14, 14),
+                c2 = f32 ? cost(64, 64, 62, 62) : cost(64, 64, 18, 18),
+                c3 = a.T <= 64 ? none : f32 ? cost(128, 128, 239, 240) : cost(128, 128, 27, 36),
+                c4 = a.T <= 64 ? none : f32 ? cost(128, 256, 466, 480) : cost(128, 256, 43, 55);
   const int64_t best = std::min({c0, c1, c2, c3, c4});
   if (best == c4) return launch_tile<DT, TM_LINEAR, 128, 256, 2, 4, 3>(t, st);
   if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
-  if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, 2, 4>(t, st);
+  if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, DT == DT_F32 ? 4 : 2, 4>(t, st);
   const bool four = a.K / Geo<DT>::KS % 4 == 0;
   if (best == c1)
     return four ? launch_tile<DT, TM_LINEAR, 64, 32, 4, 2, 4, 4>(t, st) : launch_tile<DT, TM_LINEAR, 64, 32, 2, 2, 4, 2>(t, st);
@@ -1284,13 +1292,15 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
   // experts of 768 over 2048, 8 per row, tiles of 32 x 64 / 64 x 256 / 128 x 256: 33
   // rows 156 / 173 / 178 us, 257 247 / 239 / 241, 513 303 / 270 / 283, 1025 412 /
   // 319 / 309, 8192 1845 / 1173 / 933; 8 experts of 352 over 256, 2 per row, 257
-  // rows 13.7 / 19 / 26, 8192 62 / 54 / 45.
+  // rows 13.7 / 19 / 26, 8192 62 / 54 / 45.  In fp32 the matrix instructions bound
+  // the tiles (8 experts of 1024 over 512, 2 per row, 1000 rows: 64 x 256 81 us, 128 x 256 141).
   auto cost = [&](int BM, int BN, double turn) {
     const double rt = std::max(distinct, (double)P / BM + distinct / 2);
     auto turns = [&](int cols) { return ceil(rt * ((cols + BN - 1) / BN) / 256.0); };
     return turn * (turns(2 * a.F) * a.d + turns(a.d) * a.F);
   };
-  const double c0 = cost(32, 64, 9), c1 = cost(64, 256, 30), c2 = cost(128, 256, 46);
+  const bool f32 = DT == DT_F32;
+  const double c0 = cost(32, 64, f32 ? 39 : 9), c1 = cost(64, 256, f32 ? 240 : 30), c2 = cost(128, 256, f32 ? 470 : 46);
   const int BM = P < 8 * a.E || (c0 <= c1 && c0 <= c2) ? 32 : c1 <= c2 ? 64 : 128;
   TileArgs t{};
   t.f = a;
