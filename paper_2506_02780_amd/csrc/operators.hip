@@ -1287,20 +1287,24 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   // The tile whose turns of the chip take least, as for a linear (row tiles: every
-  // expert that is met ends in half a tile on average); with fewer than eight rows
-  // per expert the weights' stream is all, and the smallest does best.  128
-  // experts of 768 over 2048, 8 per row, tiles of 32 x 64 / 64 x 256 / 128 x 256: 33
-  // rows 156 / 173 / 178 us, 257 247 / 239 / 241, 513 303 / 270 / 283, 1025 412 /
-  // 319 / 309, 8192 1845 / 1173 / 933; 8 experts of 352 over 256, 2 per row, 257
-  // rows 13.7 / 19 / 26, 8192 62 / 54 / 45.  In fp32 the matrix instructions bound
-  // the tiles (8 experts of 1024 over 512, 2 per row, 1000 rows: 64 x 256 81 us, 128 x 256 141).
+  // expert that is met ends in half a tile on average, so whether a last turn
+  // is begun is even); with fewer than eight rows per expert the weights' stream
+  // is all, and the smallest does best.  128 experts of 768 over 2048, 8 per row, tiles
+  // of 32 x 64 / 64 x 256 / 128 x 256: 33 rows 205 / 210 / 213 us, 257 236 / 238 / 243, 513
+  // 297 / 250 / 256, 1025 394 / 311 / 280, 4096 1087 / 674 / 555; 8 experts of 352 over
+  // 256, 2 per row, 257 rows 18.5 / 20.4 / 21.8, 8192 59 / 52 / 44; 8 of 2048 over 1024, 1000
+  // rows 81 / 67 / 70.  In fp32 the matrix instructions bound the tiles (8 experts of
+  // 1024 over 512, 2 per row, 1000 rows: 64 x 256 81 us, 128 x 256 141).
   auto cost = [&](int BM, int BN, double turn) {
     const double rt = std::max(distinct, (double)P / BM + distinct / 2);
-    auto turns = [&](int cols) { return ceil(rt * ((cols + BN - 1) / BN) / 256.0); };
+    auto turns = [&](int cols) {
+      const double n = rt * ((cols + BN - 1) / BN) / 256.0;
+      return std::max(1.0, (n + ceil(n)) / 2);
+    };
     return turn * (turns(2 * a.F) * a.d + turns(a.d) * a.F);
   };
   const bool f32 = DT == DT_F32;
-  const double c0 = cost(32, 64, f32 ? 39 : 9), c1 = cost(64, 256, f32 ? 240 : 30), c2 = cost(128, 256, f32 ? 470 : 46);
+  const double c0 = cost(32, 64, f32 ? 39 : 9), c1 = cost(64, 256, f32 ? 240 : 30), c2 = cost(128, 256, f32 ? 470 : 40);
   const int BM = P < 8 * a.E || (c0 <= c1 && c0 <= c2) ? 32 : c1 <= c2 ? 64 : 128;
   TileArgs t{};
   t.f = a;
