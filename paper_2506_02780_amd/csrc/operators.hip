@@ -289,12 +289,14 @@ struct TileArgs {
 
 // Products of BM rows with BN rows of weights, both streamed through LDS in
 // stages of SPS super-steps (64 bytes of a row each), NST stages deep.  What bounds
-// a large product is that every wave reads its fragments from LDS while the
-// matrix cores run: a wave of RF x FF fragments reads RF + FF per RF FF matrix
-// instructions.  The largest tile, 128 x 256 with eight waves of 64 x 64, keeps two
-// stages in flight and the matrix cores busy two thirds of the clocks; with
-// all CUs at work the clock itself falls to about 1.9 GHz (the same tile alone:
-// 0.75 of the time).
+// a large product is power, and then what shares the CU with the matrix
+// cores: fragments read from LDS (a wave of RF x FF fragments reads RF + FF per RF FF
+// matrix instructions) and requests written to it.  The largest tile, 128 x 256 with
+// eight waves of 64 x 64, keeps two stages in flight and takes 80400 clocks for 4096
+// columns where its matrix instructions alone take 65536; with all CUs at work the
+// clock falls from 2.4 to 1.6 GHz (8192 x 4096 x 11008: 590 us, 1250 TFLOP/s; all
+// requests left out, 540).  Tiles of 256 x 256 (four waves of 128 x 128, or eight) take
+// 4 % fewer clocks over 4096 features, more over 11008, and no less time.
 //   * Stages arrive by direct loads to LDS, each of whole lines (SPS = 2: eight
 //     rows of 128 bytes; 4: four of 256).  The 16-byte pieces of row r stand at
 //     place piece ^ (r / 2 % 8) or piece ^ (r % 16), so that the 16 rows that a
@@ -1223,7 +1225,7 @@ __global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a, FfnPlan p) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// (row tiles of 16 rows at least: what the smallest tile needs holds for all)
+// (what the smallest row tile needs holds for all)
 size_t ffn_tiles(int64_t P, int E, int BM) { return (size_t)(P / BM + std::min<int64_t>(P, E)); }
 constexpr int MIN_BM = 32;
 
