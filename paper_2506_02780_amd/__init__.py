@@ -128,8 +128,8 @@ ee_moe_ffn = _sig("ee_moe_ffn", _i32, [ctypes.POINTER(EEMoeFfnArgs), _vp])
 
 
 def _packed(name: str, args):
-    """An operator's C call for arguments packed into bytes: (packer, call).  Half a
-    microsecond faster than filling ``args``, which small calls feel."""
+    """An operator's C call for arguments packed into bytes: (packer, call).  A third of
+    a microsecond less than filling ``args``, a twentieth of a small call."""
     layout = "@" + "".join(t._type_ for _, t in args._fields_) + "0P"   # (padded at its end as in C)
     return struct.Struct(layout).pack, ctypes.CFUNCTYPE(_i32, ctypes.c_char_p, _vp)((name, _lib))
 
@@ -246,7 +246,7 @@ def _operand(x, what: str):
 
 
 def _out_type(out_dtype, out, x):
-    odt = out_dtype or (x.dtype if out is None else out.dtype)
+    odt = out_dtype or (x.dtype if out is None else getattr(out, "dtype", None))
     if odt not in _TYPES:
         raise EEError(EE_EINVAL, "out_dtype must be float32 or bfloat16")
     return odt

@@ -57,6 +57,8 @@ int32_t ee_linear(const ee_linear_args* p, void* stream) {
     return bad("residual must be aligned to its type with a row stride of at least `out`");
   if (q.bias && !aligned(q.bias, 4)) return bad("bias must be aligned to its type");
   if ((int64_t)((q.rows + 15) / 16) * ((q.out + 15) / 16) > MAX_BLOCKS) return bad("too many output tiles");
+  if (q.y == q.x || q.y == q.w || q.y == q.bias || (q.y == q.residual && q.ldr != q.ldy))
+    return bad("y must not be an input, except the residual with its stride");
   ee::LinearArgs a{};
   a.x = q.x; a.w = q.w; a.bias = q.bias; a.res = q.residual; a.y = q.y;
   a.ldx = q.ldx; a.ldw = q.ldw; a.ldr = q.ldr; a.ldy = q.ldy;
@@ -127,6 +129,8 @@ int32_t ee_moe_ffn(const ee_moe_ffn_args* p, void* stream) {
   if (!aligned(q.workspace, 256)) return bad("workspace must be 256-byte aligned");
   if (q.workspace_bytes < ee::ffn_workspace(q.rows, q.n_experts, q.top_k, q.d_model, q.ffn, dt_of(q.dtype)))
     return op_fail(EE_ECAPACITY, "workspace smaller than ee_moe_ffn_workspace_bytes");
+  if (q.out == q.x || q.out == q.weights || q.out == q.workspace || (q.out == q.residual && q.ldr != q.ldo))
+    return bad("out must not be an input or the workspace, except the residual with its stride");
   ee::FfnArgs a{};
   a.x = q.x; a.wgu = q.w_gate_up; a.wd = q.w_down; a.ids = q.ids; a.weights = q.weights; a.res = q.residual; a.out = q.out;
   a.ldx = q.ldx; a.ldr = q.ldr; a.ldo = q.ldo;

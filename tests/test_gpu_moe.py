@@ -7,7 +7,7 @@ import pytest
 
 from oracle import OracleSession
 from tests.helpers import reuse_session_parity
-from workloads import gen_weights, get_shape, planted_draft, random_tree, tree_tokens, zipf_tokens
+from workloads import gen_weights, get_shape, inject_edits, planted_draft, random_tree, tree_tokens, zipf_tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -144,6 +144,35 @@ def test_prompt_blocks_do_not_change_results(ee):
         for x, y in zip(eng.read_kv(0, l), eng.read_kv(1, l)):
             assert np.array_equal(x, y)
     eng.close()
+
+
+def test_other_verifications_and_an_edit_session(ee):
+    """Top-1 and low-temperature sampled verification accept what the greedy one
+    does, and an edit session with a sparse target and a sparse draft model
+    emits the target's own greedy stream."""
+    shape, dshape = _bf16(), _bf16(n_layers=1, n_experts=8, top_k=2)
+    w = gen_weights(shape, seed=41, std=0.08)
+    prompt = zipf_tokens(shape.vocab, 120, seed=42)
+    eng = ee.Engine(shape, w, max_ctx=600, k_max=32)
+    first = eng.prefill(0, prompt)
+    stream = [first] + [eng.verify(0, [])[1] for _ in range(160)]
+    g = np.random.default_rng(43)
+    for k, good in ((1, 1), (7, 3), (20, 20), (32, 11)):
+        d = planted_draft(stream[1:], good, k, shape.vocab, seed=k)
+        eng.rollback(0, 120, first)
+        assert eng.verify_topk([0], [d], 1, dynamic=False)[0][:2] == (good, stream[good + 1])
+        eng.rollback(0, 120, first)
+        assert eng.verify_sample(0, d, g.random(k) * 0.99, g.random(k + 1) * 0.99, None, 1e-4, True) == (good, stream[good + 1])
+    eng.rollback(0, 120, first)
+    original, _ = inject_edits(np.asarray(stream, dtype=np.int32), shape.vocab, seed=44, frac=0.1)
+    drf = ee.Engine(dshape, gen_weights(dshape, seed=45, std=0.08), max_ctx=600, k_max=32)
+    drf.prefill(0, prompt)
+    s = ee.EditSession(eng, 0, original, drf, 0, k_reuse=16, gamma=5)
+    while s.n < 160:
+        s.step()
+    assert s.output[:160] == stream[:160]
+    eng.close()
+    drf.close()
 
 
 def test_refused_on_sparse_models(ee):

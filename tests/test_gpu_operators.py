@@ -411,6 +411,24 @@ def test_ffn_rows_do_not_depend_on_the_others(ee, dtype, E, k):
             assert torch.equal(ee.moe_ffn(x[s], gu, dn, ids[s].contiguous(), w[s].contiguous()), whole[s]), (rows, lo)
 
 
+@pytest.mark.parametrize("rows,d,f,E,k", [(6000, 512, 512, 8, 2), (5001, 544, 288, 3, 1), (3000, 1024, 256, 64, 4), (9000, 288, 2080, 2, 2)])
+def test_ffn_many_tiles_per_workgroup(ee, rows, d, f, E, k):
+    # more row and feature tiles than compute units, experts of very different size,
+    # rows without an expert: the same bits as a few of the rows alone, which the
+    # tests above compare with float64
+    x, gu, dn, ids, w = [t.cuda() for t in _ffn_inputs(rows, d, f, E, k, "bf16", seed=rows, skew=2.0)]
+    ids[::97] = -1
+    whole = ee.moe_ffn(x, gu, dn, ids, w)
+    for lo in (0, 1000, rows // 2 - 13, rows - 31):
+        s = slice(lo, lo + 31)
+        assert torch.equal(ee.moe_ffn(x[s], gu, dn, ids[s].contiguous(), w[s].contiguous()), whole[s]), lo
+    pick = torch.arange(0, rows, rows // 50, device="cuda")
+    want, err = _ffn64(x[pick], gu, dn, ids[pick], w[pick], None, "bf16")
+    _close(whole[pick], want.cpu(), (err + UBF * (want.abs() + err) + 2 * U32 * want.abs() + 1e-30).cpu())
+    for _ in range(3):
+        assert torch.equal(ee.moe_ffn(x, gu, dn, ids, w), whole)
+
+
 @pytest.mark.parametrize("d,f", [(32, 256), (240, 272), (256, 240), (272, 528), (528, 1040), (1040, 512), (2064, 784)])
 def test_ffn_fp32_chains(ee, d, f):
     # reductions that end before, at and behind a chain of 256 columns, by the kernels
@@ -632,6 +650,17 @@ def test_python_refusals(ee):
         assert e.value.code == ee.EE_EINVAL, i
     with torch.no_grad():
         ee.linear(x, w.clone().requires_grad_())
+
+
+def test_more_python_refusals(ee):
+    x, w = torch.zeros(4, 64, device="cuda"), torch.zeros(64, 64, device="cuda")
+    for i, call in enumerate((lambda: ee.linear(x, w, out=x), lambda: ee.linear(x, w, out=5), lambda: ee.linear(x, w, out=np.zeros((4, 64))),
+                              lambda: ee.moe_route(x, 1 << 40), lambda: ee.moe_route(x, 4, n_groups=1 << 40),
+                              lambda: ee.moe_route(x, 4, scale=float("inf")), lambda: ee.moe_route(x, 4, scale=None),
+                              lambda: ee.linear(x.expand(4, 64)[:1].expand(4, 64), w))):
+        with pytest.raises(ee.EEError) as e:
+            call()
+        assert e.value.code == ee.EE_EINVAL, i
 
 
 def test_empty_calls(ee):

@@ -132,3 +132,14 @@ def test_arguments_past_their_type_are_refused(ee):
         with pytest.raises(ee.EEError) as e:
             ee._operator(ee._OP_ROUTE, 0, 0, 0, 0, 0, 0, bad, 1, 1, 0, 0, 0, 1, 1, 1, 1.0)
         assert e.value.code == ee.EE_EINVAL
+
+
+def test_outputs_that_are_inputs_are_refused(ee):
+    apart = dict(rows=1, w=2 * P, bias=3 * P, residual=4 * P, y=5 * P)
+    for kw in (dict(y=P), dict(y=2 * P), dict(y=3 * P), dict(y=4 * P, ldr=56)):
+        assert _linear(ee, **{**apart, **kw}) == ee.EE_EINVAL, kw
+        assert b"must not be an input" in ee.ee_last_error(None)
+    apart = dict(rows=1, w_gate_up=2 * P, w_down=3 * P, ids=4 * P, weights=5 * P, residual=6 * P, out=7 * P, workspace=8 * P)
+    for kw in (dict(out=P), dict(out=5 * P), dict(out=8 * P), dict(out=6 * P, ldr=72)):
+        assert _ffn(ee, **{**apart, **kw}) == ee.EE_EINVAL, kw
+        assert b"must not be an input" in ee.ee_last_error(None)
