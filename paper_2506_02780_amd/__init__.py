@@ -236,20 +236,27 @@ def _whole(t, what: str, shape, dtype, dev) -> int:
 
 
 def _operand(x, what: str):
-    """Device index and EE_* type of a call's first operand."""
+    """Checks a call's first operand, [rows, cols] of unit column stride: (device
+    index, EE_* type, rows, cols, row stride)."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda:
         raise EEError(EE_EINVAL, f"{what} must be a two-dimensional tensor on a GPU")
     dt = _TYPES.get(x.dtype)
     if dt is None:
         raise EEError(EE_EINVAL, f"{what} must be float32 or bfloat16")
-    return x.get_device(), dt
+    dev = x.get_device()
+    rows, cols = x.shape
+    ld, cs = x.stride()
+    if (cs != 1 and cols > 1) or (x.requires_grad and torch.is_grad_enabled()):
+        _refuse(what, (rows, cols), x.dtype, dev, x)
+    return dev, dt, rows, cols, ld if rows > 1 or ld > cols else cols
 
 
 def _out_type(out_dtype, out, x):
-    odt = out_dtype or (x.dtype if out is None else getattr(out, "dtype", None))
-    if odt not in _TYPES:
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else getattr(out, "dtype", None)
+    if out_dtype not in _TYPES:
         raise EEError(EE_EINVAL, "out_dtype must be float32 or bfloat16")
-    return odt
+    return out_dtype
 
 
 _current_device = torch.cuda.current_device
@@ -275,15 +282,13 @@ def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtyp
     """act(x w^T + bias) + residual (ee_linear).  x [rows, in] and w [out, in]
     in float32 or bfloat16, bias [out] float32, residual [rows, out] in the
     output's dtype (``out_dtype``: x's, or float32).  ``out`` may be the residual."""
-    dev, dt = _operand(x, "x")
+    dev, dt, rows, cols, ldx = _operand(x, "x")
     code = _ACT_OF.get(act)
     if code is None:
         raise EEError(EE_EINVAL, f"act must be one of {ACTIVATIONS}")
     if not isinstance(w, torch.Tensor) or w.dim() != 2:
         raise EEError(EE_EINVAL, "w must be [out, in]")
-    rows, cols = x.shape
     n = w.shape[0]
-    ldx = _rows_of(x, "x", (rows, cols), x.dtype, dev)
     ldw = _rows_of(w, "w", (n, cols), x.dtype, dev)
     odt = _out_type(out_dtype, out, x)
     shape = (rows, n)
@@ -302,12 +307,10 @@ def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize
               n_groups: int = 1, top_groups: int = 1, group_top: int = 1):
     """Experts and weights of every row of the router's logits [rows, experts]
     (ee_moe_route): (ids int32, weights float32), both [rows, top_k]."""
-    dev, dt = _operand(logits, "logits")
+    dev, dt, rows, n, ld = _operand(logits, "logits")
     code = _SCORE_OF.get(score)
     if code is None:
         raise EEError(EE_EINVAL, f"score must be one of {SCORES}")
-    rows, n = logits.shape
-    ld = _rows_of(logits, "logits", (rows, n), logits.dtype, dev)
     k = int(top_k)
     shape = (rows, k if 0 < k <= n else 0)   # (refused below)
     ids = logits.new_empty(shape, dtype=torch.int32)
@@ -328,13 +331,11 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     weights float32 [rows, top_k] as from ``moe_route``; residual and out
     [rows, d] in ``out_dtype`` (x's, or float32).  ``workspace``: a uint8 tensor
     of at least ee_moe_ffn_workspace_bytes, else one is allocated."""
-    dev, dt = _operand(x, "x")
+    dev, dt, rows, d, ldx = _operand(x, "x")
     if not (isinstance(w_down, torch.Tensor) and w_down.dim() == 3 and isinstance(ids, torch.Tensor) and ids.dim() == 2):
         raise EEError(EE_EINVAL, "w_down must be [experts, d, ffn], ids [rows, top_k]")
-    rows, d = x.shape
     E, _, f = w_down.shape
     k = ids.shape[1]
-    ldx = _rows_of(x, "x", (rows, d), x.dtype, dev)
     pointers = (x.data_ptr(), _whole(w_gate_up, "w_gate_up", (E, 2 * f, d), x.dtype, dev),
                 _whole(w_down, "w_down", (E, d, f), x.dtype, dev), _whole(ids, "ids", (rows, k), torch.int32, dev),
                 _whole(weights, "weights", (rows, k), torch.float32, dev))
