@@ -38,10 +38,11 @@ constexpr int EXPERT_CHAIN = 16;
 // have no branch between their steps, where the compiler would wait for more
 // than the step needs (one decoded token through 8 experts, 2048 x 768: 25 us
 // with a test per step and two alternating sets of 8, 13 us).  FOLD: every D steps
-// are a chain of their own, the chains added in order.
+// are a chain of their own, the chains added in order.  EVERY > 1: the steps are two
+// by two of every EVERY-th pair.
 typedef const __attribute__((address_space(1))) unsigned char global_bytes;
 typedef const __attribute__((address_space(1))) u32x4 global_u32x4;
-template <int DT, int NT, int MT, int D, bool FOLD = false>
+template <int DT, int NT, int MT, int D, bool FOLD = false, int EVERY = 1>
 __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], const unsigned char* const (&xptr)[MT], int S,
                                       f32x4 (&acc)[NT][MT]) {
   // (global pointers by type: through the loop the compiler loses that they
@@ -51,12 +52,15 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
   for (int n = 0; n < NT; ++n) wp[n] = (global_bytes*)wptr[n];
 #pragma unroll
   for (int m = 0; m < MT; ++m) xp[m] = (global_bytes*)xptr[m];
+  static_assert(EVERY == 1 || D % 2 == 0, "whole pairs");
+  constexpr int PAIR = 2 * STEP * EVERY;
+  auto at = [](int i) { return EVERY == 1 ? i * STEP : i / 2 * PAIR + i % 2 * STEP; };
   uint4 w[D][NT], x[D][MT];
   auto load = [&](int i) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) w[i][n] = __builtin_bit_cast(uint4, *(global_u32x4*)(wp[n] + i * STEP));
+    for (int n = 0; n < NT; ++n) w[i][n] = __builtin_bit_cast(uint4, *(global_u32x4*)(wp[n] + at(i)));
 #pragma unroll
-    for (int m = 0; m < MT; ++m) x[i][m] = __builtin_bit_cast(uint4, *(global_u32x4*)(xp[m] + i * STEP));
+    for (int m = 0; m < MT; ++m) x[i][m] = __builtin_bit_cast(uint4, *(global_u32x4*)(xp[m] + at(i)));
     __builtin_amdgcn_sched_barrier(0);   // (requests in the order of their use: a wait then leaves the later ones out)
   };
   auto mul = [&](int i) {
@@ -67,9 +71,9 @@ __device__ __forceinline__ void chain(const unsigned char* const (&wptr)[NT], co
   };
   auto next = [&]() {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) wp[n] += D * STEP;
+    for (int n = 0; n < NT; ++n) wp[n] += at(D);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) xp[m] += D * STEP;
+    for (int m = 0; m < MT; ++m) xp[m] += at(D);
   };
   f32x4 tot[NT][MT];
   auto fold = [&](bool first) {
@@ -237,6 +241,9 @@ __device__ __forceinline__ f32x4 linear_bias(const LinearArgs& a, int n) {
 // of few rows spread a long reduction over several waves; the others fold one
 // accumulator into another at a chain's end.  First super-step of chain j.
 constexpr int MAX_CHAINS = 8;
+
+// At most NARROW outputs (a router): CHAINS chains, of the 128-byte stages w, w + 8, ...
+constexpr int NARROW = 512, CHAINS = 8;
 __host__ __device__ __forceinline__ int linear_chains(int S) {
   const int c = S / 64;
   return c < 1 ? 1 : c > MAX_CHAINS ? MAX_CHAINS : c;
@@ -285,6 +292,7 @@ struct TileArgs {
   FfnPlan p;
   int nrt, nft;        // row tiles (at most), feature tiles
   unsigned kmul;       // TM_UP: 2^32 / k rounded up, the factor that divides a pair's number (< 2^24) by k <= 32; 0: k is 1
+  bool narrow;         // TM_LINEAR: the chains of a narrow linear; an even number of super-steps
 };
 
 // Products of BM rows with BN rows of weights, both streamed through LDS in
@@ -322,6 +330,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
   constexpr int LPW = (BM + BN) / RPL / WAVES;   // loads per wave and stage
   constexpr int STAGE = (BM + BN) * PPR;         // pieces of a stage
   constexpr bool KEEP = tile_keeps<DT, MODE, BM, BN, NST, SPS>();
+  constexpr bool NARROWS = MODE == TM_LINEAR && SPS == 2;
   static_assert(SPS == 2 || SPS == 4, "two fragment sets in turn, rows of 8 or 16 pieces");
   static_assert((BM + BN) % (RPL * WAVES) == 0 && BM % RPL == 0, "every wave loads as much");
   static_assert(MODE != TM_UP || FF % 2 == 0, "a wave owns gate and up tiles of the same features");
@@ -423,8 +432,11 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     const unsigned char* src = (inst < BM / RPL ? xb : wb) + (size_t)next * (SPS * STEP);
     __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
   };
+  // (narrow: every eighth stage, then those that follow the first of them)
+  const int step = NARROWS && a.narrow ? CHAINS : 1, starts = NARROWS && a.narrow ? min(CHAINS, stages) : 0;
   auto fetched = [&]() {
-    if (next < stages - 1) ++next;
+    const int on = next + step, start = (next & (step - 1)) + 1;
+    next = on < stages ? on : start < starts ? start : next;
   };
   auto fetch = [&](uint4* buf) {
 #pragma unroll
@@ -441,7 +453,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 
   f32x4 acc[FF][RF], tot[FF][RF];   // the chain, and the sum of the chains before it
   constexpr bool FOLD = MODE == TM_LINEAR || DT == DT_F32;
-  const int chains = MODE == TM_LINEAR ? linear_chains(S) : FOLD ? (S + EXPERT_CHAIN - 1) / EXPERT_CHAIN : 1;
+  const int chains = starts ? starts : MODE == TM_LINEAR ? linear_chains(S) : FOLD ? (S + EXPERT_CHAIN - 1) / EXPERT_CHAIN : 1;
   int ch, ch_end;   // the chain, its last super-step + 1
   const int q = grp ^ swizzle(c);
   const int xo = (wr * RF * 16 + c) * PPR + q, wo = (BM + wf * FF * 16 + c) * PPR + q;
@@ -498,7 +510,9 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     }
     if constexpr (FOLD)
       if ((stages - left) * SPS == ch_end) {   // the stage before ended a chain
-        ch_end = MODE == TM_LINEAR ? chain_start(++ch + 1, S, chains) : ch_end + EXPERT_CHAIN;
+        ++ch;
+        ch_end = starts ? ch_end + SPS * ((stages - ch + CHAINS - 1) / CHAINS)
+                 : MODE == TM_LINEAR ? chain_start(ch + 1, S, chains) : ch_end + EXPERT_CHAIN;
 #pragma unroll
         for (int f = 0; f < FF; ++f)
 #pragma unroll
@@ -520,7 +534,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
 #pragma unroll
       for (int r = 0; r < RF; ++r) tot[f][r] = acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
     ch = 0;
-    ch_end = MODE == TM_LINEAR ? chain_start(1, S, chains) : EXPERT_CHAIN;
+    ch_end = starts ? SPS * ((stages + CHAINS - 1) / CHAINS) : MODE == TM_LINEAR ? chain_start(1, S, chains) : EXPERT_CHAIN;
     left = stages;
     wait_vm<(NST - 1) * LPW>();
     barrier_only();
@@ -714,47 +728,27 @@ static hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
 // Products of few outputs (a router): a workgroup's eight waves each sum the
 // 128-byte stages w, w + 8, ... of the reduction for MT x NT tiles, and the
 // eight sums are added in wave order.
-constexpr int NARROW = 512, CHAINS = 8;
 template <int DT, int MT, int NT>
 __global__ __launch_bounds__(CHAINS * 64) void linear_narrow_kernel(LinearArgs a, int nblk) {
-  constexpr int ESZ = Geo<DT>::ESZ, D = MT * NT > 4 ? 2 : 4;   // stages requested ahead
+  constexpr int ESZ = Geo<DT>::ESZ;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
   const int n0 = blockIdx.x % nblk * (NT * 16), t0 = blockIdx.x / nblk * (MT * 16);
   const int S = a.K / Geo<DT>::KS;
   const unsigned char *wp[NT], *xp[MT];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
-    wp[n] = reinterpret_cast<const unsigned char*>(a.w) + (size_t)min(n0 + n * 16 + c, a.N - 1) * a.ldw * ESZ + grp * 16;
+    wp[n] = reinterpret_cast<const unsigned char*>(a.w) + (size_t)min(n0 + n * 16 + c, a.N - 1) * a.ldw * ESZ + wv * (2 * STEP) + grp * 16;
 #pragma unroll
   for (int m = 0; m < MT; ++m)
-    xp[m] = reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + m * 16 + c, a.T - 1) * a.ldx * ESZ + grp * 16;
+    xp[m] = reinterpret_cast<const unsigned char*>(a.x) + (size_t)min(t0 + m * 16 + c, a.T - 1) * a.ldx * ESZ + wv * (2 * STEP) + grp * 16;
   f32x4 acc[NT][MT];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int j = wv; 2 * j < S; j += CHAINS * D) {
-    uint4 wq[D][2][NT], xq[D][2][MT];
-#pragma unroll
-    for (int i = 0; i < D; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const size_t o = (size_t)min(2 * (j + CHAINS * i) + h, S - 1) * STEP;   // (past the end: unused)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) wq[i][h][n] = *reinterpret_cast<const uint4*>(wp[n] + o);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) xq[i][h][m] = *reinterpret_cast<const uint4*>(xp[m] + o);
-      }
-#pragma unroll
-    for (int i = 0; i < D; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (2 * (j + CHAINS * i) + h < S)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[n][m] = mma<DT>(wq[i][h][n], xq[i][h][m], acc[n][m]);
-  }
+  // (this wave's stages, less the missing half of the last one of all)
+  const int stages = (S + 1) / 2, own = (stages - wv + CHAINS - 1) / CHAINS;
+  chain<DT, NT, MT, (MT * NT > 4 ? 4 : 16), false, CHAINS>(wp, xp, 2 * own - (S % 2 && (stages - 1) % CHAINS == wv), acc);
   __shared__ f32x4 red[CHAINS][NT * MT][64];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -781,14 +775,34 @@ static hipError_t launch_narrow(const LinearArgs& a, hipStream_t st) {
 template <int DT>
 static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   const int64_t rt = (a.T + 15) / 16, nt = (a.N + 15) / 16;
-  if (a.N <= NARROW)
-    // small tiles until they fill the chip, then those that read the rows less often
+  TileArgs t{};
+  t.l = a;
+  const bool f32 = DT == DT_F32;
+  if (a.N <= NARROW) {
+    // The narrow kernel's 16 x 16 tiles while there are few, LDS tiles (in the order of
+    // its chains, for an even number of super-steps) where they take fewer turns of
+    // the chip; us over 4096 columns, alone and per turn of the 256 CUs.  1 row 2048 -> 128
+    // 4.4 us, 32 x 32 tiles 7.2; 1024 rows 2048 -> 256 19 and 8.1; 8192 rows 2048 -> 128
+    // 27, 64 x 64 11.6; 8192 rows 4096 -> 512 178, 128 x 128 35.  fp32 300 rows 8192 -> 300
+    // 59, 32 x 32 55; 1000 rows 2048 -> 256 33 and 18.
+    t.narrow = true;
+    auto cost = [&](int64_t m, int64_t n, double alone, double turn) {
+      return std::max(alone, ceil((double)((a.T + m - 1) / m * ((a.N + n - 1) / n)) / 256.0) * turn);
+    };
+    const double c0 = f32 ? cost(16, 16, 16, 16) : cost(16, 16, 9, 9), c1 = f32 ? cost(32, 32, 28, 20) : cost(32, 32, 11, 5.5),
+                 c2 = f32 ? cost(64, 64, 68, 62) : cost(64, 64, 15, 12), c3 = f32 ? cost(128, 128, 239, 240) : cost(128, 128, 25, 35);
+    const double best = std::min({c0, c1, c2, c3});
+    if (best < c0 && a.K / Geo<DT>::KS % 2 == 0) {
+      if (best == c3) return launch_tile<DT, TM_LINEAR, 128, 128, 2, 4, 4>(t, st);
+      if (best == c2) return launch_tile<DT, TM_LINEAR, 64, 64, 2, f32 ? 4 : 2, 4>(t, st);
+      return launch_tile<DT, TM_LINEAR, 32, 32, 2, 2, 4, 2>(t, st);
+    }
+    // (odd reductions of many rows: larger tiles read the rows less often)
     return rt * nt <= 2048 ? launch_narrow<DT, 1, 1>(a, st) : launch_narrow<DT, 2, 4>(a, st);
+  }
   // 4096 x 4096, weights from HBM: 9.2 us for one row, 9.6 for eight (32 x 32 tiles 11);
   // of 32256 columns 59 us (64 x 64 tiles 51)
   if (a.T <= 16 && nt <= 1024) return launch_rows<DT, 1, 1, 16>(a, st);
-  TileArgs t{};
-  t.l = a;
   // The tile that finishes first: turns of the 256 CUs times what a turn costs
   // (us over 4096 bf16 columns).  33 rows, weights from HBM, tiles of 32 x 32 /
   // 64 x 32 / 64 x 64: 4096 features 11.4 / 13.5 / 20 us, 6144 16.7 / 14.5 / 21,
@@ -807,7 +821,6 @@ static hipError_t linear_t(const LinearArgs& a, hipStream_t st) {
   // more than one on a CU, 64 x 64 67 and 62, 128 x 128 239.  513 x 4096: 32 x 32 169,
   // 64 x 64 188, 128 x 128 243; 2000 x 2000 over 2048 columns 153, 128, 125; 64 x 64
   // with eight waves 4 to 8 % faster than with four.
-  const bool f32 = DT == DT_F32;
   const int64_t c0 = f32 ? cost(32, 32, 19, 19) : cost(32, 32, 9, 9), c1 = f32 ? cost(64, 32, 40, 40) : cost(64, 32, 14, 14),
                 c2 = f32 ? cost(64, 64, 62, 62) : cost(64, 64, 18, 18),
                 c3 = a.T <= 64 ? none : f32 ? cost(128, 128, 239, 240) : cost(128, 128, 27, 36),

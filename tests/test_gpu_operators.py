@@ -107,6 +107,22 @@ def test_linear_reduction(ee, rows, n, k):
     _linear_case(ee, rows, k // 2, n, "f32", "f32", seed=k)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,k,n", [(700, 128, 500), (2100, 1088, 40), (3000, 64, 17), (9000, 576, 130), (8300, 1024, 512),
+                                      (4000, 2080, 300), (5000, 96, 256)])
+def test_narrow_linears_of_many_rows(ee, dtype, rows, k, n):
+    # reductions of fewer stages than chains, of many, and of an odd number of
+    # super-steps; every tile against single rows, and float64
+    k = k if dtype == "bf16" else k // 2
+    got = _linear_case(ee, rows, k, n, dtype, "f32", act="silu", bias=True, residual=True, seed=n)
+    g = _gen(n + 1)
+    x, w = _rand(g, rows, k, dtype=DT[dtype]).cuda(), _rand(g, n, k, dtype=DT[dtype]).cuda()
+    whole = ee.linear(x, w)
+    for lo, m in ((0, 1), (rows // 2, 20), (rows - 300, 300), (0, rows - 1)):
+        assert torch.equal(ee.linear(x[lo:lo + m], w), whole[lo:lo + m]), (lo, m)
+    assert torch.isfinite(got).all()
+
+
 @pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
 @pytest.mark.parametrize("rows,n", [(3, 130), (70, 1030), (300, 770)])
 def test_linear_epilogues(ee, rows, n, act):
