@@ -394,6 +394,10 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
     }
     int ln = lane;
     if constexpr (KEEP) asm volatile("" : "+v"(ln));   // (computed anew for each tile: kept, it would cost registers that the products need)
+    unsigned pair[LPW];   // (requested together)
+    if (MODE == TM_UP && wv * LPW < BM / RPL)
+#pragma unroll
+      for (int i = 0; i < LPW; ++i) pair[i] = a.p.order[et.p0 + min((wv * LPW + i) * RPL + ln / PPR, rows - 1)];
 #pragma unroll
     for (int i = 0; i < LPW; ++i) {
       const int inst = wv * LPW + i;
@@ -401,10 +405,7 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
       const unsigned piece = ((ln % PPR) ^ swizzle(r)) * 16;
       if (inst < BM / RPL) {
         r = min(r, rows - 1);
-        if constexpr (MODE == TM_UP) {
-          const unsigned pair = a.p.order[et.p0 + r];
-          r = a.kmul ? __umulhi(pair, a.kmul) : pair;
-        }
+        if constexpr (MODE == TM_UP) r = a.kmul ? __umulhi(pair[i], a.kmul) : pair[i];
         off[i] = (unsigned)r * ldx + piece;
       } else {
         r -= BM;
@@ -645,11 +646,14 @@ __global__ __launch_bounds__(WR * WF * 64, 2) void tile_kernel(TileArgs a) {
         }
       }
     } else {
+      int to[RF];
+#pragma unroll
+      for (int r = 0; r < RF; ++r) to[r] = a.p.order[cp0 + min((wr * RF + r) * 16 + oc, crows - 1)];
 #pragma unroll
       for (int r = 0; r < RF; ++r) {
         const int row = (wr * RF + r) * 16 + oc;
         if (row >= crows) continue;
-        float* y = a.p.y + (size_t)a.p.order[cp0 + row] * a.p.nc;
+        float* y = a.p.y + (size_t)to[r] * a.p.nc;
 #pragma unroll
         for (int f = 0; f < FF; ++f) {
           const int n = cf0 - a.p.c0 + (wf * FF + f) * 16 + og;
