@@ -1117,7 +1117,18 @@ __global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a,
   constexpr int ESZ = Geo<DT>::ESZ;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, c = lane & 15, grp = lane >> 4;
   const int t = blockIdx.x / nblk, n0 = blockIdx.x % nblk * 16;
-  __shared__ float y[ROUTE_MAX_K][16];
+  __shared__ float y[ROUTE_MAX_K][16], wj[ROUTE_MAX_K];
+  __shared__ bool on[ROUTE_MAX_K];
+  // (what joining needs is requested with the products' operands: one token
+  // 23.0 us, 23.7 with these read slot by slot at the end)
+  float res = 0.f;
+  if (threadIdx.x < a.k) {
+    const size_t p = (size_t)t * a.k + threadIdx.x;
+    const int e = a.ids[p];
+    on[threadIdx.x] = e >= 0 && e < a.E;
+    wj[threadIdx.x] = a.weights[p];
+  }
+  if (a.res && threadIdx.x < 16) res = load_elt<ODT>(a.res, (size_t)t * a.ldr + n0 + threadIdx.x);
   for (int j = wv; j < a.k; j += DOWN_WAVES) {
     const size_t p = (size_t)t * a.k + j;
     const int e = a.ids[p];
@@ -1134,13 +1145,10 @@ __global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a,
   __syncthreads();
   if (threadIdx.x < 16) {
     float o = 0.f;
-    for (int j = 0; j < a.k; ++j) {
-      const size_t p = (size_t)t * a.k + j;
-      const int e = a.ids[p];
-      if (e >= 0 && e < a.E) o = fmaf(a.weights[p], y[j][threadIdx.x], o);
-    }
+    for (int j = 0; j < a.k; ++j)
+      if (on[j]) o = fmaf(wj[j], y[j][threadIdx.x], o);
     const int n = n0 + threadIdx.x;
-    if (a.res) o += load_elt<ODT>(a.res, (size_t)t * a.ldr + n);
+    if (a.res) o += res;
     store_elt<ODT>(a.out, (size_t)t * a.ldo + n, o);
   }
 }
