@@ -445,6 +445,31 @@ def test_ffn_many_tiles_per_workgroup(ee, rows, d, f, E, k):
         assert torch.equal(ee.moe_ffn(x, gu, dn, ids, w), whole)
 
 
+@pytest.mark.parametrize("rows", [300, 1000, 5000])
+@pytest.mark.parametrize("dtype,out,pad", [("bf16", "same", 0), ("bf16", "f32", 1), ("bf16", "same", 3), ("f32", "same", 8), ("f32", "same", 5)])
+def test_ffn_one_expert_per_row(ee, rows, dtype, out, pad):
+    # stored as they are made: strides, residuals, rows without an expert, and the
+    # bits that few rows give
+    x, gu, dn, ids, w = _ffn_inputs(rows, 544, 160, 5, 1, dtype, seed=rows, skew=1.5)
+    ids[::11] = -1
+    ids[5::101] = 5
+    odt = DT[dtype] if out == "same" else torch.float32
+    res = _rand(_gen(pad), rows, 544, dtype=odt)
+    for r in (None, res):
+        got = _ffn_check(ee, x, gu, dn, ids, w, dtype, out=out, residual=r, pad=pad)
+        if r is not None:
+            assert torch.equal(got[ids[:, 0] < 0].cpu(), r[ids[:, 0] < 0])
+        else:
+            assert not got[ids[:, 0] < 0].any()
+        for lo in (0, rows - 33):
+            s = slice(lo, lo + 33)
+            some = ee.moe_ffn(x[s].cuda(), gu.cuda(), dn.cuda(), ids[s].cuda(), w[s].cuda(),
+                              residual=None if r is None else r[s].cuda(), out_dtype=odt)
+            assert torch.equal(some, got[s])
+    whole = res.cuda()
+    assert torch.equal(ee.moe_ffn(x.cuda(), gu.cuda(), dn.cuda(), ids.cuda(), w.cuda(), residual=whole, out=whole), got)
+
+
 @pytest.mark.parametrize("d,f", [(32, 256), (240, 272), (256, 240), (272, 528), (528, 1040), (1040, 512), (2064, 784)])
 def test_ffn_fp32_chains(ee, d, f):
     # reductions that end before, at and behind a chain of 256 columns, by the kernels
