@@ -544,7 +544,8 @@ int32_t ee_moe_route(const ee_moe_route_args* args, void* hip_stream);
  * or 16 (f32), at most 32768, an expert's w_gate_up below 2 GiB; rows * top_k
  * <= 2^24, ldx <= 2^21.  workspace: at least
  * ee_moe_ffn_workspace_bytes (0 for invalid sizes), 256-byte aligned, in use
- * until the call's work is done; calls that may overlap need one each. */
+ * until the call's work is done; calls that may overlap need one each.  The
+ * bytes never fall as rows grow: one sized for the most rows serves fewer. */
 typedef struct {
   const void* x;            /* [rows][ldx] dtype, 16-byte aligned rows        */
   const void* w_gate_up;    /* [n_experts][2 ffn][d_model] dtype: gate, up    */

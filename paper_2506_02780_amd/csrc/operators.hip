@@ -1279,10 +1279,17 @@ int ffn_columns(int64_t P, int d) {
   return (int)std::min<int64_t>(d, std::max<int64_t>(256, n));
 }
 
+// Bytes for the down products that are held: what any call with at most P pairs needs.
+// (ffn_columns falls in steps, so that fewer pairs may hold more than P times its columns.
+// A call in parts and an engine's smaller blocks lay out their own, fewer pairs in a
+// workspace sized for the most.)
+size_t ffn_held(size_t P, int d) { return std::min(P * d, std::max(Y_BYTES / 4, P * 256)) * 4; }
+
+// Never falls as T grows: every part does not.
 size_t ffn_workspace(int T, int E, int k, int d, int F, int dt) {
   const size_t P = (size_t)T * k;
   return align256(4) + align256(ffn_tiles(P, E, MIN_BM) * sizeof(ExpertTile)) + align256(P * 4) +
-         align256(P * F * esz_of(dt)) + align256(P * (P ? ffn_columns(P, d) : 0) * 4);
+         align256(P * F * esz_of(dt)) + align256(ffn_held(P, d));
 }
 
 static FfnPlan ffn_plan(const FfnArgs& a) {

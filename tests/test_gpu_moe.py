@@ -187,3 +187,29 @@ def test_refused_on_sparse_models(ee):
     assert times["gateup"][1] == 2 and times["down"][1] == 0
     assert eng.time_gemm("qkv", 4) > 0
     eng.close()
+
+
+def test_blocks_of_fewer_rows_stay_inside_the_workspace(ee, monkeypatch):
+    """Blocks on both sides of a step of the down products' columns: 64 sequences of
+    65 rows hold 1792 columns, 63 of them 2048, of more bytes.  Bytes behind the
+    workspace stay as they were, and the rows are those of single sequences."""
+    shape = _bf16(n_layers=1, d_model=2048, ffn=64, vocab=256, n_experts=16, top_k=8)
+    size, guard = ee.ee_moe_workspace_bytes, 64 << 20
+    monkeypatch.setattr(ee, "ee_moe_workspace_bytes", lambda *a: size(*a) + guard)
+    eng = ee.Engine(shape, gen_weights(shape, seed=51, std=0.05), max_ctx=128, max_seqs=64, k_max=64)
+    behind = eng.workspace[-guard:]
+    behind.fill_(165)
+    prompts = [zipf_tokens(shape.vocab, 3 + s % 5, seed=60 + s) for s in range(64)]
+    first = [eng.prefill(s, p) for s, p in enumerate(prompts)]
+    drafts = [zipf_tokens(shape.vocab, 64, seed=200 + s) for s in range(64)]
+    for n in (64, 63, 62, 33):
+        got = eng.verify_batch(list(range(n)), drafts[:n])
+        assert (behind == 165).all(), n
+        rows = eng.logits().reshape(n, 65, -1)
+        for s in range(n):
+            eng.rollback(s, len(prompts[s]), first[s])
+        for s in (0, n // 2, n - 1):
+            a, nxt, _ = eng.verify(s, drafts[s])
+            assert (a, nxt) == got[s][:2] and np.array_equal(eng.logits(), rows[s])
+            eng.rollback(s, len(prompts[s]), first[s])
+    eng.close()

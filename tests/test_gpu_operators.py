@@ -713,3 +713,43 @@ def test_empty_calls(ee):
                    torch.randn(4, 64, 32, device="cuda"), torch.empty(0, 2, dtype=torch.int32, device="cuda"),
                    torch.empty(0, 2, device="cuda"))
     assert y.shape == (0, 64)
+
+
+def _steps_case(rows, d, E, k, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, d, generator=g, device="cuda").to(torch.bfloat16)
+    gu = (torch.randn(E, 64, d, generator=g, device="cuda") * d ** -0.5).to(torch.bfloat16)
+    dn = (torch.randn(E, d, 32, generator=g, device="cuda") * 0.2).to(torch.bfloat16)
+    ids = torch.randint(-1, E, (rows, k), generator=g, device="cuda", dtype=torch.int32)
+    return x, gu, dn, ids, torch.rand(rows, k, generator=g, device="cuda")
+
+
+def test_a_workspace_of_the_callers_around_a_step(ee):
+    """Fewer rows that hold more columns of down products, in a workspace for the
+    most rows; the bytes behind it stay."""
+    d, E, k = 2048, 16, 8
+    most = ee.ee_moe_ffn_workspace_bytes(4160, E, k, d, 32, ee.EE_BF16)
+    ws = torch.full((most + (64 << 20),), 165, dtype=torch.uint8, device="cuda")
+    a = _steps_case(4160, d, E, k, 31)
+    whole = ee.moe_ffn(*a)
+    for rows in (4160, 4097, 4096, 4095, 3641, 3640, 33):
+        x, gu, dn, ids, w = a
+        assert torch.equal(ee.moe_ffn(x[:rows], gu, dn, ids[:rows], w[:rows], workspace=ws[:most]), whole[:rows]), rows
+        assert (ws[most:] == 165).all(), rows
+
+
+def test_a_call_in_parts_stays_inside_its_workspace(ee):
+    """1030 rows, 2^21 elements apart, run as 1023 and 7: the first part holds 2048
+    columns of down products where the whole call would hold 1792."""
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    rows, d, E, k, ld = 1030, 8192, 32, 32, 1 << 21
+    x, gu, dn, ids, w = _steps_case(rows, d, E, k, 32)
+    apart = torch.empty(rows * ld, dtype=x.dtype, device="cuda").as_strided((rows, d), (ld, 1))
+    apart.copy_(x)
+    most = ee.ee_moe_ffn_workspace_bytes(rows, E, k, d, 32, ee.EE_BF16)
+    ws = torch.full((most + (64 << 20),), 165, dtype=torch.uint8, device="cuda")
+    want = ee.moe_ffn(x, gu, dn, ids, w)
+    assert torch.equal(ee.moe_ffn(apart, gu, dn, ids, w, workspace=ws[:most]), want)
+    assert (ws[most:] == 165).all()

@@ -143,3 +143,23 @@ def test_outputs_that_are_inputs_are_refused(ee):
     for kw in (dict(out=P), dict(out=5 * P), dict(out=8 * P), dict(out=6 * P, ldr=72)):
         assert _ffn(ee, **{**apart, **kw}) == ee.EE_EINVAL, kw
         assert b"must not be an input" in ee.ee_last_error(None)
+
+
+def _rows_around_steps(k, most):
+    # (the columns that are held at once fall in steps of 256 as the pairs grow past 2^26 / 256 n)
+    steps = {(1 << 26) // (256 * n) // k for n in range(1, 130)}
+    return sorted({r for s in steps for r in (s - 1, s, s + 1, s + 2) if 0 < r <= most} | {1, 2, 17, 100, 512, 4095, 4160, most})
+
+
+@pytest.mark.parametrize("E,k,d,f,dtype", [(128, 8, 2048, 768, "bf16"), (8, 2, 256, 352, "f32"), (256, 8, 7168, 2048, "bf16"),
+                                           (32, 32, 8192, 32, "bf16"), (8, 2, 32768, 32, "bf16"), (8, 2, 32768, 16, "f32"),
+                                           (4, 3, 1056, 96, "bf16"), (6, 1, 4096, 64, "bf16")])
+def test_a_workspace_serves_fewer_rows(ee, E, k, d, f, dtype):
+    """The size never falls as the rows grow: a caller may size one workspace for its
+    largest call, an engine does, and a call in parts uses the whole call's."""
+    dt = ee.EE_BF16 if dtype == "bf16" else ee.EE_F32
+    last, at = 0, 0
+    for rows in _rows_around_steps(k, min((1 << 24) // k, (2 ** 31 - 1) * 16 // (k * max(d, f)))):
+        n = ee.ee_moe_ffn_workspace_bytes(rows, E, k, d, f, dt)
+        assert n >= max(last, 1), f"{rows} rows need {n} bytes, {at} rows {last}"
+        last, at = n, rows
