@@ -488,9 +488,9 @@ int32_t ee_time_stream_read(ee_ctx* ctx, const void* dev_buf, size_t bytes, int3
  * is ee_last_error(NULL)); zero rows are EE_OK.  Strides (ld*) count elements
  * between rows.  Sums are fp32 (the routing float64) with one rounding at the
  * end, and a row's result does not depend on the other rows of a call.
- * Outputs must not overlap inputs, except that `y` / `out` may be exactly
- * `residual` (same pointer, stride and type); the same address otherwise is
- * EE_EINVAL. */
+ * Outputs and the workspace must not overlap inputs or each other, except that
+ * `y` / `out` may be exactly `residual` (same pointer, stride and type); the same
+ * address otherwise is EE_EINVAL. */
 enum { EE_ACT_NONE = 0, EE_ACT_SILU = 1, EE_ACT_GELU = 2 /* erf */, EE_ACT_GELU_TANH = 3, EE_ACT_RELU = 4 };
 enum { EE_SCORE_SOFTMAX = 0, EE_SCORE_SIGMOID = 1 };
 

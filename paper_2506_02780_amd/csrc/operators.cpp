@@ -84,6 +84,9 @@ int32_t ee_moe_route(const ee_moe_route_args* p, void* stream) {
   if (!q.logits || !q.ids || !q.weights) return bad("logits, ids and weights must be non-NULL");
   if (!out_ok(q.logits, q.ld, q.n_experts, q.dtype)) return bad("logits must be aligned to their type with a row stride of at least n_experts");
   if (!aligned(q.ids, 4) || !aligned(q.weights, 4) || (q.bias && !aligned(q.bias, 4))) return bad("ids, weights and bias must be aligned to their type");
+  for (const void* y : {(const void*)q.ids, (const void*)q.weights})
+    if (y == q.logits || y == q.bias) return bad("ids and weights must not be an input");
+  if ((const void*)q.ids == q.weights) return bad("ids and weights must not be an input or each other");
   ee::RouteArgs a{};
   a.logits = q.logits; a.bias = q.bias; a.ids = q.ids; a.weights = q.weights; a.ld = q.ld;
   a.T = q.rows; a.E = q.n_experts; a.k = q.top_k; a.dt = dt_of(q.dtype);
@@ -129,8 +132,12 @@ int32_t ee_moe_ffn(const ee_moe_ffn_args* p, void* stream) {
   if (!aligned(q.workspace, 256)) return bad("workspace must be 256-byte aligned");
   if (q.workspace_bytes < ee::ffn_workspace(q.rows, q.n_experts, q.top_k, q.d_model, q.ffn, dt_of(q.dtype)))
     return op_fail(EE_ECAPACITY, "workspace smaller than ee_moe_ffn_workspace_bytes");
-  if (q.out == q.x || q.out == q.weights || q.out == q.workspace || (q.out == q.residual && q.ldr != q.ldo))
-    return bad("out must not be an input or the workspace, except the residual with its stride");
+  for (const void* in : {q.x, q.w_gate_up, q.w_down, (const void*)q.ids, (const void*)q.weights}) {
+    if (q.out == in) return bad("out must not be an input, except the residual with its stride");
+    if (q.workspace == in) return bad("the workspace must not be an input");
+  }
+  if (q.out == q.residual && q.ldr != q.ldo) return bad("out must not be an input, except the residual with its stride");
+  if (q.workspace == q.out || q.workspace == q.residual) return bad("the workspace must not be an input or out");
   ee::FfnArgs a{};
   a.x = q.x; a.wgu = q.w_gate_up; a.wd = q.w_down; a.ids = q.ids; a.weights = q.weights; a.res = q.residual; a.out = q.out;
   a.ldx = q.ldx; a.ldr = q.ldr; a.ldo = q.ldo;

@@ -163,3 +163,24 @@ def test_a_workspace_serves_fewer_rows(ee, E, k, d, f, dtype):
         n = ee.ee_moe_ffn_workspace_bytes(rows, E, k, d, f, dt)
         assert n >= max(last, 1), f"{rows} rows need {n} bytes, {at} rows {last}"
         last, at = n, rows
+
+
+ROUTE_APART = dict(rows=1, logits=P, bias=2 * P, ids=3 * P, weights=4 * P)
+FFN_APART = dict(rows=1, x=P, w_gate_up=2 * P, w_down=3 * P, ids=4 * P, weights=5 * P, residual=6 * P, out=7 * P, workspace=8 * P)
+
+
+@pytest.mark.parametrize("kw", [dict(ids=P), dict(ids=2 * P), dict(weights=P), dict(weights=2 * P), dict(ids=4 * P)])
+def test_route_outputs_at_an_inputs_or_the_others_address(ee, kw):
+    assert _route(ee, **{**ROUTE_APART, **kw}) == ee.EE_EINVAL
+    assert b"must not be an input" in ee.ee_last_error(None)
+
+
+@pytest.mark.parametrize("name", ["out", "workspace"])
+@pytest.mark.parametrize("at", range(1, 8))
+def test_ffn_outputs_at_an_inputs_address(ee, name, at):
+    if name == "out" and at >= 6:   # (the residual's address is allowed with its stride; 7 is its own)
+        at, kw = 6, dict(ldr=72)
+    else:
+        kw = {}
+    assert _ffn(ee, **{**FFN_APART, name: at * P, **kw}) == ee.EE_EINVAL
+    assert b"must not be an input" in ee.ee_last_error(None)
