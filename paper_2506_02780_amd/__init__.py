@@ -222,8 +222,9 @@ def _rows_of(t, what: str, shape, dtype, dev) -> int:
             and not (t.requires_grad and torch.is_grad_enabled())):
         rs, cs = t.stride()
         if cs == 1 or shape[1] <= 1:
-            # (a single row may carry any stride)
-            return rs if shape[0] > 1 or rs > shape[1] else shape[1]
+            # (a single row may carry any stride: the last position of a batch of one, a view
+            # whose stride the library might refuse)
+            return rs if shape[0] > 1 else shape[1]
     _refuse(what, shape, dtype, dev, t)
 
 
@@ -248,7 +249,7 @@ def _operand(x, what: str):
     ld, cs = x.stride()
     if (cs != 1 and cols > 1) or (x.requires_grad and torch.is_grad_enabled()):
         _refuse(what, (rows, cols), x.dtype, dev, x)
-    return dev, dt, rows, cols, ld if rows > 1 or ld > cols else cols
+    return dev, dt, rows, cols, ld if rows > 1 else cols
 
 
 def _out_type(out_dtype, out, x):

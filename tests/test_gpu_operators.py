@@ -753,3 +753,26 @@ def test_a_call_in_parts_stays_inside_its_workspace(ee):
     want = ee.moe_ffn(x, gu, dn, ids, w)
     assert torch.equal(ee.moe_ffn(apart, gu, dn, ids, w, workspace=ws[:most]), want)
     assert (ws[most:] == 165).all()
+
+
+def test_one_row_of_any_stride(ee):
+    """The last position of one sequence: its row's stride is past what the library
+    takes, or no multiple of 16 bytes."""
+    g = _gen(33)
+    d, f, E, k = 256, 64, 8, 2
+    w, gu, dn = _rand(g, 96, d).cuda(), _rand(g, E, 2 * f, d, std=0.1).cuda(), _rand(g, E, d, f, std=0.1).cuda()
+    for stride in ((1 << 21) + 4, 1001):
+        h = torch.zeros(stride + d, device="cuda").as_strided((1, d), (stride, 1))
+        h.copy_(_rand(g, 1, d))
+        x, r = h.clone(), _rand(g, 1, 96).cuda()
+        assert torch.equal(ee.linear(h, w), ee.linear(x, w))
+        assert torch.equal(ee.linear(x, h), ee.linear(x, x))
+        ids, wt = ee.moe_route(h[:, :32], k)
+        assert torch.equal(ids, ee.moe_route(x[:, :32].contiguous(), k)[0])
+        ids = ids % E
+        want = ee.moe_ffn(x, gu, dn, ids, wt, residual=x)
+        assert torch.equal(ee.moe_ffn(h, gu, dn, ids, wt, residual=h), want)
+        want = ee.linear(x, w, residual=r)
+        y = torch.zeros(stride + 96, device="cuda").as_strided((1, 96), (stride, 1))
+        y.copy_(r)
+        assert ee.linear(h, w, residual=y, out=y) is y and torch.equal(y, want)

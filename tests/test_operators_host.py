@@ -184,3 +184,10 @@ def test_ffn_outputs_at_an_inputs_address(ee, name, at):
         kw = {}
     assert _ffn(ee, **{**FFN_APART, name: at * P, **kw}) == ee.EE_EINVAL
     assert b"must not be an input" in ee.ee_last_error(None)
+
+
+def test_a_single_row_may_carry_any_stride(ee):
+    import torch
+    for rows, stride, ld in ((1, 70001, 64), (1, 1 << 22, 64), (1, 3, 64), (2, 96, 96), (2, 70001, 70001)):
+        t = torch.empty(2 * max(stride, 64) + 64).as_strided((rows, 64), (stride, 1))
+        assert ee._rows_of(t, "w", (rows, 64), torch.float32, -1) == ld
