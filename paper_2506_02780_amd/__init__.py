@@ -17,6 +17,7 @@ import struct
 
 import numpy as np
 import torch  # loaded first so the HIP runtime it ships is the one libee.so binds to
+from torch.autograd import forward_ad as _forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libee.so")
@@ -198,8 +199,8 @@ def make_moe_config(shape) -> EEMoeConfig:
 #
 # Device tensors in, device tensors out, on the tensors' device and its current
 # stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given.
-# They have no backward pass: operands that require a gradient are refused while
-# gradients are recorded.
+# They have no backward pass and no forward-mode derivative: operands that require a
+# gradient are refused while gradients are recorded, and operands that carry a tangent.
 
 _TYPES = {torch.float32: EE_F32, torch.bfloat16: EE_BF16}
 _ACT_OF = {a: i for i, a in enumerate(ACTIVATIONS)}
@@ -214,6 +215,17 @@ def _refuse(what: str, shape, dtype, dev, t):
         raise EEError(EE_EINVAL, f"{what} requires a gradient, which these operators do not have (use torch.no_grad)")
     got = f"{list(t.shape)} {t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
     raise EEError(EE_EINVAL, f"{what} must be {list(shape)} {dtype} on cuda:{dev} (rows of unit column stride), not {got}")
+
+
+def _refuse_tangents(**operands):
+    for what, t in operands.items():
+        if isinstance(t, torch.Tensor) and _forward_ad.unpack_dual(t).tangent is not None:
+            raise EEError(EE_EINVAL, f"{what} carries a tangent (forward_ad), which these operators do not propagate")
+
+
+def _tangents() -> bool:
+    """Whether operands may carry tangents (inside forward_ad.dual_level)."""
+    return getattr(_forward_ad, "_current_level", 0) >= 0
 
 
 def _rows_of(t, what: str, shape, dtype, dev) -> int:
@@ -284,6 +296,8 @@ def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtyp
     in float32 or bfloat16, bias [out] float32, residual [rows, out] in the
     output's dtype (``out_dtype``: x's, or float32).  ``out`` may be the residual."""
     dev, dt, rows, cols, ldx = _operand(x, "x")
+    if _tangents():
+        _refuse_tangents(x=x, w=w, bias=bias, residual=residual, out=out)
     code = _ACT_OF.get(act)
     if code is None:
         raise EEError(EE_EINVAL, f"act must be one of {ACTIVATIONS}")
@@ -309,6 +323,8 @@ def moe_route(logits, top_k: int, score: str = "softmax", bias=None, renormalize
     """Experts and weights of every row of the router's logits [rows, experts]
     (ee_moe_route): (ids int32, weights float32), both [rows, top_k]."""
     dev, dt, rows, n, ld = _operand(logits, "logits")
+    if _tangents():
+        _refuse_tangents(logits=logits, bias=bias)
     code = _SCORE_OF.get(score)
     if code is None:
         raise EEError(EE_EINVAL, f"score must be one of {SCORES}")
@@ -333,6 +349,8 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
     [rows, d] in ``out_dtype`` (x's, or float32).  ``workspace``: a uint8 tensor
     of at least ee_moe_ffn_workspace_bytes, else one is allocated."""
     dev, dt, rows, d, ldx = _operand(x, "x")
+    if _tangents():
+        _refuse_tangents(x=x, w_gate_up=w_gate_up, w_down=w_down, weights=weights, residual=residual, out=out)
     if not (isinstance(w_down, torch.Tensor) and w_down.dim() == 3 and isinstance(ids, torch.Tensor) and ids.dim() == 2):
         raise EEError(EE_EINVAL, "w_down must be [experts, d, ffn], ids [rows, top_k]")
     E, _, f = w_down.shape

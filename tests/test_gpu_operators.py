@@ -776,3 +776,29 @@ def test_one_row_of_any_stride(ee):
         y = torch.zeros(stride + 96, device="cuda").as_strided((1, 96), (stride, 1))
         y.copy_(r)
         assert ee.linear(h, w, residual=y, out=y) is y and torch.equal(y, want)
+
+
+def test_forward_mode_tangents_are_refused(ee):
+    """A tangent would be lost without a word."""
+    from torch.autograd import forward_ad
+    g = _gen(34)
+    x, w, b, r = _rand(g, 4, 64).cuda(), _rand(g, 64, 64).cuda(), _rand(g, 64).cuda(), _rand(g, 4, 64).cuda()
+    gu, dn = _rand(g, 3, 64, 64).cuda(), _rand(g, 3, 64, 32).cuda()
+    ids, wt = torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.rand(4, 2, device="cuda")
+    want = ee.linear(x, w, bias=b, residual=r), ee.moe_route(x, 2), ee.moe_ffn(x, gu, dn, ids, wt, residual=r)
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))
+        for i, call in enumerate((lambda: ee.linear(dual(x), w), lambda: ee.linear(x, dual(w)), lambda: ee.linear(x, w, bias=dual(b)),
+                                  lambda: ee.linear(x, w, residual=dual(r)), lambda: ee.linear(x, w, out=dual(r)),
+                                  lambda: ee.moe_route(dual(x), 2), lambda: ee.moe_route(x, 2, bias=dual(b)),
+                                  lambda: ee.moe_ffn(dual(x), gu, dn, ids, wt), lambda: ee.moe_ffn(x, dual(gu), dn, ids, wt),
+                                  lambda: ee.moe_ffn(x, gu, dual(dn), ids, wt), lambda: ee.moe_ffn(x, gu, dn, ids, dual(wt)),
+                                  lambda: ee.moe_ffn(x, gu, dn, ids, wt, residual=dual(r)),
+                                  lambda: ee.moe_ffn(x, gu, dn, ids, wt, out=dual(r)))):
+            with pytest.raises(ee.EEError) as e:
+                call()
+            assert e.value.code == ee.EE_EINVAL and "tangent" in str(e.value), i
+        # operands without one are served
+        assert torch.equal(ee.linear(x, w, bias=b, residual=r), want[0])
+        assert torch.equal(ee.moe_route(x, 2)[0], want[1][0])
+        assert torch.equal(ee.moe_ffn(x, gu, dn, ids, wt, residual=r), want[2])

@@ -191,3 +191,14 @@ def test_a_single_row_may_carry_any_stride(ee):
     for rows, stride, ld in ((1, 70001, 64), (1, 1 << 22, 64), (1, 3, 64), (2, 96, 96), (2, 70001, 70001)):
         t = torch.empty(2 * max(stride, 64) + 64).as_strided((rows, 64), (stride, 1))
         assert ee._rows_of(t, "w", (rows, 64), torch.float32, -1) == ld
+
+
+def test_tangents_are_refused(ee):
+    import torch
+    from torch.autograd import forward_ad
+    x = torch.zeros(2, 64)
+    with forward_ad.dual_level():
+        ee._refuse_tangents(x=x, bias=None, out=5)
+        with pytest.raises(ee.EEError) as e:
+            ee._refuse_tangents(x=x, w=forward_ad.make_dual(x, torch.ones(2, 64)))
+        assert e.value.code == ee.EE_EINVAL and "w carries a tangent" in str(e.value)
