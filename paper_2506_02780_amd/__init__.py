@@ -198,7 +198,8 @@ def make_moe_config(shape) -> EEMoeConfig:
 # -- stand-alone operators ---------------------------------------------------
 #
 # Device tensors in, device tensors out, on the tensors' device and its current
-# stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given.
+# stream; nothing synchronizes.  Outputs are allocated with PyTorch unless given; one
+# that is given counts as written in place (its version grows).
 # They have no backward pass and no forward-mode derivative: operands that require a
 # gradient are refused while gradients are recorded, and operands that carry a tangent.
 
@@ -273,6 +274,7 @@ def _out_type(out_dtype, out, x):
 
 
 _current_device = torch.cuda.current_device
+_written = torch.autograd.graph.increment_version
 
 
 def _operator(op, dev: int, *args):
@@ -307,14 +309,17 @@ def linear(x, w, bias=None, act: str = "none", residual=None, out=None, out_dtyp
     ldw = _rows_of(w, "w", (n, cols), x.dtype, dev)
     odt = _out_type(out_dtype, out, x)
     shape = (rows, n)
-    if out is None:
-        out, ldy = x.new_empty(shape, dtype=odt), n
-    else:
+    given = out is not None
+    if given:
         ldy = _rows_of(out, "out", shape, odt, dev)
+    else:
+        out, ldy = x.new_empty(shape, dtype=odt), n
     ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
     _operator(_OP_LINEAR, dev, x.data_ptr(), w.data_ptr(), 0 if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
               0 if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr, ldy, rows, cols, n, dt,
               _TYPES[odt], code)
+    if given:
+        _written(out)
     return out
 
 
@@ -360,10 +365,11 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
                 _whole(weights, "weights", (rows, k), torch.float32, dev))
     odt = _out_type(out_dtype, out, x)
     shape = (rows, d)
-    if out is None:
-        out, ldo = x.new_empty(shape, dtype=odt), d
-    else:
+    given = out is not None
+    if given:
         ldo = _rows_of(out, "out", shape, odt, dev)
+    else:
+        out, ldo = x.new_empty(shape, dtype=odt), d
     ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
     if workspace is None:
         workspace = x.new_empty(_ffn_workspace(rows, E, k, d, f, dt), dtype=torch.uint8)
@@ -372,6 +378,8 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
         raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")
     _operator(_OP_FFN, dev, *pointers, 0 if residual is None else residual.data_ptr(), out.data_ptr(), workspace.data_ptr(),
               workspace.numel(), ldx, ldr, ldo, rows, E, k, d, f, dt, _TYPES[odt])
+    if given:
+        _written(out)
     return out
 
 

@@ -802,3 +802,16 @@ def test_forward_mode_tangents_are_refused(ee):
         assert torch.equal(ee.linear(x, w, bias=b, residual=r), want[0])
         assert torch.equal(ee.moe_route(x, 2)[0], want[1][0])
         assert torch.equal(ee.moe_ffn(x, gu, dn, ids, wt, residual=r), want[2])
+
+
+def test_autograd_notices_an_output_that_it_saved(ee):
+    g = _gen(35)
+    x, w = _rand(g, 4, 64).cuda(), _rand(g, 64, 64).cuda()
+    for call in (lambda h: ee.linear(x, w, residual=h, out=h),
+                 lambda h: ee.moe_ffn(x, w.expand(3, 64, 64).contiguous(), w[None, :, :32].expand(3, 64, 32).contiguous(),
+                                      torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.ones(4, 2, device="cuda"), out=h)):
+        p, h = torch.ones(4, 64, device="cuda", requires_grad=True), torch.ones(4, 64, device="cuda")
+        loss = (p * h).sum()
+        assert call(h) is h
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()

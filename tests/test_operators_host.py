@@ -202,3 +202,25 @@ def test_tangents_are_refused(ee):
         with pytest.raises(ee.EEError) as e:
             ee._refuse_tangents(x=x, w=forward_ad.make_dual(x, torch.ones(2, 64)))
         assert e.value.code == ee.EE_EINVAL and "w carries a tangent" in str(e.value)
+
+
+def test_an_output_given_counts_as_written(ee, monkeypatch):
+    """A tensor that autograd saved must not be overwritten unnoticed: out's version
+    grows.  (No GPU: the calls themselves are left out.)"""
+    import torch
+    monkeypatch.setattr(ee, "_operand", lambda t, what: (-1, ee.EE_F32, *t.shape, t.stride(0)))
+    monkeypatch.setattr(ee, "_operator", lambda *a: None)
+    x, w, y = torch.zeros(4, 64), torch.zeros(64, 64), torch.zeros(8, 64)
+    ids, wt = torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    for n, call in ((1, lambda: ee.linear(x, w, out=y[:4])),
+                    (2, lambda: ee.moe_ffn(x, torch.zeros(3, 64, 64), torch.zeros(3, 64, 32), ids, wt, out=y[4:]))):
+        call()
+        assert y._version == n
+    p = torch.ones(8, 64, requires_grad=True)
+    loss = (p * y).sum()
+    with torch.no_grad():
+        ee.linear(x, w, residual=y[:4], out=y[:4])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():   # (such tensors have no version)
+        ee.linear(x, w, out=torch.zeros(4, 64))
