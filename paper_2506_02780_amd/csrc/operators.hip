@@ -282,7 +282,7 @@ struct FfnPlan {
   ExpertTile* tile;    // [ntile]
   int* order;          // [pairs] pairs (row * k + slot) sorted by expert; skipped ones are not in it
   void* z;             // [pairs][F] dt, rows in sorted order
-  float* y;            // [pairs][nc]: columns c0 .. c0 + nc - 1 of the down products, rows by pair
+  float* y;            // [pairs][nc]: columns c0 .. c0 + nc - 1 of the down products, rows by pair (k > 1)
   int c0, nc;
 };
 
@@ -1282,14 +1282,14 @@ int ffn_columns(int64_t P, int d) {
 // Bytes for the down products that are held: what any call with at most P pairs needs.
 // (ffn_columns falls in steps, so that fewer pairs may hold more than P times its columns.
 // A call in parts and an engine's smaller blocks lay out their own, fewer pairs in a
-// workspace sized for the most.)
-size_t ffn_held(size_t P, int d) { return std::min(P * d, std::max(Y_BYTES / 4, P * 256)) * 4; }
+// workspace sized for the most.)  None with one expert per row: those are stored as they are made.
+size_t ffn_held(size_t P, int k, int d) { return k == 1 ? 0 : std::min(P * d, std::max(Y_BYTES / 4, P * 256)) * 4; }
 
 // Never falls as T grows: every part does not.
 size_t ffn_workspace(int T, int E, int k, int d, int F, int dt) {
   const size_t P = (size_t)T * k;
   return align256(4) + align256(ffn_tiles(P, E, MIN_BM) * sizeof(ExpertTile)) + align256(P * 4) +
-         align256(P * F * esz_of(dt)) + align256(ffn_held(P, d));
+         align256(P * F * esz_of(dt)) + align256(ffn_held(P, k, d));
 }
 
 static FfnPlan ffn_plan(const FfnArgs& a) {

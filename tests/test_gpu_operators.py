@@ -815,3 +815,12 @@ def test_autograd_notices_an_output_that_it_saved(ee):
         assert call(h) is h
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             loss.backward()
+
+
+@pytest.mark.parametrize("rows", [5, 300, 3000])
+def test_one_expert_per_row_stays_inside_its_workspace(ee, rows):
+    x, gu, dn, ids, w = [t.cuda() for t in _ffn_inputs(rows, 544, 96, 5, 1, "bf16", seed=rows)]
+    most = ee.ee_moe_ffn_workspace_bytes(rows, 5, 1, 544, 96, ee.EE_BF16)
+    ws = torch.full((most + (16 << 20),), 165, dtype=torch.uint8, device="cuda")
+    assert torch.equal(ee.moe_ffn(x, gu, dn, ids, w, workspace=ws[:most]), ee.moe_ffn(x, gu, dn, ids, w))
+    assert (ws[most:] == 165).all()

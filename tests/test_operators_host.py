@@ -224,3 +224,9 @@ def test_an_output_given_counts_as_written(ee, monkeypatch):
         loss.backward()
     with torch.inference_mode():   # (such tensors have no version)
         ee.linear(x, w, out=torch.zeros(4, 64))
+
+
+def test_one_expert_per_row_holds_no_down_products(ee):
+    # (they are stored as they are made: what is left is z, the order and the tiles)
+    rows, f = 8192, 96
+    assert ee.ee_moe_ffn_workspace_bytes(rows, 2, 1, 3776, f, ee.EE_BF16) < rows * (2 * f + 4) + (16 << 10)
