@@ -1176,13 +1176,16 @@ __global__ __launch_bounds__(DOWN_WAVES * 64, 2) void ffn_down_kernel(FfnArgs a,
 // Workgroup b places the pairs of chunk b.  It needs the counts of all pairs and
 // of those before its chunk, and counts them itself (every workgroup reads all
 // ids, from L2): one launch and no wait between workgroups.  (65536 pairs: 61 us
-// in a single workgroup.)  The order of the pairs within an expert may differ
+// in a single workgroup.)  At most PLAN_BLOCKS chunks, so that the time grows with
+// the pairs and not with their square (2^22 pairs, 64 experts of 32 over 32: the call 4.5 ms
+// with chunks of 2048, 2.2 so; all pairs of one expert 29.8 and 10.4).  The order of the pairs within an expert may differ
 // from run to run; every row's arithmetic is its own, so the results do not.
-constexpr int PLAN_THREADS = 1024, PLAN_CHUNK = 2048;
+constexpr int PLAN_THREADS = 1024, PLAN_CHUNK = 2048, PLAN_BLOCKS = 256;
 static_assert(PLAN_THREADS >= ROUTE_MAX_E, "a thread per expert");
-__global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __restrict__ ids, int P, int E, int BM, FfnPlan p) {
+int plan_chunk(int64_t P) { return (int)std::max<int64_t>(PLAN_CHUNK, (P + PLAN_BLOCKS - 1) / PLAN_BLOCKS); }
+__global__ __launch_bounds__(PLAN_THREADS) void ffn_plan_kernel(const int* __restrict__ ids, int P, int chunk, int E, int BM, FfnPlan p) {
   __shared__ int cnt[ROUTE_MAX_E], first[ROUTE_MAX_E], tiles[ROUTE_MAX_E];
-  const int t = threadIdx.x, lo = blockIdx.x * PLAN_CHUNK, hi = min(P, lo + PLAN_CHUNK);
+  const int t = threadIdx.x, lo = blockIdx.x * chunk, hi = min(P, lo + chunk);
   if (t < E) cnt[t] = 0;
   __syncthreads();
   auto count = [&](int from, int to) {
@@ -1382,7 +1385,8 @@ static hipError_t ffn_t(const FfnArgs& a, hipStream_t st) {
   t.f = a;
   t.p = pl;
   t.nrt = (int)ffn_tiles(P, a.E, BM);
-  hipLaunchKernelGGL(ffn_plan_kernel, dim3((unsigned)((P + PLAN_CHUNK - 1) / PLAN_CHUNK)), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, a.E, BM, pl);
+  const int chunk = plan_chunk(P);
+  hipLaunchKernelGGL(ffn_plan_kernel, dim3((unsigned)((P + chunk - 1) / chunk)), dim3(PLAN_THREADS), 0, st, a.ids, (int)P, chunk, a.E, BM, pl);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (BM == 32) return ffn_tiles_t<DT, ODT, 32, 64, 2, 2, 4>(t, st);
   if (BM == 64) return ffn_tiles_t<DT, ODT, 64, 256, 1, 8, 3>(t, st);

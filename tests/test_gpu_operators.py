@@ -824,3 +824,21 @@ def test_one_expert_per_row_stays_inside_its_workspace(ee, rows):
     ws = torch.full((most + (16 << 20),), 165, dtype=torch.uint8, device="cuda")
     assert torch.equal(ee.moe_ffn(x, gu, dn, ids, w, workspace=ws[:most]), ee.moe_ffn(x, gu, dn, ids, w))
     assert (ws[most:] == 165).all()
+
+
+@pytest.mark.parametrize("rows,E,k", [(131073, 64, 4), (300007, 5, 2), (600011, 3, 1)])
+def test_pairs_sorted_in_longer_chunks(ee, rows, E, k):
+    """From 2^19 pairs on the sorting workgroups' chunks grow: every pair is in the
+    order once, so every row is what few of them alone give."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = torch.randn(rows, 32, generator=g, device="cuda").to(torch.bfloat16)
+    gu = (torch.randn(E, 64, 32, generator=g, device="cuda") * 0.2).to(torch.bfloat16)
+    dn = (torch.randn(E, 32, 32, generator=g, device="cuda") * 0.2).to(torch.bfloat16)
+    ids = torch.randint(-1, E, (rows, k), generator=g, device="cuda", dtype=torch.int32)
+    w = torch.rand(rows, k, generator=g, device="cuda")
+    want = torch.cat([ee.moe_ffn(x[i:i + 50000], gu, dn, ids[i:i + 50000], w[i:i + 50000]) for i in range(0, rows, 50000)])
+    out = torch.full((rows, 32), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(ee.moe_ffn(x, gu, dn, ids, w, out=out), want)
+    pick = torch.arange(0, rows, 997, device="cuda")
+    ref, err = _ffn64(x[pick], gu, dn, ids[pick], w[pick], None, "bf16")
+    _close(out[pick], ref.cpu(), (err + UBF * (ref.abs() + err) + 2 * U32 * ref.abs() + 1e-30).cpu())
