@@ -842,3 +842,22 @@ def test_pairs_sorted_in_longer_chunks(ee, rows, E, k):
     pick = torch.arange(0, rows, 997, device="cuda")
     ref, err = _ffn64(x[pick], gu, dn, ids[pick], w[pick], None, "bf16")
     _close(out[pick], ref.cpu(), (err + UBF * (ref.abs() + err) + 2 * U32 * ref.abs() + 1e-30).cpu())
+
+
+@pytest.mark.parametrize("make", [lambda m: -np.log((1 + m) * 2.0 ** -52), lambda m: -np.log((30000 + m) * 2.0 ** -52),
+                                  lambda m: -np.log(((1 << 20) + m) * 2.0 ** -52), lambda m: -709.78 + m * 1.3e-3,
+                                  lambda m: -708.3 + m * 0.02])
+def test_route_distinct_scores_near_their_bounds(ee, make):
+    """Sigmoid scores one or a few steps of float64 apart, just below 1 (logits of 22
+    to 36) and where they are about to leave the normal numbers: the order is the
+    definition's, and equal scores go to the lower index."""
+    l = make(np.arange(1024)).astype(np.float32)
+    rng = np.random.default_rng(36)
+    rows = np.stack([rng.permutation(l) for _ in range(16)])
+    for E in (64, 1024):
+        part = rows[:, :E]
+        ids, w = ee.moe_route(torch.from_numpy(part).contiguous().cuda(), 32, score="sigmoid", renormalize=False)
+        score = 1 / (1 + np.exp(-part.astype(np.float64)))
+        want = np.argsort(-score, axis=1, kind="stable")[:, :32]
+        assert np.array_equal(ids.cpu().numpy(), want)
+        np.testing.assert_allclose(w.cpu().numpy(), np.take_along_axis(score, want, 1), rtol=U32 * (1 + 1e-6), atol=2.0 ** -149)
