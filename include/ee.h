@@ -540,7 +540,8 @@ int32_t ee_moe_route(const ee_moe_route_args* args, void* hip_stream);
 /* out[t] = residual[t] + sum_j weights[t][j] * FFN_{ids[t][j]}(x[t]), slots in
  * order, FFN_e(x) = (silu(x Wg_e^T) * (x Wu_e^T)) Wd_e^T with the product in
  * parentheses rounded to dtype.  Slots whose id is outside [0, n_experts) are
- * skipped (a row with none: its residual, or zeros).  d_model and ffn: multiples of 32 (bf16)
+ * skipped (a row with none: its residual, or zeros).  n_experts <= 1024, top_k <= 32 and at
+ * most n_experts.  d_model and ffn: multiples of 32 (bf16)
  * or 16 (f32), at most 32768, an expert's w_gate_up below 2 GiB; rows * top_k
  * <= 2^24, ldx <= 2^21.  workspace: at least
  * ee_moe_ffn_workspace_bytes (0 for invalid sizes), 256-byte aligned, in use

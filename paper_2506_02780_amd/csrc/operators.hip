@@ -317,7 +317,8 @@ struct TileArgs {
 // Whether a workgroup takes one tile after another, so that the next one's first
 // stages are on their way while the last one's results are stored: where only one
 // workgroup fits a CU and reductions are short (8192 rows of 128 experts, 2048 x
-// 768: 942 us without, 903 so; linears and fp32 gain nothing, 8192 x 11008 606 us without,
+// 768: 942 us without, 909 so.  The down product's stores still wait for those requests:
+// the pairs' numbers that they need are loaded behind them.  Linears and fp32 gain nothing, 8192 x 11008 606 us without,
 // 612 so: the sums of their chains leave too few registers).
 template <int DT, int MODE, int BM, int BN, int NST, int SPS> constexpr bool tile_keeps() {
   return MODE != TM_LINEAR && DT != DT_F32 && (BM + BN) * SPS * 64 * NST > 80 * 1024;
