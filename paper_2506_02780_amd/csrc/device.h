@@ -129,4 +129,21 @@ __device__ __forceinline__ uint2 bload64(__amdgpu_buffer_rsrc_t r, unsigned off)
   return make_uint2(v.x, v.y);
 }
 
+// ---------------------------------------------------- waits and LDS requests --
+
+// Waits until at most N of the wave's vector memory operations are outstanding.
+template <int N> __device__ __forceinline__ void wait_vm() {
+  static_assert(N >= 0 && N < 64, "six bits");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+// Workgroup barrier that waits for no memory operation (the callers wait for
+// what they need), and that the compiler moves no access across.
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
 }  // namespace ee
