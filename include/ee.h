@@ -478,7 +478,8 @@ int32_t ee_time_gemm(ee_ctx* ctx, uint32_t cls, int32_t rows, int32_t reps, doub
  * buffer or output, or reps < 1. */
 int32_t ee_time_stream_read(ee_ctx* ctx, const void* dev_buf, size_t bytes, int32_t reps, double* us_per_pass);
 
-/* Stand-alone operators of sparse (mixture-of-experts) decoders.
+/* Stand-alone operators of decoder layers: of sparse (mixture-of-experts) ones
+ * first, then 8-bit products and a paged key-value cache.
  *
  * They need no context: device pointers, sizes and a hipStream_t, on the
  * device that is current and owns the stream.  They are asynchronous on that
@@ -564,6 +565,109 @@ typedef struct {
 size_t ee_moe_ffn_workspace_bytes(int32_t rows, int32_t n_experts, int32_t top_k, int32_t d_model, int32_t ffn,
                                   int32_t dtype);
 int32_t ee_moe_ffn(const ee_moe_ffn_args* args, void* hip_stream);
+
+/* e4m3 codes of x with one scale per block of block_rows (1 or 128) rows and 128
+ * columns, counted from row and column 0; the last ones may be smaller:
+ *   scale = max(largest finite |x| of the block / 448, 2^-126)
+ *   code  = x / scale to the nearest e4m3 value (even on ties), at most 448 in
+ *           magnitude; NaN stays NaN
+ * each quotient rounded once to fp32.  block_rows 1 makes the rows of ee_fp8_linear, 128 its
+ * weights.  rows <= 2^22; `in` a multiple of 16, at most 2^20. */
+typedef struct {
+  const void* x;            /* [rows][ldx] dtype, 16-byte aligned rows        */
+  uint8_t* codes;           /* [rows][ldc], 16-byte aligned rows              */
+  float* scales;            /* [ceil(rows / block_rows)][ceil(in / 128)]      */
+  int64_t ldx, ldc;
+  int32_t rows, in, block_rows, dtype;
+} ee_fp8_quant_args;
+int32_t ee_fp8_quant(const ee_fp8_quant_args* args, void* hip_stream);
+
+/* y[t][n] = act(sum_b xs[t][b] ws[n / 128][b] D_b + bias[n]) + residual[t][n],
+ * D_b the sum of x[t][k] w[n][k] over the columns of block b, 128 b .. 128 b + 127.
+ * Blocks are added in order in fp32.  D_b is an fp32 sum where out_dtype is EE_F32; where it
+ * is EE_BF16 it is the 8-bit matrix instruction's, which may be off by 2^-15 of the
+ * block's sum |x w| (by more where a few products dwarf the others: up to 2^-12 of it),
+ * a hundredth of what rounding to bf16 costs.  rows <= 2^22;
+ * `in` a multiple of 16, at most 2^20; any `out` up to 2^20. */
+typedef struct {
+  const uint8_t* x;         /* [rows][ldx] e4m3, 16-byte aligned rows         */
+  const float* x_scales;    /* [rows][ceil(in / 128)]                         */
+  const uint8_t* w;         /* [out][ldw] e4m3, 16-byte aligned rows          */
+  const float* w_scales;    /* [ceil(out / 128)][ceil(in / 128)]              */
+  const float* bias;        /* [out] or NULL                                  */
+  const void* residual;     /* [rows][ldr] out_dtype or NULL                  */
+  void* y;                  /* [rows][ldy] out_dtype                          */
+  int64_t ldx, ldw, ldr, ldy;
+  int32_t rows, in, out, out_dtype, act;
+} ee_fp8_linear_args;
+int32_t ee_fp8_linear(const ee_fp8_linear_args* args, void* hip_stream);
+
+/* A paged cache of the caller's: position p of sequence s is slot p % page_size of page
+ * tables[s][p / page_size].  Vector (page, slot, head) of k starts at element page *
+ * k_page + slot * k_slot + head * k_head, so pages may be [slot][head] or [head][slot], k and v
+ * one allocation or two.  Strides are multiples of 16 bytes; page_size is a multiple of 16.
+ * A table's entry outside [0, n_pages) is no page: its positions hold nothing. */
+typedef struct {
+  void* k;                  /* dtype, 16-byte aligned                         */
+  void* v;
+  const int32_t* tables;    /* [n_seqs][ld]                                   */
+  int64_t k_page, k_slot, k_head, v_page, v_slot, v_head, ld;
+  int32_t n_seqs, n_pages, max_pages, page_size;
+} ee_paged_cache;
+
+/* Appends a row's keys and values to its sequence's pages, the keys (and the
+ * queries, if given) rotated by the row's position:
+ *   (a, b) -> (a cos - b sin, a sin + b cos), angle positions[r] * inv_freq[i]
+ * for the pairs (i, i + rot_dim / 2) of every head, or (2i, 2i + 1) where
+ * interleaved; dimensions from rot_dim on stay as they are.  The angle is
+ * formed in float64, the rotation in fp32 and rounded once.  A row whose sequence is
+ * outside [0, n_seqs), whose position is negative or past max_pages pages, or whose page is
+ * none, is not stored (its q is rotated); nothing else of the cache is written.
+ * Rows of one call should name different slots: of two at one slot either may
+ * remain, piece by piece.  head_dim 64, 128 or 256; n_heads a multiple of n_kv_heads, at most 1024 (n_kv_heads
+ * itself where q is NULL would do); rot_dim a multiple of 16. */
+typedef struct {
+  const void* q;            /* [rows][ldq] n_heads vectors, or NULL           */
+  const void* k;            /* [rows][ldk] n_kv_heads vectors                 */
+  const void* v;            /* [rows][ldv]                                    */
+  void* q_out;              /* [rows][ldqo]; may be q (same stride)           */
+  ee_paged_cache cache;
+  const int32_t* seqs;      /* [rows], or NULL: row r is of r / (rows / n_seqs) */
+  const int32_t* positions; /* [rows]                                         */
+  const double* inv_freq;   /* [rot_dim / 2]                                  */
+  int64_t ldq, ldk, ldv, ldqo;
+  int32_t rows, n_heads, n_kv_heads, head_dim, rot_dim, interleaved, dtype;
+} ee_kv_append_args;
+int32_t ee_kv_append(const ee_kv_append_args* args, void* hip_stream);
+
+/* Attention of the newest `rows` rows of every sequence over its pages.  Row t of
+ * sequence s (row s * rows + t of q and out) stands at position end - 1, end = lens[s] -
+ * rows + 1 + t, and sees the positions [max(0, end - window), end) that its pages hold
+ * (window 0: all of them), the rows' own among them: they are appended
+ * first.  out = sum_j softmax_j(scale q . k_j) v_j per query head, which reads KV head
+ * head / (n_heads / n_kv_heads); lse = the natural log of the sum of e^(scale q . k_j).
+ * A row that sees nothing (or only scores of -inf) is zeros with lse -inf; what a row does not
+ * see does not matter, NaN included.  lens are cut to [0, max_pages * page_size].
+ * Scores, weights and sums are fp32; a row's result depends on what it sees alone, so
+ * a block of rows equals its rows one by one.  rows 1 is a decoding step; at most 1024.
+ * workspace: at least ee_paged_attention_workspace_bytes (0 for invalid sizes), 256-byte aligned, in
+ * use until the call's work is done; calls that may overlap need one each.  The bytes never
+ * fall as n_seqs, rows or max_pages grow. */
+typedef struct {
+  const void* q;            /* [n_seqs * rows][ldq] dtype, 16-byte aligned rows */
+  ee_paged_cache cache;
+  const int32_t* lens;      /* [n_seqs]                                       */
+  void* out;                /* [n_seqs * rows][ldo] out_dtype                 */
+  float* lse;               /* [n_seqs * rows][n_heads] or NULL               */
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t ldq, ldo;
+  int32_t rows, n_heads, n_kv_heads, head_dim, window, dtype, out_dtype;
+  float scale;
+} ee_paged_attention_args;
+size_t ee_paged_attention_workspace_bytes(int32_t n_seqs, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          int32_t page_size, int32_t max_pages, int32_t window);
+int32_t ee_paged_attention(const ee_paged_attention_args* args, void* hip_stream);
 
 /* Message for the last failed call on ctx (or the last failed context-free
  * call when ctx is NULL).  Never NULL; the pointer stays valid until the next

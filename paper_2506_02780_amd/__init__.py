@@ -123,9 +123,43 @@ class EEMoeFfnArgs(ctypes.Structure):
                 ("dtype", _i32), ("out_dtype", _i32)]
 
 
+class EEFp8QuantArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("codes", _vp), ("scales", _vp), ("ldx", _i64), ("ldc", _i64),
+                ("rows", _i32), ("in_", _i32), ("block_rows", _i32), ("dtype", _i32)]
+
+
+class EEFp8LinearArgs(ctypes.Structure):
+    _fields_ = [("x", _vp), ("x_scales", _vp), ("w", _vp), ("w_scales", _vp), ("bias", _vp), ("residual", _vp), ("y", _vp),
+                ("ldx", _i64), ("ldw", _i64), ("ldr", _i64), ("ldy", _i64),
+                ("rows", _i32), ("in_", _i32), ("out", _i32), ("out_dtype", _i32), ("act", _i32)]
+
+
+# (ee_paged_cache, a member of both: its fields stand in its place)
+_CACHE = [("k_cache", _vp), ("v_cache", _vp), ("tables", _vp), ("k_page", _i64), ("k_slot", _i64), ("k_head", _i64),
+          ("v_page", _i64), ("v_slot", _i64), ("v_head", _i64), ("ld", _i64),
+          ("n_seqs", _i32), ("n_pages", _i32), ("max_pages", _i32), ("page_size", _i32)]
+
+
+class EEKvAppendArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("q_out", _vp), *_CACHE,
+                ("seqs", _vp), ("positions", _vp), ("inv_freq", _vp), ("ldq", _i64), ("ldk", _i64), ("ldv", _i64), ("ldqo", _i64),
+                ("rows", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("rot_dim", _i32),
+                ("interleaved", _i32), ("dtype", _i32)]
+
+
+class EEPagedAttentionArgs(ctypes.Structure):
+    _fields_ = [("q", _vp), *_CACHE, ("lens", _vp), ("out", _vp), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _sz),
+                ("ldq", _i64), ("ldo", _i64), ("rows", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32),
+                ("window", _i32), ("dtype", _i32), ("out_dtype", _i32), ("scale", ctypes.c_float)]
+
+
 ee_linear = _sig("ee_linear", _i32, [ctypes.POINTER(EELinearArgs), _vp])
 ee_moe_route = _sig("ee_moe_route", _i32, [ctypes.POINTER(EEMoeRouteArgs), _vp])
 ee_moe_ffn = _sig("ee_moe_ffn", _i32, [ctypes.POINTER(EEMoeFfnArgs), _vp])
+ee_fp8_quant = _sig("ee_fp8_quant", _i32, [ctypes.POINTER(EEFp8QuantArgs), _vp])
+ee_fp8_linear = _sig("ee_fp8_linear", _i32, [ctypes.POINTER(EEFp8LinearArgs), _vp])
+ee_kv_append = _sig("ee_kv_append", _i32, [ctypes.POINTER(EEKvAppendArgs), _vp])
+ee_paged_attention = _sig("ee_paged_attention", _i32, [ctypes.POINTER(EEPagedAttentionArgs), _vp])
 
 
 def _packed(name: str, args):
@@ -138,6 +172,11 @@ def _packed(name: str, args):
 _OP_LINEAR = _packed("ee_linear", EELinearArgs)
 _OP_ROUTE = _packed("ee_moe_route", EEMoeRouteArgs)
 _OP_FFN = _packed("ee_moe_ffn", EEMoeFfnArgs)
+_OP_FP8_QUANT = _packed("ee_fp8_quant", EEFp8QuantArgs)
+_OP_FP8_LINEAR = _packed("ee_fp8_linear", EEFp8LinearArgs)
+_OP_KV_APPEND = _packed("ee_kv_append", EEKvAppendArgs)
+_OP_PAGED_ATTENTION = _packed("ee_paged_attention", EEPagedAttentionArgs)
+ee_paged_attention_workspace_bytes = _sig("ee_paged_attention_workspace_bytes", _sz, [_i32] * 8)
 ee_moe_ffn_workspace_bytes = _sig("ee_moe_ffn_workspace_bytes", _sz, [_i32] * 6)
 
 ACTIVATIONS = ("none", "silu", "gelu", "gelu_tanh", "relu")
@@ -380,6 +419,188 @@ def moe_ffn(x, w_gate_up, w_down, ids, weights, residual=None, out=None, out_dty
               workspace.numel(), ldx, ldr, ldo, rows, E, k, d, f, dt, _TYPES[odt])
     if given:
         _written(out)
+    return out
+
+
+def _codes(t, what: str):
+    """Checks e4m3 codes [rows, cols] of unit column stride: (device index, rows, cols, row stride)."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or not t.is_cuda or t.dtype is not torch.float8_e4m3fn:
+        raise EEError(EE_EINVAL, f"{what} must be a two-dimensional float8_e4m3fn tensor on a GPU")
+    rows, cols = t.shape
+    dev = t.get_device()
+    return dev, rows, cols, _rows_of(t, what, t.shape, t.dtype, dev)
+
+
+def fp8_quant(x, block_rows: int = 1, codes=None, scales=None):
+    """e4m3 codes of x [rows, in] (float32 or bfloat16) and their scales, one per
+    block of ``block_rows`` (1, or 128 for weights) rows and 128 columns
+    (ee_fp8_quant): (float8_e4m3fn [rows, in], float32 [ceil(rows / block_rows), ceil(in / 128)])."""
+    dev, dt, rows, cols, ldx = _operand(x, "x")
+    if _tangents():
+        _refuse_tangents(x=x)
+    if block_rows not in (1, 128):
+        raise EEError(EE_EINVAL, "block_rows must be 1 or 128")
+    shape = (-(-rows // block_rows), -(-cols // 128))
+    given = codes, scales
+    if codes is None:
+        codes, ldc = x.new_empty((rows, cols), dtype=torch.float8_e4m3fn), cols
+    else:
+        ldc = _rows_of(codes, "codes", (rows, cols), torch.float8_e4m3fn, dev)
+    if scales is None:
+        scales = x.new_empty(shape, dtype=torch.float32)
+    _operator(_OP_FP8_QUANT, dev, x.data_ptr(), codes.data_ptr(), _whole(scales, "scales", shape, torch.float32, dev), ldx, ldc,
+              rows, cols, block_rows, dt)
+    for t in given:
+        if t is not None:
+            _written(t)
+    return codes, scales
+
+
+def fp8_linear(x, x_scales, w, w_scales, bias=None, act: str = "none", residual=None, out=None, out_dtype=None):
+    """act(x w^T + bias) + residual of e4m3 codes and their scales (ee_fp8_linear): x
+    [rows, in] with a scale per row and 128 columns, w [out, in] with one per 128
+    rows and 128 columns, as ``fp8_quant`` makes them with ``block_rows`` 1 and 128.  ``out_dtype``:
+    bfloat16 (the default), or float32, whose products are summed in float32
+    throughout.  ``out`` may be the residual."""
+    dev, rows, cols, ldx = _codes(x, "x")
+    if _tangents():
+        _refuse_tangents(x_scales=x_scales, w_scales=w_scales, bias=bias, residual=residual, out=out)
+    code = _ACT_OF.get(act)
+    if code is None:
+        raise EEError(EE_EINVAL, f"act must be one of {ACTIVATIONS}")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise EEError(EE_EINVAL, "w must be [out, in]")
+    n, blocks = w.shape[0], -(-cols // 128)
+    ldw = _rows_of(w, "w", (n, cols), x.dtype, dev)
+    if out_dtype is None and out is None:
+        odt = torch.bfloat16
+    else:
+        odt = _out_type(out_dtype, out, x)
+    shape = (rows, n)
+    given = out is not None
+    if given:
+        ldy = _rows_of(out, "out", shape, odt, dev)
+    else:
+        out, ldy = x.new_empty(shape, dtype=odt), n
+    ldr = 0 if residual is None else _rows_of(residual, "residual", shape, odt, dev)
+    _operator(_OP_FP8_LINEAR, dev, x.data_ptr(), _whole(x_scales, "x_scales", (rows, blocks), torch.float32, dev), w.data_ptr(),
+              _whole(w_scales, "w_scales", (-(-n // 128), blocks), torch.float32, dev),
+              0 if bias is None else _whole(bias, "bias", (n,), torch.float32, dev),
+              0 if residual is None else residual.data_ptr(), out.data_ptr(), ldx, ldw, ldr, ldy, rows, cols, n, _TYPES[odt], code)
+    if given:
+        _written(out)
+    return out
+
+
+def _cache(k_cache, v_cache, tables, dtype, dev: int):
+    """Checks a paged cache: (its arguments, page size, KV heads, head_dim, max_pages, sequences)."""
+    if not (isinstance(k_cache, torch.Tensor) and isinstance(v_cache, torch.Tensor) and k_cache.dim() == 4
+            and k_cache.shape == v_cache.shape and k_cache.dtype is dtype and v_cache.dtype is dtype
+            and k_cache.get_device() == dev and v_cache.get_device() == dev):
+        raise EEError(EE_EINVAL, f"k_cache and v_cache must be [pages, page size, KV heads, head_dim] {dtype} on cuda:{dev}")
+    if (k_cache.requires_grad or v_cache.requires_grad) and torch.is_grad_enabled():
+        raise EEError(EE_EINVAL, "the cache requires a gradient, which these operators do not have (use torch.no_grad)")
+    pages, page, heads, hd = k_cache.shape
+    kp, ks, kh, kd = k_cache.stride()
+    vp, vs, vh, vd = v_cache.stride()
+    if kd != 1 or vd != 1:
+        raise EEError(EE_EINVAL, "k_cache and v_cache must have unit stride within a vector")
+    if not isinstance(tables, torch.Tensor) or tables.dim() != 2:
+        raise EEError(EE_EINVAL, "tables must be [sequences, pages of one]")
+    n, most = tables.shape
+    ld = _rows_of(tables, "tables", (n, most), torch.int32, dev)
+    # (a dimension of one element may carry any stride)
+    if pages <= 1:
+        kp = vp = 0
+    if heads <= 1:
+        kh = vh = 0
+    return (k_cache.data_ptr(), v_cache.data_ptr(), tables.data_ptr(), kp, ks, kh, vp, vs, vh, ld, n, pages, most, page), page, heads, hd, most, n
+
+
+def kv_append(k, v, k_cache, v_cache, tables, positions, seqs=None, q=None, inv_freq=None, interleaved: bool = False, q_out=None):
+    """Writes the rows of k and v [rows, KV heads * head_dim] to their sequences'
+    pages, k rotated by its row's position; q [rows, heads * head_dim], if given, is rotated
+    too and returned (``q_out``, which may be q; else None) (ee_kv_append).  k_cache and
+    v_cache [pages, page size, KV heads, head_dim] of any strides, tables int32 [sequences,
+    pages of one], positions int32 [rows], seqs int32 [rows] (the default: equally many
+    consecutive rows of every sequence), inv_freq float64 [rotated dimensions / 2] (None: no
+    rotation).  Operands are float32 or bfloat16, all of one type."""
+    dev, dt, rows, kd, ldk = _operand(k, "k")
+    if _tangents():
+        _refuse_tangents(q=q, k=k, v=v, k_cache=k_cache, v_cache=v_cache, inv_freq=inv_freq, q_out=q_out)
+    cache, _, heads, hd, _, _ = _cache(k_cache, v_cache, tables, k.dtype, dev)
+    if kd != heads * hd:
+        raise EEError(EE_EINVAL, f"k must be [rows, {heads} * {hd}]")
+    ldv = _rows_of(v, "v", (rows, kd), k.dtype, dev)
+    n_heads, ldq, ldqo, given = heads, 0, 0, q_out is not None
+    if q is None:
+        if given:
+            raise EEError(EE_EINVAL, "q_out needs q")
+    else:
+        if not isinstance(q, torch.Tensor) or q.dim() != 2 or hd < 1 or q.shape[1] % hd:
+            raise EEError(EE_EINVAL, f"q must be [rows, heads * {hd}]")
+        qd = q.shape[1]
+        n_heads = qd // hd
+        ldq = _rows_of(q, "q", (rows, qd), k.dtype, dev)
+        if given:
+            ldqo = _rows_of(q_out, "q_out", (rows, qd), k.dtype, dev)
+        else:
+            q_out, ldqo = q.new_empty((rows, qd)), qd
+    rot, freq = 0, 0
+    if inv_freq is not None:
+        if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+            raise EEError(EE_EINVAL, "inv_freq must be [rotated dimensions / 2]")
+        rot = 2 * inv_freq.shape[0]
+        freq = _whole(inv_freq, "inv_freq", inv_freq.shape, torch.float64, dev)
+    _operator(_OP_KV_APPEND, dev, 0 if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), 0 if q is None else q_out.data_ptr(),
+              *cache, 0 if seqs is None else _whole(seqs, "seqs", (rows,), torch.int32, dev),
+              _whole(positions, "positions", (rows,), torch.int32, dev), freq, ldq, ldk, ldv, ldqo,
+              rows, n_heads, heads, hd, rot, 1 if interleaved else 0, dt)
+    _written(k_cache)
+    _written(v_cache)
+    if given:
+        _written(q_out)
+    return q_out
+
+
+_attention_workspace = functools.lru_cache(maxsize=1024)(ee_paged_attention_workspace_bytes)   # (a function of its arguments)
+
+
+def paged_attention(q, k_cache, v_cache, tables, lens, window: int = 0, scale=None, out=None, out_dtype=None, lse=None, workspace=None):
+    """Attention of the newest rows of every sequence over its pages (ee_paged_attention):
+    q [sequences * rows, heads * head_dim], a sequence's rows one after another, the
+    cache and tables as ``kv_append`` writes them, lens int32 [sequences] (positions
+    held, these rows' among them).  ``window``: positions a row sees, its own last (0:
+    all).  ``scale``: of the scores, 1 / sqrt(head_dim) unless given.  ``lse``: a float32
+    tensor [sequences * rows, heads] for the logarithms of the softmax's sums.
+    ``workspace``: a uint8 tensor of at least ee_paged_attention_workspace_bytes, else one is allocated."""
+    dev, dt, total, qd, ldq = _operand(q, "q")
+    if _tangents():
+        _refuse_tangents(q=q, k_cache=k_cache, v_cache=v_cache, out=out, lse=lse)
+    cache, page, heads, hd, most, n = _cache(k_cache, v_cache, tables, q.dtype, dev)
+    if hd < 1 or qd % hd or (total % n if n else total):
+        raise EEError(EE_EINVAL, f"q must be [{n} * rows, heads * {hd}]")
+    rows = total // n if n else 1
+    odt = _out_type(out_dtype, out, q)
+    shape = (total, qd)
+    given = out is not None
+    if given:
+        ldo = _rows_of(out, "out", shape, odt, dev)
+    else:
+        out, ldo = q.new_empty(shape, dtype=odt), qd
+    window, n_heads = int(window), qd // hd
+    if workspace is None:
+        workspace = q.new_empty(_attention_workspace(n, rows, n_heads, heads, hd, page, most, window), dtype=torch.uint8)
+    elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or workspace.get_device() != dev
+          or not workspace.is_contiguous()):
+        raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")
+    _operator(_OP_PAGED_ATTENTION, dev, q.data_ptr(), *cache, _whole(lens, "lens", (n,), torch.int32, dev), out.data_ptr(),
+              0 if lse is None else _whole(lse, "lse", (total, n_heads), torch.float32, dev), workspace.data_ptr(), workspace.numel(),
+              ldq, ldo, rows, n_heads, heads, hd, window, dt, _TYPES[odt], hd ** -0.5 if scale is None else scale)
+    if given:
+        _written(out)
+    if lse is not None:
+        _written(lse)
     return out
 
 

@@ -7,7 +7,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libee.so")
-SOURCES = ["kernels.hip", "operators.hip", "engine.cpp", "operators.cpp", "match.cpp", "driver.cpp"]
+SOURCES = ["kernels.hip", "operators.hip", "fp8.hip", "attention.hip", "engine.cpp", "operators.cpp", "match.cpp", "driver.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -58,4 +58,64 @@ struct FfnArgs {
 size_t ffn_workspace(int T, int E, int k, int d, int F, int dt);
 hipError_t run_ffn(const FfnArgs& a, hipStream_t st);
 
+// e4m3 codes of x and their scales, one per block of block_rows rows and BLOCK columns.
+constexpr int BLOCK = 128;
+struct Fp8QuantArgs {
+  const void* x;        // [T][ldx] dt
+  uint8_t* codes;       // [T][ldc]
+  float* scales;        // [ceil(T / block_rows)][ceil(K / BLOCK)]
+  int64_t ldx, ldc;
+  int T, K, dt, block_rows;
+};
+hipError_t run_fp8_quant(const Fp8QuantArgs& a, hipStream_t st);
+
+// A linear of e4m3 codes (l.x, l.w: bytes) with their scales.
+struct Fp8LinearArgs {
+  LinearArgs l;
+  const float* xs;      // [T][ceil(K / BLOCK)]
+  const float* ws;      // [ceil(N / BLOCK)][ceil(K / BLOCK)]
+};
+hipError_t run_fp8_linear(const Fp8LinearArgs& a, hipStream_t st);
+
+// Position p of sequence s: slot p % page of page tables[s][p / page], where that is in
+// [0, n_pages).  Strides in elements, of pages, slots and heads.
+struct PagedCache {
+  const void *k, *v;
+  int64_t kp, ks, kh, vp, vs, vh;
+  const int* tables;    // [sequences][ldt]
+  int64_t ldt;
+  int n_pages, max_pages, page;
+};
+constexpr int MAX_HEAD_DIM = 256;
+
+struct AppendArgs {
+  const void *q, *k, *v;    // [R][ld] dt: heads of hd; q may be null
+  void* q_out;
+  PagedCache c;
+  const int *seqs, *positions;   // [R]; seqs null: row / per_seq
+  const double* inv_freq;        // [rot / 2]
+  int64_t ldq, ldk, ldv, ldqo;
+  int R, B, per_seq, H, Hkv, hd, rot, interleaved, dt;
+};
+hipError_t run_append(const AppendArgs& a, hipStream_t st);
+
+constexpr int ATTEND_CHUNK = 256;   // positions whose state is held
+struct AttendArgs {
+  const void* q;        // [B T][ldq] dt
+  void* out;            // [B T][ldo] odt
+  float* lse;           // [B T][H] or null
+  PagedCache c;
+  const int* lens;      // [B] positions, the T rows' own among them
+  unsigned char* ws;    // attend_workspace(...) bytes
+  int64_t ldq, ldo;
+  int B, T, H, Hkv, G, hd, dt, odt, window;
+  float scale_log2;     // of scores, times log2 e
+  // (filled in by run_attend)
+  float2* ml;           // [B][ring][Hkv][T G] largest score and sum of the chunks' states
+  float* o;             // [..][hd] their weighted values
+  int ring, ctiles, splits;
+};
+size_t attend_workspace(int B, int T, int H, int hd, int64_t positions, int window);
+hipError_t run_attend(const AttendArgs& a, hipStream_t st);
+
 }  // namespace ee
