@@ -19,6 +19,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "epilogue.h"
@@ -171,40 +172,480 @@ template <bool EXACT> __device__ __forceinline__ f32x4 block_product(Codes w, Co
   return d;
 }
 
-// One wave per 16 x 16 tile, operands from memory.
-template <bool EXACT>
-__global__ __launch_bounds__(64) void fp8_tile_kernel(Fp8LinearArgs a, int nft) {
-  const int lane = threadIdx.x, c = lane & 15, grp = lane >> 4;
-  const int f0 = blockIdx.x % nft * 16, t0 = blockIdx.x / nft * 16, K = a.l.K, kb = (K + BLOCK - 1) / BLOCK;
-  const uint8_t* w = (const uint8_t*)a.l.w + min(f0 + c, a.l.N - 1) * a.l.ldw + grp * 16;
-  const uint8_t* x = (const uint8_t*)a.l.x + min(t0 + c, a.l.T - 1) * a.l.ldx + grp * 16;
-  const float* xs = a.xs + (int64_t)min(t0 + c, a.l.T - 1) * kb;
-  const float* ws = a.ws + (int64_t)(f0 / BLOCK) * kb;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int b = 0; b < kb; ++b) {
-    Codes wf, xf;
+// The block that a feature's sum begins with (then the ones behind it, and round to the
+// first): each of four runs of 256 features two blocks on, so that the
+// tiles of a product that run side by side do not all read the same columns.  Where rows
+// are a power of two of bytes apart, one column's lines of all rows are on few of the
+// caches' channels (8192 x 4096 x 11008: 485 us from block 0 everywhere, 426 so; with a
+// quarter of the reduction between the runs, where they no longer share lines, 456).
+// A last block that is not whole stays the last.
+__device__ __forceinline__ int first_block(int K, int n) { return K % BLOCK ? 0 : (n / 256 & 3) * 2 % (K / BLOCK); }
+
+// ------------------------------------------------------- product, few rows --
+
+// At most 16 MT rows: the weights stream past them once, and what bounds the call is
+// how much of them is on its way.  A workgroup owns 16 NT features; its waves
+// share the blocks of the reduction, ROUND of them at a time: wave w multiplies
+// blocks w, w + W, ... and leaves every D_b in LDS, where threads then add a result's
+// terms in the order of the blocks.  The next round's operands are requested before that.
+constexpr int ROWS_WAVES = 8;
+template <bool EXACT, int MT, int NT, int U>
+__global__ __launch_bounds__(ROWS_WAVES * 64, 2) void fp8_rows_kernel(Fp8LinearArgs a) {
+  constexpr int W = ROWS_WAVES, ROUND = W * U, VALUES = MT * NT * 256, PER = (VALUES + W * 64 - 1) / (W * 64);
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  __shared__ uint4 sd[2][ROUND][MT * NT][64];   // D_b; lane quads of group grp at place lane ^ 4 grp, so that 16 features of 4 rows are on all banks
+  __shared__ float ss[2][ROUND][MT * NT][16];   // xs_b ws_b of the rows
+  const int f0 = blockIdx.x * (16 * NT), K = a.l.K, kb = (K + BLOCK - 1) / BLOCK;
+  const int t0 = blockIdx.y * (16 * MT);
+  const int start = first_block(K, a.n0 + f0);
+  const auto wr = make_rsrc((const uint8_t*)a.l.w + f0 * a.l.ldw, 0x7fffffffu);
+  const auto xr = make_rsrc((const uint8_t*)a.l.x + t0 * a.l.ldx, 0x7fffffffu);
+  unsigned wo[NT], xo[MT];
+  const float *xs[MT], *ws[NT];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int k = b * BLOCK + i * 64;
-      const bool in = k + grp * 16 < K;
-      wf.u[i] = in ? *(const uint4*)(w + k) : make_uint4(0u, 0u, 0u, 0u);
-      xf.u[i] = in ? *(const uint4*)(x + k) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    const f32x4 d = block_product<EXACT>(wf, xf);
-    const float s = xs[b] * ws[b];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] = fmaf(d[r], s, acc[r]);
+  for (int n = 0; n < NT; ++n) {
+    wo[n] = (unsigned)min(n * 16 + c, a.l.N - 1 - f0) * (unsigned)a.l.ldw + grp * 16;
+    ws[n] = a.ws + (int64_t)(min(f0 + n * 16, a.l.N - 1) / BLOCK) * kb;
   }
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int t = min(m * 16 + c, a.l.T - 1 - t0);
+    xo[m] = (unsigned)t * (unsigned)a.l.ldx + grp * 16;
+    xs[m] = a.xs + (int64_t)(t0 + t) * kb;
+  }
+  Codes wf[U][NT], xf[U][MT];
+  float xv[U][MT], wsv[U][NT];
+  auto load = [&](int b0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int b = b0 + u * W + wv;
+      const bool some = b < kb;
+      b += start;
+      b -= b < kb ? 0 : kb;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const unsigned k = b * BLOCK + h * 64;
+        const bool in = some && k + grp * 16 < (unsigned)K;   // (past the reduction: zeros)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wf[u][n].u[h] = bload<0>(wr, in ? wo[n] + k : OOB);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xf[u][m].u[h] = bload<0>(xr, in ? xo[m] + k : OOB);
+      }
+      const int bc = some ? b : 0;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xv[u][m] = xs[m][bc];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) wsv[u][n] = ws[n][bc];
+    }
+  };
+  float acc[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+  load(0);
+  int buf = 0;
+  for (int b0 = 0; b0 < kb; b0 += ROUND) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const f32x4 d = block_product<EXACT>(wf[u][n], xf[u][m]);
+          sd[buf][u * W + wv][m * NT + n][lane ^ (4 * grp)] = __builtin_bit_cast(uint4, d);
+          if (grp == 0) ss[buf][u * W + wv][m * NT + n][c] = xv[u][m] * wsv[u][n];
+        }
+    if (b0 + ROUND < kb) load(b0 + ROUND);
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+    barrier_only();
+    const int terms = min(ROUND, kb - b0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = threadIdx.x + i * (W * 64), tile = e / 256, f = e & 15, t = (e >> 4) & 15;
+      if (VALUES % (W * 64) == 0 || e < VALUES) {
+        const float* d = (const float*)&sd[buf][0][tile][((f >> 2) * 16 + t) ^ (f & 12)] + (f & 3);
+        const float* s = &ss[buf][0][tile][t];
+        if (terms == ROUND) {
+#pragma unroll
+          for (int j = 0; j < ROUND; ++j) acc[i] = fmaf(d[j * MT * NT * 256], s[j * MT * NT * 16], acc[i]);
+        } else {
+          for (int j = 0; j < terms; ++j) acc[i] = fmaf(d[j * MT * NT * 256], s[j * MT * NT * 16], acc[i]);
+        }
+      }
+    }
+    buf ^= 1;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = threadIdx.x + i * (W * 64), tile = e / 256;
+    const int n = f0 + tile % NT * 16 + (e & 15), t = t0 + tile / NT * 16 + ((e >> 4) & 15);
+    if (e >= VALUES || n >= a.l.N || t >= a.l.T) continue;
+    float v = activate(a.l.bias ? acc[i] + a.l.bias[n] : acc[i] + 0.f, a.l.act);
+    if (a.l.odt == DT_BF16) {
+      v += a.l.res ? load_elt<DT_BF16>(a.l.res, (size_t)t * a.l.ldr + n) : 0.f;
+      store_elt<DT_BF16>(a.l.y, (size_t)t * a.l.ldy + n, v);
+    } else {
+      v += a.l.res ? load_elt<DT_F32>(a.l.res, (size_t)t * a.l.ldr + n) : 0.f;
+      store_elt<DT_F32>(a.l.y, (size_t)t * a.l.ldy + n, v);
+    }
+  }
+}
+
+// ------------------------------------------------------ product, many rows --
+
+// Tiles of BM rows and BN features, both operands streamed through LDS, a block of the
+// reduction (128 bytes of a row) per stage, NST stages deep.  A wave holds the
+// fragments of its rows and takes those of its features one after another; D_b of
+// one product is scaled and added (four fma) while the next ones run.
+//   * Stages arrive by direct loads to LDS, eight rows of 128 bytes each; piece p of
+//     row r stands at place p ^ (r / 2 % 8), so that the 16 rows a fragment read
+//     touches fall on all banks.
+// Rows past the end repeat the last one; their results are not stored.
+template <bool EXACT, int BM, int BN, int WR, int WF, int NST>
+__global__ __launch_bounds__(WR * WF * 64, WR * WF >= 4 ? 2 : 1) void fp8_tile_kernel(Fp8LinearArgs a, int nrt, int nft) {
+  constexpr int WAVES = WR * WF, RF = BM / WR / 16, FF = BN / WF / 16;
+  constexpr int LOADS = (BM + BN) / 8, LPW = (LOADS + WAVES - 1) / WAVES, STAGE = (BM + BN) * 8;
+  static_assert(RF * WR * 16 == BM && FF * WF * 16 == BN, "whole fragments");
+  static_assert(BN % BLOCK == 0 || BLOCK % BN == 0, "whole blocks of features, or parts of one");
+  static_assert(FF % 2 == 0 && (NST == 4 || (NST == 2 && FF > 2)) && (NST - 1) * LPW < 64, "");
+  // (arrays of their own: the compiler then knows that a request into one does not touch the
+  // others, for up to four.  The last one has room for the scales: a wave's rows', then its features')
+  constexpr int SROWS = RF * 16 + 1;
+  __shared__ uint4 b0[STAGE], b1[STAGE + (NST == 2 ? WAVES * SROWS : 0)], b2[NST > 2 ? STAGE : 1], b3[NST > 2 ? STAGE + WAVES * SROWS : 1];
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  const int wr = wv / WF, wf = wv % WF;
+  // Each XCD takes a run of the tiles, GR row tiles side by side under one feature tile after another.
+  constexpr int GR = 8;
+  const int ntile = nrt * nft, per = (ntile + 7) / 8, tile = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || tile >= ntile) return;
+  const int gsz = GR * nft, gi = tile / gsz, gr0 = gi * GR, gh = min(GR, nrt - gr0), gj = tile - gi * gsz;
+  const int t0 = (gr0 + gj % gh) * BM, f0 = gj / gh * BN;
+  const int K = a.l.K, kb = (K + BLOCK - 1) / BLOCK, tail = K % BLOCK, start = first_block(K, a.n0 + f0);
+  const uint8_t* xb = (const uint8_t*)a.l.x + (size_t)t0 * a.l.ldx;
+  const uint8_t* wb = (const uint8_t*)a.l.w + (size_t)f0 * a.l.ldw;
+
+  // The order of the features within a wave's tiles, as for the other linears: eight in a row per lane.
+  const bool wide = linear_wide(a.l);
+  auto feature = [&](int f, int m) { return wide ? (f >> 1) * 32 + (m >> 2) * 8 + (f & 1) * 4 + (m & 3) : f * 16 + m; };
+
+  // (every wave requests as much, since it counts them: the last one may come more than once)
+  auto load = [&](int i) { return min(wv * LPW + i, LOADS - 1); };
+  unsigned off[LPW];
+#pragma unroll
+  for (int i = 0; i < LPW; ++i) {
+    const int inst = load(i);
+    int r = inst * 8 + lane / 8;
+    const unsigned piece = ((lane % 8) ^ ((r >> 1) & 7)) * 16;
+    if (inst < BM / 8) {
+      off[i] = (unsigned)min(r, a.l.T - 1 - t0) * (unsigned)a.l.ldx + piece;
+    } else {
+      r -= BM;
+      const int w = r / (FF * 16), j = r % (FF * 16);
+      r = min(w * (FF * 16) + feature(j / 16, j % 16), a.l.N - 1 - f0);
+      off[i] = (unsigned)r * (unsigned)a.l.ldw + piece;
+    }
+  }
+  // Requests load i of block `next` (past the last one: the first ones again, unused).  Pieces past
+  // the reduction are not there: the row's first one of the block comes in their place.
+  unsigned past[2];   // (by the parity of the load: piece p of row r is at p ^ (r / 2 % 8))
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const unsigned piece = ((lane % 8) ^ (i * 4 + (lane >> 4))) * 16;
+    past[i] = tail && piece >= (unsigned)tail ? piece : 0u;
+  }
+  int next = start;
+  unsigned at_end = kb == 1 ? ~0u : 0u;
+  auto fetch_one = [&](uint4* buf, int i) {
+    const int inst = load(i);
+    const unsigned over = past[inst & 1] & at_end;
+    const uint8_t* src = (inst < BM / 8 ? xb : wb) + (size_t)next * BLOCK;
+    __builtin_amdgcn_global_load_lds((global_void*)(src + (off[i] - over)), (lds_void*)(buf + inst * 64), 16, 0, 0);
+  };
+  auto fetched = [&]() {
+    next = next + 1 < kb ? next + 1 : 0;
+    at_end = next == kb - 1 ? ~0u : 0u;
+  };
+
+  // xs_b ws_b of the 4 g-th to 4 g + 3-rd block for the wave's rows, one row a lane.  They are
+  // requested to LDS too, to a place of the wave's own, and taken from there at once: the
+  // compiler would let loads to registers wait for all requests to LDS, and every
+  // read of an array in LDS that is not requested so.
+  static_assert(RF <= 4, "a lane per row");
+  const float* xs = a.xs + (int64_t)t0 * kb;
+  const float* ws = a.ws + (int64_t)min((f0 + wf * (FF * 16)) / BLOCK, (a.l.N - 1) / BLOCK) * kb;
+  uint4* const sx = (NST > 2 ? b3 : b1) + STAGE + wv * SROWS;
+  auto scales_request = [&](int g) {
+    const int i = min(4 * g + (lane & 3), kb - 1) + start;
+    const unsigned b = i < kb ? i : i - kb;
+#pragma unroll
+    for (int r = 0; r < RF; ++r) {
+      const float* src = xs + ((unsigned)min((wr * RF + r) * 16 + lane / 4, a.l.T - 1 - t0) * (unsigned)kb + b);
+      __builtin_amdgcn_global_load_lds((global_void*)src, (lds_void*)(sx + r * 16), 4, 0, 0);
+    }
+    if (lane < 4) __builtin_amdgcn_global_load_lds((global_void*)(ws + b), (lds_void*)(sx + RF * 16), 4, 0, 0);
+  };
+  f32x4 sv;
+  auto scales_take = [&]() {
+    const f32x4 x = __builtin_bit_cast(f32x4, sx[lane % (RF * 16)]), w = __builtin_bit_cast(f32x4, sx[RF * 16]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sv[j] = x[j] * w[j];
+  };
+  auto scale = [&](int j, int r) { return __uint_as_float(__builtin_amdgcn_ds_bpermute((r * 16 + c) * 4, __float_as_uint(sv[j]))); };
+
+  f32x4 acc[FF][RF];
+#pragma unroll
+  for (int f = 0; f < FF; ++f)
+#pragma unroll
+    for (int r = 0; r < RF; ++r) acc[f][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int q = grp ^ ((c >> 1) & 7);
+  const int xo = (wr * RF * 16 + c) * 8 + q, wo = (BM + wf * FF * 16 + c) * 8 + q;
+  Codes xf[RF], wt[4];
+  float s[RF], sn[RF];
+  auto read = [&](const uint4* buf, int at, Codes& f) {
+    f.u[0] = buf[at];
+    f.u[1] = buf[at ^ 4];
+  };
+  // (in the last block, what is past the reduction becomes zeros)
+  auto masked = [&](Codes& f, bool last) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t m = last && tail && (grp + 4 * h) * 16 >= tail ? 0u : ~0u;
+      f.u[h].x &= m; f.u[h].y &= m; f.u[h].z &= m; f.u[h].w &= m;
+    }
+  };
+  f32x4 d[3];
+  auto add = [&](int n, int f, int r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[f][r][i] = fmaf(d[n % 3][i], s[r], acc[f][r][i]);
+    asm volatile("" : "+v"(acc[f][r]));   // (here: moved behind the stage's branches, all products' sums would be live at once)
+  };
+  constexpr int EARLY = (LPW + 1) / 2, GROUPS = FF / 2, PG = 2 * RF;   // products of a group
+  // The b-th block, in `cur`; the next one is in `nxt`.  Once every wave has read it, `cur` takes the
+  // block NST on, half of it requested at once and half in the next stage, where it is `prev`.
+  auto stage = [&](uint4* cur, uint4* nxt, uint4* prev, int b, auto place, auto rest) {
+    constexpr bool REST = decltype(rest)::value;
+    constexpr int J = decltype(place)::value;   // b % 4
+    if constexpr (J == 0) scales_request(b / 4 + 1);
+    if constexpr (REST)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) masked(xf[r], b == kb - 1);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      Codes* const now = wt + (J * GROUPS + g) % 2 * 2;
+      Codes* const then = wt + (J * GROUPS + g + 1) % 2 * 2;
+      const bool last = g == GROUPS - 1;
+      if constexpr (REST) {
+        masked(now[0], b == kb - 1);
+        masked(now[1], b == kb - 1);
+      }
+      if (last) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): this wave's reads of `cur` are done
+        // its part of `nxt` has arrived: later stages' requests may be left (of one group: half of the last one's)
+        wait_vm<(GROUPS > 1 ? (NST - 2) * LPW : (NST > 2 ? NST - 3 : 0) * LPW + EARLY)>();
+        barrier_only();
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) read(last ? nxt : cur, wo + (last ? k : 2 * g + 2 + k) * 128, then[k]);
+      if (g == 0) {
+#pragma unroll
+        for (int i = EARLY; i < LPW; ++i) fetch_one(prev, i);
+        fetched();
+      }
+      if (last) {
+        if constexpr (J == 3) scales_take();
+#pragma unroll
+        for (int r = 0; r < RF; ++r) sn[r] = scale((J + 1) & 3, r);
+      }
+#pragma unroll
+      for (int i = 0; i < PG; ++i) {
+        const int r = i / 2, n = g * PG + i;
+        __builtin_amdgcn_sched_barrier(0);
+        d[n % 3] = block_product<EXACT>(now[i & 1], xf[r]);
+        if (last && (i & 1)) {
+          read(nxt, xo + r * 128, xf[r]);
+#pragma unroll
+          for (int j = r * EARLY / RF; j < (r + 1) * EARLY / RF; ++j) fetch_one(cur, j);
+        }
+        if (n >= 2) {
+          const int m = n - 2;
+          add(m, m / PG * 2 + m % PG % 2, m % PG / 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    add(GROUPS * PG - 2, FF - 2, RF - 1);
+    add(GROUPS * PG - 1, FF - 1, RF - 1);
+#pragma unroll
+    for (int r = 0; r < RF; ++r) s[r] = sn[r];
+  };
+
+  scales_request(0);
+  auto fetch = [&](uint4* buf) {
+#pragma unroll
+    for (int i = 0; i < LPW; ++i) fetch_one(buf, i);
+    fetched();
+  };
+  fetch(b0);
+  if constexpr (NST > 2) {
+    fetch(b1);
+    fetch(b2);
+  }
+#pragma unroll
+  for (int i = 0; i < EARLY; ++i) fetch_one(NST > 2 ? b3 : b1, i);
+  wait_vm<(NST - 2) * LPW + EARLY>();
+  barrier_only();
+  scales_take();
+  read(b0, wo, wt[0]);
+  read(b0, wo + 128, wt[1]);
+#pragma unroll
+  for (int r = 0; r < RF; ++r) {
+    read(b0, xo + r * 128, xf[r]);
+    s[r] = scale(0, r);
+  }
+  {
+    // (whole turns without an exit between the stages, so that the compiler sees
+    // which request each read follows and adds no wait of its own)
+    const int turns = (kb - 1) / 4;
+    int b = 0;
+    constexpr std::integral_constant<int, 0> p0{};
+    constexpr std::integral_constant<int, 1> p1{};
+    constexpr std::integral_constant<int, 2> p2{};
+    constexpr std::integral_constant<int, 3> p3{};
+    uint4 *const c2 = NST > 2 ? b2 : b0, *const c3 = NST > 2 ? b3 : b1;
+    for (; b < turns * 4; b += 4) {
+      constexpr std::false_type go{};
+      stage(b0, b1, c3, b, p0, go);
+      stage(b1, c2, b0, b + 1, p1, go);
+      stage(c2, c3, b1, b + 2, p2, go);
+      stage(c3, b0, c2, b + 3, p3, go);
+    }
+    constexpr std::true_type end{};
+    stage(b0, b1, c3, b, p0, end);
+    if (b + 1 < kb) stage(b1, c2, b0, b + 1, p1, end);
+    if (b + 2 < kb) stage(c2, c3, b1, b + 2, p2, end);
+    if (b + 3 < kb) stage(c3, b0, c2, b + 3, p3, end);
+  }
+  wait_vm<0>();   // (nothing may arrive in LDS after the workgroup's end)
+
   const bool vec = linear_vec(a.l);
-  const int t = t0 + c, n = f0 + 4 * grp;
-  linear_out(a.l, t, n, acc, linear_bias(a.l, n), linear_residual(a.l, t, n, vec), vec);
+  auto each = [&](int fa, int fb, auto fn) {
+#pragma unroll
+    for (int f = fa; f < fb; ++f)
+#pragma unroll
+      for (int r = 0; r < RF; ++r) fn(f, r, t0 + (wr * RF + r) * 16 + c, f0 + wf * (FF * 16) + feature(f, 4 * grp));
+  };
+#pragma unroll
+  for (int f = 0; f < FF; ++f) {
+    const f32x4 bias = linear_bias(a.l, f0 + wf * (FF * 16) + feature(f, 4 * grp));
+#pragma unroll
+    for (int r = 0; r < RF; ++r) acc[f][r] += bias;
+  }
+  auto act = [&](auto kind) { each(0, FF, [&](int f, int r, int, int) { acc[f][r] = activate4(acc[f][r], decltype(kind)::value); asm volatile("" : "+v"(acc[f][r])); }); };
+  switch (a.l.act) {
+    case ACT_SILU: act(std::integral_constant<int, ACT_SILU>{}); break;
+    case ACT_GELU: act(std::integral_constant<int, ACT_GELU>{}); break;
+    case ACT_GELU_TANH: act(std::integral_constant<int, ACT_GELU_TANH>{}); break;
+    case ACT_RELU: act(std::integral_constant<int, ACT_RELU>{}); break;
+    default: break;
+  }
+  // (the residual of two features' tiles at a time: y may be the residual, so the compiler keeps each load behind the stores before it)
+#pragma unroll
+  for (int f = 0; f < FF; f += 2) {
+    f32x4 res[2][RF];
+    each(f, f + 2, [&](int g, int r, int, int) { res[g - f][r] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    if (a.l.res) each(f, f + 2, [&](int g, int r, int t, int n) { res[g - f][r] = linear_residual(a.l, t, n, vec); });
+    each(f, f + 2, [&](int g, int r, int, int) { acc[g][r] += res[g - f][r]; });
+    if (wide) each(f, f + 1, [&](int g, int r, int t, int n) { linear_store8(a.l, t, n, acc[g][r], acc[g + 1][r]); });
+    else if (vec) each(f, f + 2, [&](int g, int r, int t, int n) { linear_store(a.l, t, n, acc[g][r], true); });
+    else each(f, f + 2, [&](int g, int r, int t, int n) { linear_store(a.l, t, n, acc[g][r], false); });
+  }
+}
+
+template <bool EXACT, int MT, int NT, int U>
+static hipError_t rows_t(const Fp8LinearArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((fp8_rows_kernel<EXACT, MT, NT, U>), dim3((unsigned)((a.l.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.l.T + 16 * MT - 1) / (16 * MT))),
+                     dim3(ROWS_WAVES * 64), 0, st, a);
+  return hipGetLastError();
+}
+template <bool EXACT, int BM, int BN, int WR, int WF, int NST>
+static hipError_t tiles_t(const Fp8LinearArgs& a, hipStream_t st) {
+  const int nrt = (a.l.T + BM - 1) / BM, nft = (a.l.N + BN - 1) / BN;
+  const int64_t per = ((int64_t)nrt * nft + 7) / 8;
+  hipLaunchKernelGGL((fp8_tile_kernel<EXACT, BM, BN, WR, WF, NST>), dim3((unsigned)(per * 8)), dim3(WR * WF * 64), 0, st, a, nrt, nft);
+  return hipGetLastError();
+}
+
+// The tile whose turns of the chip take least: us for a turn of 256 tiles over 32
+// blocks (measured at 1 to 8192 rows, reductions of 2048 to 11008 and 512 to 22016 features; a
+// tile's turn takes about as long when it is not full).
+struct Fp8Tile {
+  int bm, bn;
+  double turn;
+  hipError_t (*run)(const Fp8LinearArgs&, hipStream_t);
+};
+template <bool EXACT> static const auto& fp8_tiles() {
+  if constexpr (EXACT) {
+    static constexpr Fp8Tile tiles[] = {{32, 64, 17, tiles_t<true, 32, 64, 1, 2, 4>},
+                                        {64, 64, 18, tiles_t<true, 64, 64, 2, 2, 4>},
+                                        {128, 128, 37, tiles_t<true, 128, 128, 4, 2, 4>}};
+    return tiles;
+  } else {
+    static constexpr Fp8Tile tiles[] = {{16, 64, 10, tiles_t<false, 16, 64, 1, 2, 4>},
+                                        {32, 64, 11, tiles_t<false, 32, 64, 1, 2, 4>},
+                                        {64, 64, 11.5, tiles_t<false, 64, 64, 2, 2, 4>},
+                                        {64, 128, 16, tiles_t<false, 64, 128, 2, 4, 4>},
+                                        {80, 128, 20, tiles_t<false, 80, 128, 5, 2, 4>},
+                                        {128, 128, 24, tiles_t<false, 128, 128, 4, 2, 4>},
+                                        {256, 128, 40, tiles_t<false, 256, 128, 4, 2, 2>},
+                                        {256, 256, 66, tiles_t<false, 256, 256, 4, 2, 2>}};
+    return tiles;
+  }
+}
+template <bool EXACT> static double fp8_best(int T, int N, const Fp8Tile** best) {
+  double least = 1e30;
+  for (const Fp8Tile& t : fp8_tiles<EXACT>()) {
+    const double n = (double)((T + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn), c = ceil(n / 256) * t.turn;
+    if (c < least) {
+      least = c;
+      *best = &t;
+    }
+  }
+  return least;
+}
+
+template <bool EXACT> static hipError_t fp8_linear_t(Fp8LinearArgs a, hipStream_t st) {
+  // Few rows, or few features: the blocks of the reduction spread over waves (16 rows, 4096 ->
+  // 4096 7.5 us, 9.8 on tiles of 16 x 64; 24 rows, 11008 -> 4096 23.4, 28.8; 16 rows, 4096 -> 22016
+  // 30.3, 22.7).
+  if (a.l.T <= 4 || (int64_t)((a.l.N + 15) / 16) * ((a.l.T + 15) / 16) <= 512) return rows_t<EXACT, 1, 1, 4>(a, st);
+  const Fp8Tile *best = nullptr, *rest = nullptr;
+  const double all = fp8_best<EXACT>(a.l.T, a.l.N, &best);
+  // Whole turns of the largest tile, and the features that are left on the tile that
+  // does best for them, where that is worth its launch, 3 us (8192 x 4096 x 11008, 40 and 3 tiles of
+  // features: 5 turns and one of the half as large instead of 6).
+  const int kb = (a.l.K + BLOCK - 1) / BLOCK, nrt = (a.l.T + best->bm - 1) / best->bm;
+  const int64_t n = (int64_t)nrt * ((a.l.N + best->bn - 1) / best->bn);
+  if (best->bn == 256 && n > 256) {
+    const int cut = (int)(n / 256 * 256 / nrt) * 256;
+    if (cut > 0 && cut < a.l.N && ceil((double)(cut / 256) * nrt / 256) * best->turn + fp8_best<EXACT>(a.l.T, a.l.N - cut, &rest) + 3.0 * 32 / kb < all) {
+      Fp8LinearArgs b = a;
+      b.l.w = (const uint8_t*)a.l.w + (size_t)cut * a.l.ldw;
+      b.l.bias = a.l.bias ? a.l.bias + cut : nullptr;
+      const size_t off = (size_t)cut * (a.l.odt == DT_F32 ? 4 : 2);
+      b.l.res = a.l.res ? (const uint8_t*)a.l.res + off : nullptr;
+      b.l.y = (uint8_t*)a.l.y + off;
+      b.ws = a.ws + (size_t)(cut / BLOCK) * kb;
+      b.l.N = a.l.N - cut;
+      b.n0 = cut;
+      a.l.N = cut;
+      const hipError_t e = best->run(a, st);
+      return e == hipSuccess ? rest->run(b, st) : e;
+    }
+  }
+  return best->run(a, st);
 }
 
 hipError_t run_fp8_linear(const Fp8LinearArgs& a, hipStream_t st) {
-  const int nft = (a.l.N + 15) / 16, nrt = (a.l.T + 15) / 16;
-  if (a.l.odt == DT_F32) hipLaunchKernelGGL((fp8_tile_kernel<true>), dim3((unsigned)nft * nrt), dim3(64), 0, st, a, nft);
-  else hipLaunchKernelGGL((fp8_tile_kernel<false>), dim3((unsigned)nft * nrt), dim3(64), 0, st, a, nft);
-  return hipGetLastError();
+  return a.l.odt == DT_F32 ? fp8_linear_t<true>(a, st) : fp8_linear_t<false>(a, st);
 }
 
 }  // namespace ee

@@ -74,6 +74,7 @@ struct Fp8LinearArgs {
   LinearArgs l;
   const float* xs;      // [T][ceil(K / BLOCK)]
   const float* ws;      // [ceil(N / BLOCK)][ceil(K / BLOCK)]
+  int n0;               // feature 0's number in the whole product, a multiple of 256
 };
 hipError_t run_fp8_linear(const Fp8LinearArgs& a, hipStream_t st);
 

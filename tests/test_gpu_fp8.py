@@ -317,8 +317,9 @@ def test_linear_past_32_bit_offsets(ee):
     for rows in (1, 20):
         y = ee.fp8_linear(x[:rows], xs[:rows], w, ws)
         assert (y[:, :-300] == 0).all()
-        # (the last 300 features' own call: their scales are all one number, so the block borders do not matter)
-        assert torch.equal(y[:, -300:], ee.fp8_linear(x[:rows], xs[:rows], part, ws[:3].contiguous()))
+        # (their scales are all one number, so the block borders do not matter)
+        want, err = _product64(x[:rows], xs[:rows], part, ws[:3], "bf16")
+        assert ((y[:, -300:].double() - want).abs() <= err + UBF * (want.abs() + err)).all()
     del w, y
     x, xs, w, ws = _operands(_gen(10), 40000, 16, 65536)
     y = ee.fp8_linear(x, xs, w, ws)
