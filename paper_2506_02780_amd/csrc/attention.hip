@@ -8,17 +8,22 @@
 //   * positions in chunks of 256 of four runs of 64 each, counted from position 0.
 //     A run's state is m = its largest score (times log2 e), l = sum 2^(s - m) and
 //     o = sum 2^(s - m) v, from nothing;
-//   * a chunk's state joins its runs, a row's result its chunks: each state times
-//     2^(m - M) for the largest m, added in a fixed order.
+//   * a chunk's state takes its runs' in one after another: m' = max(m, m_r),
+//     o' = fma(o_r, 2^(m_r - m'), o 2^(m - m')), l alike;
+//   * a row's result adds its chunks' states, each times 2^(m - M) for the largest m, in a
+//     fixed order.
 // Scores, weights, l and o are fp32.  The matrix instruction of a bf16 cache takes
 // the weights as two bf16 parts (p = hi + lo to 2^-17): as one they would add as much error as
 // the rounding of a bf16 result, and half the chip's matrix rate waits on the cache anyway.
 
 #include "operators.h"
 
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
+#include <array>
+#include <type_traits>
 
 #include "device.h"
 
@@ -155,7 +160,7 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 //     c EPV ... of every pass.  bf16 values are transposed in registers, 8
 //     positions by the dimensions of a piece; the output's lane (grp, c) then
 //     holds columns 4 grp + r, dimensions (pass, c EPV + e).
-// No operand passes through LDS.
+// Keys, values and weights never pass through LDS.
 template <int DT, int HD> struct AttGeo {
   static constexpr int ESZ = Geo<DT>::ESZ, EPL = Geo<DT>::EPL, KS = Geo<DT>::KS;
   static constexpr int NS = HD / KS;                         // fragments of a key
@@ -165,177 +170,290 @@ template <int DT, int HD> struct AttGeo {
   static constexpr int SP = VK * 4;                          // positions of a step
   static constexpr int STEPS = RUN / SP;
   static constexpr int ND = HD / 16;                         // output tiles
+  // Whether a wave's registers hold a run's keys and values beside the rest: the next
+  // run's are then requested as soon as this one's are used.
+  static constexpr bool AHEAD = HD * ESZ <= 256;
+  static constexpr int BUFFERS = HD <= 128 ? 2 : 1;          // of runs' states
+  using Piece = std::conditional_t<EPV * ESZ == 16, uint4, uint2>;
 };
+template <class P> __device__ __forceinline__ uint32_t word(const P& p, int i) { return __builtin_bit_cast(std::array<uint32_t, sizeof(P) / 4>, p)[i]; }
 
-template <int DT, int HD>
-__global__ __launch_bounds__(RUNS * 64) void attend_kernel(AttendArgs a) {
-  using G = AttGeo<DT, HD>;
-  constexpr int ESZ = G::ESZ;
-  const PagedCache& pc = a.c;
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
-  __shared__ float sm[RUNS][COLS], sl[RUNS][COLS];
-  __shared__ __attribute__((aligned(16))) float so[RUNS][COLS][HD];
 
-  // (heads first: workgroups are dealt to the eight XCDs in turn, and the tiles of a head then share one's L2)
-  int id = blockIdx.x;
-  const int h = id % a.Hkv; id /= a.Hkv;
-  const int ct = id % a.ctiles; id /= a.ctiles;
-  const int split = id % a.splits, b = id / a.splits;
-  const int cols = a.T * a.G, len = min(max(a.lens[b], 0), pc.max_pages * pc.page);
-  const int t_lo = ct * COLS / a.G, t_hi = min(ct * COLS + COLS - 1, cols - 1) / a.G;
-  const int e_lo = len - a.T + 1 + t_lo, e_hi = len - a.T + 1 + t_hi;   // ends of the tile's rows
-  const int start = a.window ? max(0, e_lo - a.window) : 0;
-  if (e_hi <= 0) return;
-  const int ncol = min(COLS, cols - ct * COLS);
-  const int col = min(ct * COLS + c, cols - 1), t = col / a.G;          // (columns past the last repeat it)
-  const int end = len - a.T + 1 + t, first = a.window ? max(0, end - a.window) : 0;
+// A state takes in a later run's.
+__device__ __forceinline__ float join_scale(float m, float M) { return M == -INFINITY ? 1.f : exp2_(m - M); }   // (of two empty ones: as they are)
 
-  uint4 qf[G::NS];
-  {
-    const uint8_t* q = (const uint8_t*)a.q + ((int64_t)(b * a.T + t) * a.ldq + (h * a.G + col % a.G) * HD) * ESZ + grp * 16;
-#pragma unroll
-    for (int s = 0; s < G::NS; ++s) qf[s] = *(const uint4*)(q + s * 64);
+// Longest sequences first, 64 at a time, so that short ones fill the gaps at the end (64
+// sequences to 8192, 32 heads over 8 of 128: 228 us, 274 in their own order): the i-th to be taken.
+__device__ __forceinline__ int by_length(const int* lens, int B, int i, int lane) {
+  if (B == 1) return 0;
+  const int b64 = i & ~63, n = min(64, B - b64), own = lane < n ? lens[b64 + lane] : INT_MIN;
+  int rank = 0;
+  for (int j = 0; j < n; ++j) {
+    const int other = __builtin_amdgcn_readlane(own, j);
+    rank += other > own || (other == own && j < lane);
   }
-  const int* table = pc.tables + b * pc.ldt;
-  const int ch1 = (e_hi + CHUNK - 1) / CHUNK;
-  for (int ch = start / CHUNK + split; ch < ch1; ch += a.splits) {
-    const int base = ch * CHUNK + wv * RUN;
-    f32x4 o[G::ND];
-#pragma unroll
-    for (int i = 0; i < G::ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    if (base < e_hi && base + RUN > start) {
-      // pages of the run's four 16-position tiles
-      __amdgpu_buffer_rsrc_t kr[4], vr[4];
-      bool there[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p0 = base + 16 * i, pg = p0 / pc.page;
-        there[i] = p0 < e_hi && p0 + 16 > start;
-        int page = there[i] ? table[pg] : -1;
-        page = __builtin_amdgcn_readfirstlane(page);
-        there[i] = page >= 0 && page < pc.n_pages;
-        const int64_t pb = there[i] ? page : 0, at = p0 - pg * pc.page;
-        kr[i] = make_rsrc((const uint8_t*)pc.k + (pb * pc.kp + at * pc.ks + h * pc.kh) * ESZ, there[i] ? 0x7fffffffu : 0u);
-        vr[i] = make_rsrc((const uint8_t*)pc.v + (pb * pc.vp + at * pc.vs + h * pc.vh) * ESZ, there[i] ? 0x7fffffffu : 0u);
-      }
-      f32x4 s[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const unsigned off = (unsigned)(c * (int)pc.ks * ESZ + grp * 16);
-#pragma unroll
-        for (int f = 0; f < G::NS; ++f) s[i] = mma<DT>(bload<0>(kr[i], off + f * 64), qf[f], s[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int p = base + 16 * i + 4 * grp + r;
-          s[i][r] = there[i] && p < end && p >= first ? s[i][r] * a.scale_log2 : -INFINITY;
-          m = fmaxf(m, s[i][r]);
-        }
-      m = xmax32(xmax16(m));
-      const float mu = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[i][r] = exp2_(s[i][r] - mu);
-          l += s[i][r];
-        }
-      l = xsum32(xsum16(l));
+  return b64 + __ffsll(__ballot(lane < n && rank == (i & 63))) - 1;
+}
 
-      // o += weights x values of the positions in [from, to), for a lane's columns
-      auto values = [&](int from, int to, f32x4 (&acc)[G::ND]) {
+// What a wave streams: the pages, keys and values of runs of one KV head.
+template <int DT, int HD> struct Stream {
+  using G = AttGeo<DT, HD>;
+  static constexpr int ESZ = G::ESZ;
+  const PagedCache& pc;
+  const int* table;
+  const uint8_t *kh, *vh;   // the head's
+  uint64_t page_mul;
+  int start, e_hi;          // positions that some row sees
+  int lane, c, grp;
+  int entries, entry0, entry_step;
+  // Pages of a run's four 16-position tiles, -1 where there is none or no row sees it: lane
+  // 4 i + j holds that of tile j of the run i turns on, for sixteen turns.  (As loads by
+  // the whole wave in the loop they waited for the keys and values before them.)
+  struct Pages {
+    int page[4], at[4];
+  };
+  uint4 k[4][G::NS];
+  typename G::Piece v[G::STEPS][G::NP][G::VK];
+
+  __device__ __forceinline__ int page_of(int p0) const { return (int)(((uint64_t)(uint32_t)(p0 >> 4) * page_mul) >> 38); }
+  // Turns are `step` positions apart, the first at p.
+  __device__ __forceinline__ void entries_load(int64_t p, int64_t step, int inner, int64_t inner_step) {
+    const int turn = lane >> 2;
+    const int64_t p0 = p + turn / inner * step + turn % inner * inner_step + 16 * (lane & 3);
+    entries = p0 < (int64_t)pc.max_pages * pc.page ? table[page_of((int)p0)] : -1;
+    asm volatile("" : "+v"(entries));   // (waited for here, not wherever they are used)
+  }
+  __device__ __forceinline__ Pages pages(int turn, int base) const {
+    Pages p;
 #pragma unroll
-        for (int st = 0; st < G::STEPS; ++st) {
-          uint4 hi, lo;
-          if constexpr (DT == DT_BF16) {
-            uint32_t u[4], w[4];
+    for (int i = 0; i < 4; ++i) {
+      const int p0 = base + 16 * i, page = __builtin_amdgcn_readlane(entries, turn * 4 + i);
+      p.page[i] = page >= 0 && page < pc.n_pages && p0 < e_hi && p0 + 16 > start ? page : -1;
+      p.at[i] = p0 - page_of(p0) * pc.page;
+    }
+    return p;
+  }
+  __device__ __forceinline__ void load_k(const Pages& p) {
+    const unsigned off = (unsigned)(c * (int)pc.ks * ESZ + grp * 16);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float x = s[2 * st + (j >> 1)][2 * (j & 1)], y = s[2 * st + (j >> 1)][2 * (j & 1) + 1];
-              u[j] = bf16x2_bits(x, y);
-              w[j] = bf16x2_bits(x - bf2f(u[j] & 0xffffu), y - __uint_as_float(u[j] & 0xffff0000u));
-            }
-            hi = make_uint4(u[0], u[1], u[2], u[3]);
-            lo = make_uint4(w[0], w[1], w[2], w[3]);
-          } else {
-            hi = make_uint4(__float_as_uint(s[st][0]), __float_as_uint(s[st][1]), __float_as_uint(s[st][2]), __float_as_uint(s[st][3]));
-          }
-          // slot j of lane group grp: position 4 grp + j of the step's first tile, then of its second
-          unsigned off[G::VK];
+    for (int i = 0; i < 4; ++i) {
+      const auto r = make_rsrc(kh + (max(p.page[i], 0) * pc.kp + p.at[i] * pc.ks) * ESZ, p.page[i] >= 0 ? 0x7fffffffu : 0u);
 #pragma unroll
-          for (int j = 0; j < G::VK; ++j) {
-            const int p = base + st * G::SP + 16 * (j >> 2) + 4 * grp + (j & 3);
-            off[j] = p >= from && p < to ? (unsigned)((4 * grp + (j & 3)) * (int)pc.vs * ESZ + c * G::EPV * ESZ) : OOB;
-          }
+      for (int f = 0; f < G::NS; ++f) k[i][f] = bload<0>(r, off + f * 64);
+    }
+  }
+  // Values of a lane's positions; zeros where no row sees the position (what its slot holds may
+  // be no number): past the last one by the range of the tile, before the first by the offset.
+  __device__ __forceinline__ void load_v(const Pages& p, int base) {
+    const unsigned slot = (unsigned)((int)pc.vs * ESZ);
 #pragma unroll
-          for (int np = 0; np < G::NP; ++np) {
-            if constexpr (DT == DT_F32) {
-              uint4 v[4];
+    for (int tile = 0; tile < 4; ++tile) {
+      const unsigned last = (unsigned)min(e_hi - (base + 16 * tile), 16) - 1u;
+      const auto r = make_rsrc(vh + (max(p.page[tile], 0) * pc.vp + p.at[tile] * pc.vs) * ESZ, p.page[tile] >= 0 ? last * slot + HD * ESZ : 0u);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) v[j] = bload<0>(vr[st], off[j] + np * 256);
-              acc[np * 4 + 0] = mma<DT>(hi, make_uint4(v[0].x, v[1].x, v[2].x, v[3].x), acc[np * 4 + 0]);
-              acc[np * 4 + 1] = mma<DT>(hi, make_uint4(v[0].y, v[1].y, v[2].y, v[3].y), acc[np * 4 + 1]);
-              acc[np * 4 + 2] = mma<DT>(hi, make_uint4(v[0].z, v[1].z, v[2].z, v[3].z), acc[np * 4 + 2]);
-              acc[np * 4 + 3] = mma<DT>(hi, make_uint4(v[0].w, v[1].w, v[2].w, v[3].w), acc[np * 4 + 3]);
-            } else {
-              uint32_t v[8][4];
+      for (int i = 0; i < 4; ++i) {
+        // slot j of lane group grp: position 4 grp + j of the step's first tile, then of its second
+        const int st = tile / (G::SP / 16), j = tile % (G::SP / 16) * 4 + i;
+        const unsigned off = ((4 * grp + i) * slot + c * G::EPV * ESZ) | ((unsigned)(base - start + 16 * tile + i + 4 * grp) & OOB);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const auto& r = vr[2 * st + (j >> 2)];
-                if constexpr (G::EPV == 8) {
-                  const uint4 x = bload<0>(r, off[j] + np * 256);
-                  v[j][0] = x.x; v[j][1] = x.y; v[j][2] = x.z; v[j][3] = x.w;
-                } else {
-                  const uint2 x = bload64<0>(r, off[j]);
-                  v[j][0] = x.x; v[j][1] = x.y;
-                }
-              }
-#pragma unroll
-              for (int w = 0; w < G::EPV / 2; ++w) {
-                uint32_t even[4], odd[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  even[j] = __builtin_amdgcn_perm(v[2 * j + 1][w], v[2 * j][w], 0x05040100u);
-                  odd[j] = __builtin_amdgcn_perm(v[2 * j + 1][w], v[2 * j][w], 0x07060302u);
-                }
-                const uint4 ve = make_uint4(even[0], even[1], even[2], even[3]), vo = make_uint4(odd[0], odd[1], odd[2], odd[3]);
-                const int d = np * G::EPV + 2 * w;
-                acc[d] = mma<DT>(hi, ve, acc[d]);
-                acc[d] = mma<DT>(lo, ve, acc[d]);
-                acc[d + 1] = mma<DT>(hi, vo, acc[d + 1]);
-                acc[d + 1] = mma<DT>(lo, vo, acc[d + 1]);
-              }
-            }
-          }
-        }
-      };
-      // Where some row does not see what another does, a value that it does not see
-      // may be no number, and its weight of 0 would not remove it: row by row, with the others' values zeroed.
-      if (a.T > 1 && (base + RUN > e_lo || (a.window && base < e_hi - a.window))) {
-        for (int tt = t_lo; tt <= t_hi; ++tt) {
-          const int e = len - a.T + 1 + tt;
-          f32x4 one[G::ND];
-#pragma unroll
-          for (int i = 0; i < G::ND; ++i) one[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-          values(a.window ? max(0, e - a.window) : 0, e, one);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if ((ct * COLS + 4 * grp + r) / a.G == tt)
-#pragma unroll
-              for (int i = 0; i < G::ND; ++i) o[i][r] = one[i][r];
-        }
-      } else {
-        values(start, e_hi, o);
+        for (int np = 0; np < G::NP; ++np)
+          if constexpr (G::EPV * ESZ == 16) v[st][np][j] = bload<0>(r, off + np * 256);
+          else v[st][np][j] = bload64<0>(r, off);
       }
     }
-    if (grp == 0) {
-      sm[wv][c] = m;
-      sl[wv][c] = l;
+  }
+  // Scores of a lane's column, as weights: m, l and s = 2^(s - m).
+  __device__ __forceinline__ void scores(const uint4 (&q)[G::NS], f32x4 (&s)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int f = 0; f < G::NS; ++f) s[i] = mma<DT>(k[i][f], q[f], s[i]);
     }
+  }
+  // whole: every column sees the run.
+  __device__ __forceinline__ void weights(const Pages& p, int base, int first, int end, bool whole, float scale, f32x4 (&s)[4], float& m, float& l) const {
+    m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[i][r] *= scale;
+    if (!whole || (p.page[0] | p.page[1] | p.page[2] | p.page[3]) < 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int pos = base + 16 * i + 4 * grp + r;
+          if (!(p.page[i] >= 0 && pos < end && pos >= first)) s[i][r] = -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) m = fmaxf(m, s[i][r]);
+    m = xmax32(xmax16(m));
+    const float mu = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[i][r] = exp2_(s[i][r] - mu);
+        l += s[i][r];
+      }
+    l = xsum32(xsum16(l));
+  }
+  // Operand word j of dimension d: a pair of positions, from pairs of dimensions of one position.
+  __device__ __forceinline__ uint32_t turned(int st, int d, int j) const {
+    if constexpr (DT == DT_F32) {
+      return word(v[st][d / 4][j], d % 4);
+    } else {
+      const int np = d / G::EPV, w = d % G::EPV / 2;
+      const uint32_t x = word(v[st][np][2 * j], w), y = word(v[st][np][2 * j + 1], w);
+      return d & 1 ? __builtin_amdgcn_perm(y, x, 0x07060302u) : __builtin_amdgcn_perm(y, x, 0x05040100u);
+    }
+  }
+};
+// The weights of a step of V as an operand: bf16 in two parts.
+template <int DT> struct Weights {
+  uint4 hi, lo;
+};
+template <int DT> __device__ __forceinline__ Weights<DT> operand_weights(const f32x4 (&s)[4], int st) {
+  Weights<DT> w;
+  if constexpr (DT == DT_BF16) {
+    uint32_t u[4], v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x = s[2 * st + (j >> 1)][2 * (j & 1)], y = s[2 * st + (j >> 1)][2 * (j & 1) + 1];
+      u[j] = bf16x2_bits(x, y);
+      v[j] = bf16x2_bits(x - bf2f(u[j] & 0xffffu), y - __uint_as_float(u[j] & 0xffff0000u));
+    }
+    w.hi = make_uint4(u[0], u[1], u[2], u[3]);
+    w.lo = make_uint4(v[0], v[1], v[2], v[3]);
+  } else {
+    w.hi = __builtin_bit_cast(uint4, s[st]);
+  }
+  return w;
+}
+// acc[d] += weights x values of a step, x(d) the values of dimension tile d.  (A tile's two
+// parts apart, so that neither waits for the other.)
+template <int DT, int ND, class X> __device__ __forceinline__ void weigh(const Weights<DT>& w, X x, f32x4 (&acc)[ND]) {
+#pragma unroll
+  for (int d0 = 0; d0 < ND; d0 += 4) {
+    uint4 y[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) y[d] = x(d0 + d);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) acc[d0 + d] = mma<DT>(w.hi, y[d], acc[d0 + d]);
+    if constexpr (DT == DT_BF16)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) acc[d0 + d] = mma<DT>(w.lo, y[d], acc[d0 + d]);
+  }
+}
+
+// One row per sequence.  What bounds it is the cache's stream (64 sequences up to 8192, 32
+// heads over 8 of 128: 1.07 GB): a wave takes a KV head's chunks split, split + splits, ...
+// of a sequence, run after run, and requests the next run's keys and values as soon
+// as this one's are used.  The waves of a workgroup take a sequence's heads side by side, which
+// stand next to each other where a position's heads do (read so 6.2 TB/s, a head per
+// workgroup 5.5), and wait for nothing of each other.
+// (Four waves with all of a SIMD's registers each where a run's keys and values take more.)
+template <int DT, int HD> constexpr int stream_waves() { return AttGeo<DT, HD>::AHEAD ? 8 : 4; }
+template <int DT, int HD>
+__global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD>() / 4)) void attend_stream_kernel(AttendArgs a) {
+  using G = AttGeo<DT, HD>;
+  constexpr int ESZ = G::ESZ, STREAM_WAVES = stream_waves<DT, HD>();
+  __shared__ uint4 sq[STREAM_WAVES][G::NS][64];   // the queries' fragments
+  const PagedCache& pc = a.c;
+  const int lane = threadIdx.x & 63, c = lane & 15, grp = lane >> 4;
+  const int unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x * STREAM_WAVES + (int)(threadIdx.x >> 6));
+  const int per = a.Hkv * a.cgroups, share = unit / per, h = unit % per / a.cgroups, ct = unit % a.cgroups;
+  if (share >= a.splits * a.B) return;
+  const int split = share % a.splits, b = by_length(a.lens, a.B, share / a.splits, lane);
+  const int len = min(max(a.lens[b], 0), pc.max_pages * pc.page), start = a.window ? max(0, len - a.window) : 0;
+  const int ch1 = (len + CHUNK - 1) / CHUNK;
+  int ch = start / CHUNK + split, run0 = 0, runs = RUNS;
+  // Few chunks for the waves that share them (tables much wider than the sequence): a run each, joined
+  // by what reads the states (a sequence of 2048 in tables for 65536: 14 us, 27.5 by chunks).
+  if (ch1 - start / CHUNK <= a.apart) {
+    ch = start / CHUNK + split / RUNS;
+    run0 = split % RUNS;
+    runs = 1;
+  }
+  if (ch >= ch1) return;
+  const int ncol = min(COLS, a.G - ct * COLS), col = min(ct * COLS + c, a.G - 1);   // (columns past the last repeat it)
+
+  uint4 (&qs)[G::NS][64] = sq[threadIdx.x >> 6];   // (the wave's own: no barrier)
+  const uint8_t* qp = (const uint8_t*)a.q + ((int64_t)b * a.ldq + (h * a.G + col) * HD) * ESZ + grp * 16;
+#pragma unroll
+  for (int f = 0; f < G::NS; ++f) qs[f][lane] = *(const uint4*)(qp + f * 64);
+  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, len, lane, c, grp};
+  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK, (int64_t)a.splits * CHUNK, RUNS, RUN); };   // of four chunks
+  entries(ch);
+  int ahead = 0;   // chunks on since then
+  typename Stream<DT, HD>::Pages now = x.pages(run0, ch * CHUNK + run0 * RUN), next;
+  if constexpr (G::AHEAD) {
+    x.load_k(now);
+    x.load_v(now, ch * CHUNK + run0 * RUN);
+  }
+  for (; ch < ch1; ch += a.splits) {
+    f32x4 o[G::ND];
+    float m = -INFINITY, l = 0.f;
+    for (int run = run0; run < run0 + runs; ++run) {
+      const int base = ch * CHUNK + run * RUN;
+      if constexpr (!G::AHEAD) {
+        x.load_k(now);
+        x.load_v(now, base);
+      }
+      // (past the last chunk there are no pages, and requests read nothing: a condition
+      // around them would make the compiler wait for more than the oldest)
+      int after = base + RUN;
+      if (run == run0 + runs - 1) {
+        after = (ch + a.splits) * CHUNK;
+        if (++ahead == 4) {
+          entries(ch + a.splits);
+          ahead = 0;
+        }
+      }
+      next = x.pages(ahead * RUNS + (run + 1) % RUNS, after);
+      f32x4 s[4];
+      {
+        uint4 q[G::NS];
+#pragma unroll
+        for (int f = 0; f < G::NS; ++f) q[f] = qs[f][lane];
+        x.scores(q, s);
+      }
+      if constexpr (G::AHEAD) x.load_k(next);
+      float mr, lr;
+      x.weights(now, base, start, len, base >= start && base + RUN <= len, a.scale_log2, s, mr, lr);
+      f32x4 one[G::ND];
+#pragma unroll
+      for (int i = 0; i < G::ND; ++i) one[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < G::STEPS; ++st)
+        weigh<DT>(operand_weights<DT>(s, st), [&](int d) { return make_uint4(x.turned(st, d, 0), x.turned(st, d, 1), x.turned(st, d, 2), x.turned(st, d, 3)); }, one);
+      if constexpr (G::AHEAD) x.load_v(next, after);
+      if (run == run0) {
+        m = mr;
+        l = lr;
+#pragma unroll
+        for (int i = 0; i < G::ND; ++i) o[i] = one[i];
+      } else {
+        // m, l and the scales belong to column c, the values to columns 4 grp + r
+        const float M = fmaxf(m, mr), fa = join_scale(m, M), fb = join_scale(mr, M);
+        l = fmaf(lr, fb, l * fa);
+        m = M;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float ra = __shfl(fa, 4 * grp + r), rb = __shfl(fb, 4 * grp + r);
+#pragma unroll
+          for (int i = 0; i < G::ND; ++i) o[i][r] = fmaf(one[i][r], rb, o[i][r] * ra);
+        }
+      }
+      now = next;
+    }
+    const int64_t state = ((int64_t)(b * a.ring + (runs == 1 ? split : ch % a.ring)) * a.Hkv + h) * a.G + ct * COLS;
+    if (grp == 0 && c < ncol) a.ml[state + c] = make_float2(m, l);
     // o[np EPV + e] of lane (grp, c): columns 4 grp + r, dimension np 16 EPV + c EPV + e
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -344,80 +462,340 @@ __global__ __launch_bounds__(RUNS * 64) void attend_kernel(AttendArgs a) {
         for (int np = 0; np < G::NP; ++np)
 #pragma unroll
           for (int e = 0; e < G::EPV; e += 4)
-            *(f32x4*)&so[wv][4 * grp + r][np * 16 * G::EPV + c * G::EPV + e] =
+            *(f32x4*)(a.o + (state + 4 * grp + r) * HD + np * 16 * G::EPV + c * G::EPV + e) =
                 f32x4{o[np * G::EPV + e][r], o[np * G::EPV + e + 1][r], o[np * G::EPV + e + 2][r], o[np * G::EPV + e + 3][r]};
-    __syncthreads();
-    for (int i = threadIdx.x; i < ncol * (HD / 4); i += RUNS * 64) {
-      const int q = i / (HD / 4), d = i % (HD / 4) * 4;
-      float M = sm[0][q];
-#pragma unroll
-      for (int w = 1; w < RUNS; ++w) M = fmaxf(M, sm[w][q]);
-      const float mu = M == -INFINITY ? 0.f : M;
-      float L = 0.f;
-      f32x4 O = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < RUNS; ++w) {
-        const float f = exp2_(sm[w][q] - mu);
-        L += f * sl[w][q];
-        const f32x4 x = *(const f32x4*)&so[w][q][d];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) O[e] += f * x[e];
-      }
-      const int64_t state = ((int64_t)(b * a.ring + ch % a.ring) * a.Hkv + h) * cols + ct * COLS + q;
-      *(f32x4*)(a.o + state * HD + d) = O;
-      if (d == 0) a.ml[state] = make_float2(M, L);
-    }
-    __syncthreads();
   }
 }
 
-// Joins a row's chunks: workgroup (row, head), groups of HD / 4 threads take every
-// NG-th chunk from the row's first on, then the groups in order.
-constexpr int JOIN_THREADS = 256;
-template <int HD, int ODT>
-__global__ __launch_bounds__(JOIN_THREADS) void attend_join_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4, NG = JOIN_THREADS / LPS;
-  __shared__ float sM[JOIN_THREADS / 64], sL[NG];
-  __shared__ __attribute__((aligned(16))) float sO[NG][HD];
-  const int row = blockIdx.x / a.H, head = blockIdx.x % a.H, b = row / a.T, t = row % a.T, h = head / a.G;
+// Several rows per sequence, or one where there are few chunks (8 KV heads of 128, one row of a
+// sequence of 8192: 18 us so, 33 by the waves above; of 32768 39 and 44; of 65536 68 and
+// 63).  The four waves of a workgroup take the runs of a chunk, whose states they
+// join through LDS, and keep its keys and values in registers for all of the workgroup's
+// column tiles: read anew for each, 33 rows of 4 sequences to 4096 took 88 us, so 58.
+constexpr int att_tiles(int row_bytes) { return std::max(1, 32768 / (COLS * row_bytes)); }   // whose queries LDS holds
+template <int DT, int HD>
+__global__ __launch_bounds__(RUNS * 64, 1) void attend_rows_kernel(AttendArgs a) {
+  using G = AttGeo<DT, HD>;
+  constexpr int ESZ = G::ESZ;
+  const PagedCache& pc = a.c;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
+  __shared__ float sm[G::BUFFERS][RUNS][COLS], sl[G::BUFFERS][RUNS][COLS];
+  __shared__ __attribute__((aligned(16))) float so[G::BUFFERS][RUNS][COLS][HD];
+  __shared__ uint4 sq[att_tiles(HD * ESZ)][G::NS][64];   // the queries' fragments
+
+  // Workgroups are dealt to the eight XCDs in turn: all heads and column tiles of a share of a
+  // sequence's length go to one, whose L2 then has what several ask for.
+  const int per = a.Hkv * a.cgroups, turn = (int)(blockIdx.x >> 3);
+  const int share = turn / per * 8 + (int)(blockIdx.x & 7), h = turn % per / a.cgroups, cg = turn % a.cgroups;
+  if (share >= a.splits * a.B) return;
+  const int split = share % a.splits, b = by_length(a.lens, a.B, share / a.splits, lane);
+  const int cols = a.T * a.G, len = min(max(a.lens[b], 0), pc.max_pages * pc.page);
+  const int ct0 = cg * a.ctw, ct1 = min(ct0 + a.ctw, (cols + COLS - 1) / COLS);   // column tiles
+  const int before = len - a.T + 1;                                              // the end of row 0
+  const int e_lo = before + ct0 * COLS / a.G, e_hi = before + (min(ct1 * COLS, cols) - 1) / a.G;   // of the first and last row
+  if (e_hi <= 0) return;
+  const int start = a.window ? max(0, e_lo - a.window) : 0;
+  const int ch1 = (e_hi + CHUNK - 1) / CHUNK;
+  int ch = start / CHUNK + split;
+  if (ch >= ch1) return;
+
+  for (int i = wv; i < (ct1 - ct0) * G::NS; i += RUNS) {
+    const int ct = i / G::NS, f = i % G::NS, col = min((ct0 + ct) * COLS + c, cols - 1);   // (columns past the last repeat it)
+    sq[ct][f][lane] = *(const uint4*)((const uint8_t*)a.q + ((int64_t)(b * a.T + col / a.G) * a.ldq + (h * a.G + col % a.G) * HD) * ESZ + grp * 16 + f * 64);
+  }
+  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, e_hi, lane, c, grp};
+  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK + wv * RUN, (int64_t)a.splits * CHUNK, 1, 0); };
+  entries(ch);
+  int ahead = 0;
+  typename Stream<DT, HD>::Pages now = x.pages(0, ch * CHUNK + wv * RUN), next;
+  x.load_k(now);
+  x.load_v(now, ch * CHUNK + wv * RUN);
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  barrier_only();
+  int buf = 0;
+  for (; ch < ch1; ch += a.splits) {
+    const int base = ch * CHUNK + wv * RUN, after = base + a.splits * CHUNK;
+    // (past the last chunk there are no pages, and requests read nothing)
+    if (++ahead == 16) {
+      entries(ch + a.splits);
+      ahead = 0;
+    }
+    next = x.pages(ahead, after);
+    // The values turned once for all tiles; their registers take the next run's.
+    uint32_t vt[G::STEPS][G::ND][4];
+#pragma unroll
+    for (int st = 0; st < G::STEPS; ++st)
+#pragma unroll
+      for (int d = 0; d < G::ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vt[st][d][j] = x.turned(st, d, j);
+    if constexpr (G::AHEAD) x.load_v(next, after);
+    // Where some row does not see what another does, and a value there is no finite number, its
+    // weight of 0 would not remove it: row by row then.
+    const bool whole = base + RUN <= e_lo && base >= (a.window ? max(0, e_hi - a.window) : 0);
+    bool mixed = a.T > 1 && !whole;
+    if (mixed) {
+      bool odd = false;
+#pragma unroll
+      for (int st = 0; st < G::STEPS; ++st)
+#pragma unroll
+        for (int d = 0; d < G::ND; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t y = vt[st][d][j];
+            if constexpr (DT == DT_BF16) odd |= (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u;
+            else odd |= (y & 0x7f800000u) == 0x7f800000u;
+          }
+      mixed = __ballot(odd) != 0;
+    }
+    for (int ct = ct0; ct < ct1; ++ct, buf ^= G::BUFFERS - 1) {
+      const int ncol = min(COLS, cols - ct * COLS), t = min(ct * COLS + c, cols - 1) / a.G;
+      const int end = before + t, first = a.window ? max(0, end - a.window) : 0;
+      uint4 q[G::NS];
+#pragma unroll
+      for (int f = 0; f < G::NS; ++f) q[f] = sq[ct - ct0][f][lane];
+      f32x4 s[4];
+      x.scores(q, s);
+      float m, l;
+      x.weights(now, base, first, end, whole, a.scale_log2, s, m, l);
+      f32x4 o[G::ND];
+#pragma unroll
+      for (int i = 0; i < G::ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (!mixed) {
+#pragma unroll
+        for (int st = 0; st < G::STEPS; ++st)
+          weigh<DT>(operand_weights<DT>(s, st), [&](int d) { return make_uint4(vt[st][d][0], vt[st][d][1], vt[st][d][2], vt[st][d][3]); }, o);
+      } else {
+        const int t_lo = ct * COLS / a.G, t_hi = (ct * COLS + ncol - 1) / a.G;
+        for (int tt = t_lo; tt <= t_hi; ++tt) {
+          const int to = before + tt, from = a.window ? max(0, to - a.window) : 0;
+#pragma unroll
+          for (int d = 0; d < G::ND; ++d) {
+            f32x4 one = {0.f, 0.f, 0.f, 0.f};   // (a tile's parts in the order of weigh)
+#pragma unroll
+            for (int st = 0; st < G::STEPS; ++st) {
+              const Weights<DT> w = operand_weights<DT>(s, st);
+              uint32_t y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                auto in = [&](int i) {
+                  const int p = base + st * G::SP + 16 * (i >> 2) + 4 * grp + (i & 3);
+                  return p >= from && p < to;
+                };
+                if constexpr (DT == DT_BF16) y[j] = vt[st][d][j] & ((in(2 * j) ? 0xffffu : 0u) | (in(2 * j + 1) ? 0xffff0000u : 0u));
+                else y[j] = in(j) ? vt[st][d][j] : 0u;
+              }
+              one = mma<DT>(w.hi, make_uint4(y[0], y[1], y[2], y[3]), one);
+              if constexpr (DT == DT_BF16) one = mma<DT>(w.lo, make_uint4(y[0], y[1], y[2], y[3]), one);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if ((ct * COLS + 4 * grp + r) / a.G == tt) o[d][r] = one[r];
+          }
+        }
+      }
+      if (grp == 0) {
+        sm[buf][wv][c] = m;
+        sl[buf][wv][c] = l;
+      }
+      // o[np EPV + e] of lane (grp, c): columns 4 grp + r, dimension np 16 EPV + c EPV + e
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * grp + r < ncol)
+#pragma unroll
+          for (int np = 0; np < G::NP; ++np)
+#pragma unroll
+            for (int e = 0; e < G::EPV; e += 4)
+              *(f32x4*)&so[buf][wv][4 * grp + r][np * 16 * G::EPV + c * G::EPV + e] =
+                  f32x4{o[np * G::EPV + e][r], o[np * G::EPV + e + 1][r], o[np * G::EPV + e + 2][r], o[np * G::EPV + e + 3][r]};
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+      barrier_only();                       // (the next run's requests go on)
+      for (int i = threadIdx.x; i < ncol * (HD / 4); i += RUNS * 64) {
+        const int y = i / (HD / 4), d = i % (HD / 4) * 4;
+        float M = sm[buf][0][y], L = sl[buf][0][y];
+        f32x4 O = *(const f32x4*)&so[buf][0][y][d];
+#pragma unroll
+        for (int w = 1; w < RUNS; ++w) {
+          const float mw = sm[buf][w][y], N = fmaxf(M, mw), fa = join_scale(M, N), fb = join_scale(mw, N);
+          L = fmaf(sl[buf][w][y], fb, L * fa);
+          M = N;
+          const f32x4 z = *(const f32x4*)&so[buf][w][y][d];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) O[e] = fmaf(z[e], fb, O[e] * fa);
+        }
+        const int64_t state = ((int64_t)(b * a.ring + ch % a.ring) * a.Hkv + h) * cols + ct * COLS + y;
+        *(f32x4*)(a.o + state * HD + d) = O;
+        if (d == 0) a.ml[state] = make_float2(M, L);
+      }
+      if constexpr (G::BUFFERS == 1) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        barrier_only();
+      }
+    }
+    x.load_k(next);
+    if constexpr (!G::AHEAD) x.load_v(next, after);
+    now = next;
+  }
+}
+
+// Joins a row's chunks, each times 2^(m - M): the j-th from the row's first on is added to sum
+// j % JOIN_GROUPS, then the sums in order.  HD / 4 lanes hold a sum.
+constexpr int JOIN_GROUPS = 32;
+// The row and head that a sum's lanes are for.
+struct Joined {
+  int64_t row;
+  int head, c0, n;      // its first chunk and their number
+  int64_t state0, step; // of the states of chunk 0 of the ring, and between chunks
+};
+__device__ __forceinline__ Joined joined(const AttendArgs& a, int64_t item) {
+  Joined j;
+  j.row = item / a.H;
+  j.head = (int)(item % a.H);
+  const int b = (int)(j.row / a.T), t = (int)(j.row % a.T);
   const int len = min(max(a.lens[b], 0), a.c.max_pages * a.c.page), end = len - a.T + 1 + t;
-  const int c0 = (a.window ? max(0, end - a.window) : 0) / CHUNK, c1 = end > 0 ? (end + CHUNK - 1) / CHUNK : c0;
-  const int cols = a.T * a.G, col = t * a.G + head % a.G;
-  auto state = [&](int ch) { return ((int64_t)(b * a.ring + ch % a.ring) * a.Hkv + h) * cols + col; };
-  float M = -INFINITY;
-  for (int ch = c0 + threadIdx.x; ch < c1; ch += JOIN_THREADS) M = fmaxf(M, a.ml[state(ch)].x);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-  if ((threadIdx.x & 63) == 0) sM[threadIdx.x >> 6] = M;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < JOIN_THREADS / 64; ++i) M = fmaxf(M, sM[i]);
-  const float mu = M == -INFINITY ? 0.f : M;
-  const int g = threadIdx.x / LPS, d = threadIdx.x % LPS * 4;
-  float L = 0.f;
-  f32x4 O = {0.f, 0.f, 0.f, 0.f};
-  for (int ch = c0 + g; ch < c1; ch += NG) {
-    const int64_t s = state(ch);
-    const float2 ml = a.ml[s];
-    const f32x4 x = *(const f32x4*)(a.o + s * HD + d);
-    const float f = exp2_(ml.x - mu);
-    L += f * ml.y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) O[e] += f * x[e];
-  }
-  *(f32x4*)&sO[g][d] = O;
-  if (d == 0) sL[g] = L;
-  __syncthreads();
-  if (g) return;
-#pragma unroll
-  for (int i = 1; i < NG; ++i) {
-    L += sL[i];
-    O += *(const f32x4*)&sO[i][d];
-  }
+  j.c0 = (a.window ? max(0, end - a.window) : 0) / CHUNK;
+  j.n = end > 0 ? (end + CHUNK - 1) / CHUNK - j.c0 : 0;
+  j.step = (int64_t)a.T * a.H;
+  j.state0 = (int64_t)b * a.ring * j.step + (int64_t)(j.head / a.G) * a.T * a.G + t * a.G + j.head % a.G;
+  return j;
+}
+template <int HD, int ODT>
+__device__ __forceinline__ void join_store(const AttendArgs& a, const Joined& j, int d, float M, float l, f32x4 o) {
   // (no position, or none with a score above -inf: zeros)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) store_elt<ODT>(a.out, (size_t)row * a.ldo + head * HD + d + e, L == 0.f ? 0.f : O[e] / L);
-  if (a.lse && d == 0) a.lse[(size_t)row * a.H + head] = L == 0.f ? -INFINITY : 0.69314718055994531f * (M + log2f(L));
+  for (int e = 0; e < 4; ++e) o[e] = l == 0.f ? 0.f : o[e] / l;
+  const size_t at = (size_t)j.row * a.ldo + j.head * HD + d;
+  if (((a.ldo & 3) | (reinterpret_cast<uintptr_t>(a.out) & (ODT == DT_BF16 ? 7 : 15))) == 0) {
+    if constexpr (ODT == DT_BF16) *(uint2*)((uint16_t*)a.out + at) = make_uint2(f2bf_bits(o[0]) | f2bf_bits(o[1]) << 16, f2bf_bits(o[2]) | f2bf_bits(o[3]) << 16);
+    else *(f32x4*)((float*)a.out + at) = o;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) store_elt<ODT>(a.out, at + e, o[e]);
+  }
+  if (a.lse && d == 0) a.lse[(size_t)j.row * a.H + j.head] = l == 0.f ? -INFINITY : 0.69314718055994531f * (M + log2f(l));
+}
+
+// A product that no addition takes in (its rounding is part of the sums above).
+__device__ __forceinline__ float product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
+// Four states at a time, of one chunk's runs where those are apart: joined as in the kernels above.
+__device__ __forceinline__ void join_runs(float2* ml, f32x4* x) {
+#pragma unroll
+  for (int r = 1; r < RUNS; ++r) {
+    const float M = fmaxf(ml[0].x, ml[r].x), fa = join_scale(ml[0].x, M), fb = join_scale(ml[r].x, M);
+    ml[0] = make_float2(M, fmaf(ml[r].y, fb, ml[0].y * fa));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[0][e] = fmaf(x[r][e], fb, x[0][e] * fa);
+  }
+}
+
+// At most JOIN_GROUPS chunks are held: every sum is one chunk's state.
+template <int HD, int ODT>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+  constexpr int LPS = HD / 4, AT_ONCE = 8;
+  const int64_t item = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
+  if (item >= (int64_t)a.B * a.T * a.H) return;
+  const int at = threadIdx.x % LPS, d = at * 4;
+  const Joined j = joined(a, item);
+  const bool apart = j.n <= a.apart;
+  const int n = apart ? j.n * RUNS : j.n;
+  auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
+  float M = -INFINITY;
+  for (int i = at; i < n; i += LPS) M = fmaxf(M, a.ml[state(i)].x);
+#pragma unroll
+  for (int o = 1; o < LPS; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+  const float mu = M == -INFINITY ? 0.f : M;
+  float l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
+    float2 ml[AT_ONCE];
+    f32x4 x[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int64_t s = state(min(i0 + i, n - 1));
+      ml[i] = a.ml[s];
+      x[i] = *(const f32x4*)(a.o + s * HD + d);
+    }
+    if (apart)
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (i0 + i >= n || (apart && i % RUNS)) continue;
+      const float f = exp2_(ml[i].x - mu), fl = product(f, ml[i].y);
+      l = i0 + i ? l + fl : fl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y = product(f, x[i][e]);
+        o[e] = i0 + i ? o[e] + y : y;
+      }
+    }
+  }
+  join_store<HD, ODT>(a, j, d, M, l, o);
+}
+
+// More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us).
+template <int HD, int ODT>
+__global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
+  constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = RUNS;
+  __shared__ float sM[16], sL[JOIN_GROUPS];
+  __shared__ __attribute__((aligned(16))) float sO[JOIN_GROUPS][HD];
+  const int tid = threadIdx.x, set = tid / LPS, d = tid % LPS * 4;
+  const Joined j = joined(a, blockIdx.x);
+  const bool apart = j.n <= a.apart;
+  const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1, next = apart ? 1 : JOIN_GROUPS;   // states of a chunk; to the next at once
+  auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
+  float M = -INFINITY;
+  for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) sM[tid >> 6] = M;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) M = fmaxf(M, sM[i]);
+  const float mu = M == -INFINITY ? 0.f : M;
+  if (set < SETS)
+#pragma unroll
+    for (int p = 0; p < PER; ++p) {
+      const int g = set * PER + p;
+      float l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int i0 = g * per; i0 < n; i0 += AT_ONCE * JOIN_GROUPS) {   // (apart: of one chunk)
+        float2 ml[AT_ONCE];
+        f32x4 x[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int64_t s = state(min(i0 + i * next, n - 1));
+          ml[i] = a.ml[s];
+          x[i] = *(const f32x4*)(a.o + s * HD + d);
+        }
+        if (apart) join_runs(ml, x);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (i0 + i * next >= n || (apart && i)) continue;
+          const float f = exp2_(ml[i].x - mu);
+          l = fmaf(f, ml[i].y, l);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
+        }
+      }
+      *(f32x4*)&sO[g][d] = o;
+      if (d == 0) sL[g] = l;
+    }
+  __syncthreads();
+  if (set) return;
+  float l = sL[0];
+  f32x4 o = *(const f32x4*)&sO[0][d];
+  for (int i = 1; i < min(j.n, JOIN_GROUPS); ++i) {
+    l += sL[i];
+    const f32x4 y = *(const f32x4*)&sO[i][d];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += y[e];
+  }
+  join_store<HD, ODT>(a, j, d, M, l, o);
 }
 
 // Chunks whose states are held at once: a row's window reaches over that many.
@@ -431,6 +809,7 @@ size_t attend_workspace(int B, int T, int H, int hd, int64_t positions, int wind
   return (states * 8 + 255) / 256 * 256 + states * hd * 4;
 }
 
+constexpr int64_t STREAM_TARGET = 4096, ROWS_TARGET = 256;
 template <int DT, int HD, int ODT>
 static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   const int64_t positions = (int64_t)a.c.max_pages * a.c.page;
@@ -438,12 +817,36 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   const size_t states = (size_t)a.B * a.ring * a.T * a.H;
   a.ml = reinterpret_cast<float2*>(a.ws);
   a.o = reinterpret_cast<float*>(a.ws + (states * 8 + 255) / 256 * 256);
-  a.ctiles = (a.T * a.G + COLS - 1) / COLS;
-  a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, 4096 / ((int64_t)a.B * a.Hkv * a.ctiles)));
-  hipLaunchKernelGGL((attend_kernel<DT, HD>), dim3((unsigned)((int64_t)a.Hkv * a.ctiles * a.splits * a.B)), dim3(RUNS * 64), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attend_join_kernel<HD, ODT>), dim3((unsigned)((int64_t)a.B * a.T * a.H)), dim3(JOIN_THREADS), 0, st, a);
+  // (positions below 2^30 and pages of at most 2^16, in units of 16: the quotient is exact
+  // since 2^26 times the factor's error, less than 2^12, stays below 2^38)
+  a.page_mul = ((1ull << 38) + a.c.page / 16 - 1) / (a.c.page / 16);
+  const int ctiles = (a.T * a.G + COLS - 1) / COLS;
+  const int64_t heads = (int64_t)a.B * a.Hkv;
+  hipError_t e;
+  a.apart = 0;
+  if (a.T == 1 && heads * ctiles * a.ring > 1024) {
+    // Some 4096 waves, twice what the chip holds at once (64 sequences to 8192: 228 us; 2048
+    // waves 273, 6144 233).
+    a.cgroups = ctiles;
+    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, STREAM_TARGET / (heads * ctiles)));
+    a.apart = a.splits / RUNS;
+    const int64_t units = (int64_t)a.B * a.splits * a.Hkv * a.cgroups;
+    constexpr int waves = stream_waves<DT, HD>();
+    hipLaunchKernelGGL((attend_stream_kernel<DT, HD>), dim3((unsigned)((units + waves - 1) / waves)), dim3(waves * 64), 0, st, a);
+  } else {
+    // Splits of the length first, some 256 workgroups, then of the column tiles (33 rows of 4
+    // sequences to 4096: 59 us; 128 and 512 workgroups 68 and 66).
+    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, ROWS_TARGET / heads));
+    const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT));
+    a.cgroups = (int)std::min<int64_t>(ctiles, std::max<int64_t>(least, 512 / (heads * a.splits)));
+    a.ctw = (ctiles + a.cgroups - 1) / a.cgroups;
+    a.cgroups = (ctiles + a.ctw - 1) / a.ctw;
+    hipLaunchKernelGGL((attend_rows_kernel<DT, HD>), dim3((unsigned)(((int64_t)a.B * a.splits + 7) / 8 * 8 * a.Hkv * a.cgroups)), dim3(RUNS * 64), 0, st, a);
+  }
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
+  if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)items), dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((attend_join_kernel<HD, ODT>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

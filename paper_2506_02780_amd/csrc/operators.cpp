@@ -219,6 +219,7 @@ static const char* cache_memory(const ee_paged_cache& c, int32_t n_kv_heads, int
   if (!aligned(c.k, 16) || !aligned(c.v, 16)) return "the cache must be 16-byte aligned";
   for (int i = 0; i < 6; i += 3)
     if (strides[i + 1] * e * c.page_size >= int64_t(1) << 31) return "a head's slots of a page must lie within 2 GiB";
+  if (c.k_slot < head_dim || c.v_slot < head_dim) return "a head's slots must not share memory";
   if (!aligned(c.tables, 4) || c.ld < c.max_pages || c.ld >= int64_t(1) << 40) return "tables must be aligned to their type with a row stride of at least max_pages";
   return nullptr;
 }

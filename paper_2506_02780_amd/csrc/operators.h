@@ -114,7 +114,10 @@ struct AttendArgs {
   // (filled in by run_attend)
   float2* ml;           // [B][ring][Hkv][T G] largest score and sum of the chunks' states
   float* o;             // [..][hd] their weighted values
-  int ring, ctiles, splits;
+  int ring, splits;     // chunks held; workgroups that share a sequence's
+  int apart;            // up to so many chunks of a sequence, their runs' states are held instead
+  int cgroups, ctw;     // workgroups that share a head's column tiles, tiles of each
+  uint64_t page_mul;    // 2^38 / (page / 16), rounded up: divides positions by page
 };
 size_t attend_workspace(int B, int T, int H, int hd, int64_t positions, int window);
 hipError_t run_attend(const AttendArgs& a, hipStream_t st);

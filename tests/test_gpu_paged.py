@@ -409,6 +409,40 @@ def test_attend_does_not_depend_on_the_batch(ee):
     assert torch.equal(got, s["y"].repeat(70, 1))
 
 
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 256)])
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("lens,kv,capacity", [
+    ([0, 1, 64, 65, 256, 257, 5000], 2, 300_000),                      # short ones in wide tables: shared out by runs
+    ([1024, 700, 256, 257, 255, 0, 1] + [30] * 33, 8, 1024),           # some by runs, some by chunks
+    ([2048, 1700, 900, 300, 513, 0, 1, 256] + [5] * 56, 32, 2048),     # several chunks in turn
+    ([1300, 40], 3, 270_000),
+])
+def test_attend_shared_out_over_waves(ee, dtype, hd, window, lens, kv, capacity):
+    """Against float64, and bit for bit as alone with tables no wider than the sequence."""
+    s = _attend_case(ee, lens=lens, heads=2 * kv, kv=kv, hd=hd, dtype=dtype, window=window, most=capacity // 64, seed=kv)
+
+    def alone(tables, y):
+        for b in range(min(len(lens), 8)):
+            pages = max(1, -(-lens[b] // 64))
+            one = ee.paged_attention(s["q"][b:b + 1], s["k_cache"], s["v_cache"], tables[b:b + 1, :pages].contiguous(), s["lens"][b:b + 1],
+                                     window=window)
+            got = y[b:b + 1]
+            assert torch.equal(torch.isnan(one), torch.isnan(got)) and torch.equal(one[~torch.isnan(one)], got[~torch.isnan(got)]), b
+    alone(s["tables"], s["y"])
+    gone = s["tables"].clone()      # pages that are not there, and values of no number that all see
+    gone[:, 1::3] = -1
+    gone[-1, 0] = -1
+    s["v_cache"][int(s["tables"][0, 0]) if lens[0] else 0, 40] = float("inf")
+    alone(gone, ee.paged_attention(s["q"], s["k_cache"], s["v_cache"], gone, s["lens"], window=window))
+
+
+@pytest.mark.parametrize("heads,kv", [(20, 1), (33, 3)])
+def test_attend_many_heads_shared_out_over_waves(ee, heads, kv):
+    """More queries of a KV head than a tile has columns."""
+    _attend_case(ee, lens=[300, 1100, 0, 5], heads=heads, kv=kv, hd=128, most=300_000 // 64)
+    _attend_case(ee, lens=[300, 1100, 0, 5] + [3] * 300, heads=heads, kv=kv, hd=64, most=1100 // 16, page=16)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_long(ee, dtype):
     _attend_case(ee, lens=[70001, 3], heads=2, kv=1, hd=64, dtype=dtype, page=128, poison=False)
