@@ -173,7 +173,6 @@ template <int DT, int HD> struct AttGeo {
   // Whether a wave's registers hold a run's keys and values beside the rest: the next
   // run's are then requested as soon as this one's are used.
   static constexpr bool AHEAD = HD * ESZ <= 256;
-  static constexpr int BUFFERS = HD <= 128 ? 2 : 1;          // of runs' states
   using Piece = std::conditional_t<EPV * ESZ == 16, uint4, uint2>;
 };
 template <class P> __device__ __forceinline__ uint32_t word(const P& p, int i) { return __builtin_bit_cast(std::array<uint32_t, sizeof(P) / 4>, p)[i]; }
@@ -471,16 +470,19 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
 // sequence of 8192: 18 us so, 33 by the waves above; of 32768 39 and 44; of 65536 68 and
 // 63).  The four waves of a workgroup take the runs of a chunk, whose states they
 // join through LDS, and keep its keys and values in registers for all of the workgroup's
-// column tiles: read anew for each, 33 rows of 4 sequences to 4096 took 88 us, so 58.
+// column tiles: read anew for each, 33 rows of 4 sequences to 4096 took 88 us, so 59.
 constexpr int att_tiles(int row_bytes) { return std::max(1, 32768 / (COLS * row_bytes)); }   // whose queries LDS holds
-template <int DT, int HD>
-__global__ __launch_bounds__(RUNS * 64, 1) void attend_rows_kernel(AttendArgs a) {
+// For one column tile the next run's are requested ahead; for several, two workgroups share a
+// CU instead, each working while the other waits (33 rows 45 us; one row of 8192 20).
+template <int DT, int HD, bool SEVERAL>
+__global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   using G = AttGeo<DT, HD>;
-  constexpr int ESZ = G::ESZ;
+  constexpr int ESZ = G::ESZ, BUFFERS = SEVERAL || HD > 128 ? 1 : 2;   // of runs' states
+  constexpr bool AHEAD = G::AHEAD && !SEVERAL;
   const PagedCache& pc = a.c;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
-  __shared__ float sm[G::BUFFERS][RUNS][COLS], sl[G::BUFFERS][RUNS][COLS];
-  __shared__ __attribute__((aligned(16))) float so[G::BUFFERS][RUNS][COLS][HD];
+  __shared__ float sm[BUFFERS][RUNS][COLS], sl[BUFFERS][RUNS][COLS];
+  __shared__ __attribute__((aligned(16))) float so[BUFFERS][RUNS][COLS][HD];
   __shared__ uint4 sq[att_tiles(HD * ESZ)][G::NS][64];   // the queries' fragments
 
   // Workgroups are dealt to the eight XCDs in turn: all heads and column tiles of a share of a
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(RUNS * 64, 1) void attend_rows_kernel(AttendArgs a)
       for (int d = 0; d < G::ND; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j) vt[st][d][j] = x.turned(st, d, j);
-    if constexpr (G::AHEAD) x.load_v(next, after);
+    if constexpr (AHEAD) x.load_v(next, after);
     // Where some row does not see what another does, and a value there is no finite number, its
     // weight of 0 would not remove it: row by row then.
     const bool whole = base + RUN <= e_lo && base >= (a.window ? max(0, e_hi - a.window) : 0);
@@ -548,7 +550,7 @@ __global__ __launch_bounds__(RUNS * 64, 1) void attend_rows_kernel(AttendArgs a)
           }
       mixed = __ballot(odd) != 0;
     }
-    for (int ct = ct0; ct < ct1; ++ct, buf ^= G::BUFFERS - 1) {
+    for (int ct = ct0; ct < ct1; ++ct, buf ^= BUFFERS - 1) {
       const int ncol = min(COLS, cols - ct * COLS), t = min(ct * COLS + c, cols - 1) / a.G;
       const int end = before + t, first = a.window ? max(0, end - a.window) : 0;
       uint4 q[G::NS];
@@ -627,13 +629,13 @@ __global__ __launch_bounds__(RUNS * 64, 1) void attend_rows_kernel(AttendArgs a)
         *(f32x4*)(a.o + state * HD + d) = O;
         if (d == 0) a.ml[state] = make_float2(M, L);
       }
-      if constexpr (G::BUFFERS == 1) {
+      if constexpr (BUFFERS == 1) {
         __builtin_amdgcn_s_waitcnt(0xc07f);
         barrier_only();
       }
     }
     x.load_k(next);
-    if constexpr (!G::AHEAD) x.load_v(next, after);
+    if constexpr (!AHEAD) x.load_v(next, after);
     now = next;
   }
 }
@@ -809,7 +811,6 @@ size_t attend_workspace(int B, int T, int H, int hd, int64_t positions, int wind
   return (states * 8 + 255) / 256 * 256 + states * hd * 4;
 }
 
-constexpr int64_t STREAM_TARGET = 4096, ROWS_TARGET = 256;
 template <int DT, int HD, int ODT>
 static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   const int64_t positions = (int64_t)a.c.max_pages * a.c.page;
@@ -828,20 +829,23 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
     // Some 4096 waves, twice what the chip holds at once (64 sequences to 8192: 228 us; 2048
     // waves 273, 6144 233).
     a.cgroups = ctiles;
-    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, STREAM_TARGET / (heads * ctiles)));
+    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, 4096 / (heads * ctiles)));
     a.apart = a.splits / RUNS;
     const int64_t units = (int64_t)a.B * a.splits * a.Hkv * a.cgroups;
     constexpr int waves = stream_waves<DT, HD>();
     hipLaunchKernelGGL((attend_stream_kernel<DT, HD>), dim3((unsigned)((units + waves - 1) / waves)), dim3(waves * 64), 0, st, a);
   } else {
-    // Splits of the length first, some 256 workgroups, then of the column tiles (33 rows of 4
-    // sequences to 4096: 59 us; 128 and 512 workgroups 68 and 66).
-    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, ROWS_TARGET / heads));
+    // Splits of the length first, some 512 workgroups where there are few column tiles to share
+    // out and 256 else, then of the column tiles to 512 (5 rows of 16 sequences of 4096, two
+    // tiles: 73 us, 92 from 256; 33 rows, nine: 181 us, 189 from 512).
+    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, (ctiles <= 4 ? 512 : 256) / heads));
     const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT));
     a.cgroups = (int)std::min<int64_t>(ctiles, std::max<int64_t>(least, 512 / (heads * a.splits)));
     a.ctw = (ctiles + a.cgroups - 1) / a.cgroups;
     a.cgroups = (ctiles + a.ctw - 1) / a.ctw;
-    hipLaunchKernelGGL((attend_rows_kernel<DT, HD>), dim3((unsigned)(((int64_t)a.B * a.splits + 7) / 8 * 8 * a.Hkv * a.cgroups)), dim3(RUNS * 64), 0, st, a);
+    const dim3 grid((unsigned)(((int64_t)a.B * a.splits + 7) / 8 * 8 * a.Hkv * a.cgroups));
+    if (AttGeo<DT, HD>::AHEAD && a.ctw > 1) hipLaunchKernelGGL((attend_rows_kernel<DT, HD, AttGeo<DT, HD>::AHEAD>), grid, dim3(RUNS * 64), 0, st, a);
+    else hipLaunchKernelGGL((attend_rows_kernel<DT, HD, false>), grid, dim3(RUNS * 64), 0, st, a);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
