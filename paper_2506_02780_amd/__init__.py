@@ -556,8 +556,7 @@ def kv_append(k, v, k_cache, v_cache, tables, positions, seqs=None, q=None, inv_
               *cache, 0 if seqs is None else _whole(seqs, "seqs", (rows,), torch.int32, dev),
               _whole(positions, "positions", (rows,), torch.int32, dev), freq, ldq, ldk, ldv, ldqo,
               rows, n_heads, heads, hd, rot, 1 if interleaved else 0, dt)
-    _written(k_cache)
-    _written(v_cache)
+    _written((k_cache, v_cache))
     if given:
         _written(q_out)
     return q_out

@@ -298,6 +298,23 @@ def test_linear_rows_do_not_depend_on_the_others(ee, out, n, k):
             assert torch.equal(part, whole[lo:lo + rows]), (rows, lo)
 
 
+@pytest.mark.parametrize("k", [272, 512])
+@pytest.mark.parametrize("rows,n", [(7, 10240), (17, 4200), (21, 10241), (33, 10300), (65, 10250), (135, 11001), (1537, 1303), (261, 10245),
+                                    (515, 10250), (4201, 1303), (2049, 4205), (3001, 11008)])
+def test_linear_of_every_tile(ee, rows, n, k):
+    """Sizes at which each of the tiles runs (the last one's features in two launches), with
+    ragged edges: against float64, and bit for bit the rows alone."""
+    for out in ("bf16", "f32"):
+        y = _linear_case(ee, rows, k, n, out, act="silu", bias=True, residual=True, seed=rows)
+        g = _gen(rows)
+        x, xs, w, ws = _operands(g, rows, k, n)
+        b = _rand(g, n).cuda()
+        r = _rand(g, rows, n, dtype=DT[out]).cuda()
+        for lo, hi in ((0, 1), (rows // 2, rows // 2 + 3), (rows - 6, rows)):
+            part = ee.fp8_linear(x[lo:hi], xs[lo:hi], w, ws, bias=b, act="silu", residual=r[lo:hi], out_dtype=DT[out])
+            assert torch.equal(part, y[lo:hi]), (out, lo)
+
+
 def test_linear_residual_in_place(ee):
     x, xs, w, ws = _operands(_gen(3), 33, 256, 96)
     h = _rand(_gen(1), 33, 96, dtype=torch.bfloat16).cuda()
