@@ -697,7 +697,7 @@ __device__ __forceinline__ void join_runs(float2* ml, f32x4* x) {
 // At most JOIN_GROUPS chunks are held: every sum is one chunk's state.
 template <int HD, int ODT>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4, AT_ONCE = 8;
+  constexpr int LPS = HD / 4, AT_ONCE = 16;
   const int64_t item = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
   if (item >= (int64_t)a.B * a.T * a.H) return;
   const int at = threadIdx.x % LPS, d = at * 4;
@@ -728,12 +728,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     for (int i = 0; i < AT_ONCE; ++i) {
       if (i0 + i >= n || (apart && i % RUNS)) continue;
       const float f = exp2_(ml[i].x - mu), fl = product(f, ml[i].y);
-      l = i0 + i ? l + fl : fl;
+      l += fl;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float y = product(f, x[i][e]);
-        o[e] = i0 + i ? o[e] + y : y;
-      }
+      for (int e = 0; e < 4; ++e) o[e] += product(f, x[i][e]);
     }
   }
   join_store<HD, ODT>(a, j, d, M, l, o);
@@ -742,13 +739,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us).
 template <int HD, int ODT>
 __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = RUNS;
+  constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = 8;
   __shared__ float sM[16], sL[JOIN_GROUPS];
   __shared__ __attribute__((aligned(16))) float sO[JOIN_GROUPS][HD];
   const int tid = threadIdx.x, set = tid / LPS, d = tid % LPS * 4;
   const Joined j = joined(a, blockIdx.x);
   const bool apart = j.n <= a.apart;
-  const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1, next = apart ? 1 : JOIN_GROUPS;   // states of a chunk; to the next at once
+  const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1;   // states of a chunk
   auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
   float M = -INFINITY;
   for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
@@ -765,19 +762,22 @@ __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
       const int g = set * PER + p;
       float l = 0.f;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int i0 = g * per; i0 < n; i0 += AT_ONCE * JOIN_GROUPS) {   // (apart: of one chunk)
+      // (apart: AT_ONCE / RUNS chunks of the group, the runs of each side by side)
+      for (int c0 = g; c0 < j.n; c0 += AT_ONCE / per * JOIN_GROUPS) {
         float2 ml[AT_ONCE];
         f32x4 x[AT_ONCE];
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-          const int64_t s = state(min(i0 + i * next, n - 1));
+          const int64_t s = state(min(apart ? (c0 + i / RUNS * JOIN_GROUPS) * RUNS + i % RUNS : c0 + i * JOIN_GROUPS, n - 1));
           ml[i] = a.ml[s];
           x[i] = *(const f32x4*)(a.o + s * HD + d);
         }
-        if (apart) join_runs(ml, x);
+        if (apart)
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-          if (i0 + i * next >= n || (apart && i)) continue;
+          if (c0 + i / per * JOIN_GROUPS >= j.n || (apart && i % RUNS)) continue;
           const float f = exp2_(ml[i].x - mu);
           l = fmaf(f, ml[i].y, l);
 #pragma unroll
@@ -791,7 +791,9 @@ __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
   if (set) return;
   float l = sL[0];
   f32x4 o = *(const f32x4*)&sO[0][d];
-  for (int i = 1; i < min(j.n, JOIN_GROUPS); ++i) {
+  // (groups that hold no chunk were left at +0, which adds nothing: no sum is -0 but one of such)
+#pragma unroll 8
+  for (int i = 1; i < JOIN_GROUPS; ++i) {
     l += sL[i];
     const f32x4 y = *(const f32x4*)&sO[i][d];
 #pragma unroll
