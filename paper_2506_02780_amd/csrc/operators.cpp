@@ -330,7 +330,8 @@ int32_t ee_paged_attention(const ee_paged_attention_args* p, void* stream) {
   a.q = q.q; a.out = q.out; a.lse = q.lse; a.c = paged(c); a.lens = q.lens; a.ws = reinterpret_cast<unsigned char*>(q.workspace);
   a.ldq = q.ldq; a.ldo = q.ldo;
   a.B = c.n_seqs; a.T = q.rows; a.H = q.n_heads; a.Hkv = q.n_kv_heads; a.G = q.n_heads / q.n_kv_heads; a.hd = q.head_dim;
-  a.dt = dt_of(q.dtype); a.odt = dt_of(q.out_dtype); a.window = q.window;
+  a.dt = dt_of(q.dtype); a.odt = dt_of(q.out_dtype);
+  a.window = q.window < positions ? q.window : 0;   // (so that kernels may subtract it from a negative end)
   a.scale_log2 = q.scale * 1.4426950408889634f;
   return launched(ee::run_attend(a, reinterpret_cast<hipStream_t>(stream)));
 }

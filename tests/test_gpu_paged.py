@@ -332,6 +332,14 @@ def test_attend_missing_pages(ee, rows, dtype):
                      page=page, window=window, tables=tables)
 
 
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 5, 2 ** 30])
+def test_attend_windows_past_every_position(ee, window):
+    """Sequences shorter than the block, whose first rows stand before position 0."""
+    for rows in (1, 6, 40):
+        a, b = (_attend_case(ee, lens=[3, 1, 100, 0], heads=4, kv=2, hd=64, rows=rows, window=w) for w in (window, 0))
+        assert torch.equal(a["y"], b["y"])
+
+
 def test_attend_negative_lengths_and_empty_batches(ee):
     _attend_case(ee, lens=[-5, -2 ** 31, 0, 3], heads=2, kv=1, hd=64, tables=torch.zeros(4, 1, dtype=torch.int32, device="cuda"))
     kc, vc = _cache(_gen(0), 2, 16, 1, 64, torch.float32)
