@@ -651,7 +651,8 @@ int32_t ee_kv_append(const ee_kv_append_args* args, void* hip_stream);
  * see does not matter, NaN included.  (Of visible ones, NaN gives NaN, and an infinite value an
  * infinity or, in bf16, where weights are multiplied as two parts, NaN.)  lens are cut to [0, max_pages * page_size].
  * Scores, weights and sums are fp32; a row's result depends on what it sees alone, so
- * a block of rows equals its rows one by one.  rows 1 is a decoding step; at most 1024.
+ * a block of rows equals its rows one by one.  rows 1 is a decoding step; at most 1024,
+ * n_seqs * rows * n_heads at most 2^24.
  * workspace: at least ee_paged_attention_workspace_bytes (0 for invalid sizes), 256-byte aligned, in
  * use until the call's work is done; calls that may overlap need one each.  The bytes never
  * fall as n_seqs, rows or max_pages grow. */

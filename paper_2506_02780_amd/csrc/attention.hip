@@ -736,70 +736,75 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   join_store<HD, ODT>(a, j, d, M, l, o);
 }
 
-// More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us).
+// More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us), from
+// 2^20 on in turn, since a launch holds less than 2^32 threads.
 template <int HD, int ODT>
 __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
   constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = 8;
   __shared__ float sM[16], sL[JOIN_GROUPS];
   __shared__ __attribute__((aligned(16))) float sO[JOIN_GROUPS][HD];
   const int tid = threadIdx.x, set = tid / LPS, d = tid % LPS * 4;
-  const Joined j = joined(a, blockIdx.x);
-  const bool apart = j.n <= a.apart;
-  const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1;   // states of a chunk
-  auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
-  float M = -INFINITY;
-  for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
+  for (int64_t item = blockIdx.x; item < (int64_t)a.B * a.T * a.H; item += gridDim.x) {
+    const Joined j = joined(a, item);
+    const bool apart = j.n <= a.apart;
+    const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1;   // states of a chunk
+    auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
+    float M = -INFINITY;
+    for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-  if ((tid & 63) == 0) sM[tid >> 6] = M;
-  __syncthreads();
+    for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+    if ((tid & 63) == 0) sM[tid >> 6] = M;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 16; ++i) M = fmaxf(M, sM[i]);
-  const float mu = M == -INFINITY ? 0.f : M;
-  if (set < SETS)
+    for (int i = 0; i < 16; ++i) M = fmaxf(M, sM[i]);
+    const float mu = M == -INFINITY ? 0.f : M;
+    if (set < SETS)
 #pragma unroll
-    for (int p = 0; p < PER; ++p) {
-      const int g = set * PER + p;
-      float l = 0.f;
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      // (apart: AT_ONCE / RUNS chunks of the group, the runs of each side by side)
-      for (int c0 = g; c0 < j.n; c0 += AT_ONCE / per * JOIN_GROUPS) {
-        float2 ml[AT_ONCE];
-        f32x4 x[AT_ONCE];
+      for (int p = 0; p < PER; ++p) {
+        const int g = set * PER + p;
+        float l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        // (apart: AT_ONCE / RUNS chunks of the group, the runs of each side by side)
+        for (int c0 = g; c0 < j.n; c0 += AT_ONCE / per * JOIN_GROUPS) {
+          float2 ml[AT_ONCE];
+          f32x4 x[AT_ONCE];
 #pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-          const int64_t s = state(min(apart ? (c0 + i / RUNS * JOIN_GROUPS) * RUNS + i % RUNS : c0 + i * JOIN_GROUPS, n - 1));
-          ml[i] = a.ml[s];
-          x[i] = *(const f32x4*)(a.o + s * HD + d);
+          for (int i = 0; i < AT_ONCE; ++i) {
+            const int64_t s = state(min(apart ? (c0 + i / RUNS * JOIN_GROUPS) * RUNS + i % RUNS : c0 + i * JOIN_GROUPS, n - 1));
+            ml[i] = a.ml[s];
+            x[i] = *(const f32x4*)(a.o + s * HD + d);
+          }
+          if (apart)
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i) {
+            if (c0 + i / per * JOIN_GROUPS >= j.n || (apart && i % RUNS)) continue;
+            const float f = exp2_(ml[i].x - mu);
+            l = fmaf(f, ml[i].y, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
+          }
         }
-        if (apart)
-#pragma unroll
-          for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
-#pragma unroll
-        for (int i = 0; i < AT_ONCE; ++i) {
-          if (c0 + i / per * JOIN_GROUPS >= j.n || (apart && i % RUNS)) continue;
-          const float f = exp2_(ml[i].x - mu);
-          l = fmaf(f, ml[i].y, l);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
-        }
+        *(f32x4*)&sO[g][d] = o;
+        if (d == 0) sL[g] = l;
       }
-      *(f32x4*)&sO[g][d] = o;
-      if (d == 0) sL[g] = l;
-    }
-  __syncthreads();
-  if (set) return;
-  float l = sL[0];
-  f32x4 o = *(const f32x4*)&sO[0][d];
-  // (groups that hold no chunk were left at +0, which adds nothing: no sum is -0 but one of such)
+    __syncthreads();
+    if (set == 0) {
+      float l = sL[0];
+      f32x4 o = *(const f32x4*)&sO[0][d];
+      // (groups that hold no chunk were left at +0, which adds nothing: no sum is -0 but one of such)
 #pragma unroll 8
-  for (int i = 1; i < JOIN_GROUPS; ++i) {
-    l += sL[i];
-    const f32x4 y = *(const f32x4*)&sO[i][d];
+      for (int i = 1; i < JOIN_GROUPS; ++i) {
+        l += sL[i];
+        const f32x4 y = *(const f32x4*)&sO[i][d];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += y[e];
+        for (int e = 0; e < 4; ++e) o[e] += y[e];
+      }
+      join_store<HD, ODT>(a, j, d, M, l, o);
+    }
+    __syncthreads();
   }
-  join_store<HD, ODT>(a, j, d, M, l, o);
 }
 
 // Chunks whose states are held at once: a row's window reaches over that many.
@@ -851,7 +856,7 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
-  if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)items), dim3(1024), 0, st, a);
+  if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)std::min<int64_t>(items, 1 << 20)), dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((attend_join_kernel<HD, ODT>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }

@@ -201,6 +201,7 @@ int32_t ee_fp8_linear(const ee_fp8_linear_args* p, void* stream) {
 
 // What appending and attention check of a cache and the heads around it.
 constexpr int MAX_HEADS = 1024, MAX_POSITIONS = 1 << 30;
+constexpr int64_t MAX_STATES = 1 << 24;   // rows times heads of a call: its launches stay below 2^32 threads
 static const char* cache_shape(const ee_paged_cache& c, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
   if (!dtype_ok(dtype)) return "dtype must be EE_F32 or EE_BF16";
   if (head_dim != 64 && head_dim != 128 && head_dim != 256) return "head_dim must be 64, 128 or 256";
@@ -285,7 +286,7 @@ int32_t ee_kv_append(const ee_kv_append_args* p, void* stream) {
 static const char* attend_shape(int64_t n_seqs, int64_t rows, int32_t n_heads, int64_t positions, int32_t head_dim, int32_t window) {
   if (rows < 1 || rows > 1024 || n_seqs * rows > MAX_ROWS) return "rows must be in [1, 1024], n_seqs * rows at most 2^22";
   if (window < 0) return "window must not be negative";
-  if (n_seqs * rows * n_heads > MAX_BLOCKS) return "too many rows and heads";
+  if (n_seqs * rows * n_heads > MAX_STATES) return "too many rows and heads: n_seqs * rows * n_heads must be at most 2^24";
   return nullptr;
 }
 

@@ -457,6 +457,23 @@ def test_attend_long(ee, dtype):
     _attend_case(ee, lens=[40000], heads=4, kv=2, hd=128, dtype=dtype, page=64, poison=False, window=9000)
 
 
+def test_attend_more_rows_than_a_launch_of_workgroups(ee):
+    """1.1 million rows and heads, whose states of 33 chunks take 9.8 GB."""
+    seqs, rows, heads, page = 17, 1024, 64, 64
+    lens = [1024 + 64 * i for i in range(seqs)]
+    g = _gen(0)
+    tables, n_pages = _tables(g, lens, page)
+    kc, vc = _cache(g, n_pages, page, 1, 64, torch.bfloat16)
+    q = _rand(g, 1024, heads * 64, dtype=torch.bfloat16).cuda().repeat(seqs, 1)
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    wide = torch.full((seqs, 132 + 1), -1, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    y = ee.paged_attention(q, kc, vc, wide, length)
+    for b in (0, 8, 16):
+        one = ee.paged_attention(q[:rows], kc, vc, tables[b:b + 1].contiguous(), length[b:b + 1])
+        assert torch.equal(y[b * rows:(b + 1) * rows], one), b
+
+
 def test_attend_past_32_bit_offsets(ee):
     pages, page, kv, hd = 2200, 64, 64, 256      # 4.6 GB each of k and v
     kc, vc = (torch.zeros(pages, page, kv, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2))

@@ -133,7 +133,8 @@ def test_append_refusals(ee, kw, word):
 
 @pytest.mark.parametrize("kw,word", CACHE_REFUSALS + MEMORY_REFUSALS + [
     (dict(rows=0), "rows"), (dict(rows=1025), "rows"), (dict(rows=1024, n_seqs=4097), "rows"), (dict(window=-1), "window"),
-    (dict(n_seqs=1 << 22, n_heads=1024, n_kv_heads=1), "too many"), (dict(out_dtype=2), "out_dtype"), (dict(dtype=0, out_dtype=1), "out_dtype"),
+    (dict(n_seqs=1 << 22, n_heads=1024, n_kv_heads=1), "too many"), (dict(n_seqs=1 << 22, n_heads=8), "too many"),
+    (dict(n_seqs=(1 << 14) + 1, rows=1024, n_heads=1, n_kv_heads=1), "rows"), (dict(out_dtype=2), "out_dtype"), (dict(dtype=0, out_dtype=1), "out_dtype"),
     (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(q=None), "non-NULL"), (dict(out=None), "non-NULL"),
     (dict(lens=None), "non-NULL"), (dict(workspace=None), "non-NULL"), (dict(q=P + 8), "q must"), (dict(ldq=248), "q must"), (dict(ldq=260), "q must"),
     (dict(ldq=(1 << 21) + 64), "q must"), (dict(out=P + 1), "out must"), (dict(ldo=255), "out must"), (dict(lens=P + 2), "lens"), (dict(lse=P + 2), "lens"),
