@@ -220,8 +220,8 @@ template <int DT, int HD> struct Stream {
     const int turn = lane >> 2;
     const int64_t p0 = p + turn / inner * step + turn % inner * inner_step + 16 * (lane & 3);
     entries = p0 < (int64_t)pc.max_pages * pc.page ? table[page_of((int)p0)] : -1;
-    asm volatile("" : "+v"(entries));   // (waited for here, not wherever they are used)
   }
+  __device__ __forceinline__ void entries_wait() { asm volatile("" : "+v"(entries)); }   // (here, not wherever they are used)
   __device__ __forceinline__ Pages pages(int turn, int base) const {
     Pages p;
 #pragma unroll
@@ -382,13 +382,14 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
   if (ch >= ch1) return;
   const int ncol = min(COLS, a.G - ct * COLS), col = min(ct * COLS + c, a.G - 1);   // (columns past the last repeat it)
 
+  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, len, lane, c, grp};
+  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK, (int64_t)a.splits * CHUNK, RUNS, RUN); };   // of four chunks
+  entries(ch);   // (on its way with the queries)
   uint4 (&qs)[G::NS][64] = sq[threadIdx.x >> 6];   // (the wave's own: no barrier)
   const uint8_t* qp = (const uint8_t*)a.q + ((int64_t)b * a.ldq + (h * a.G + col) * HD) * ESZ + grp * 16;
 #pragma unroll
   for (int f = 0; f < G::NS; ++f) qs[f][lane] = *(const uint4*)(qp + f * 64);
-  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, len, lane, c, grp};
-  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK, (int64_t)a.splits * CHUNK, RUNS, RUN); };   // of four chunks
-  entries(ch);
+  x.entries_wait();
   int ahead = 0;   // chunks on since then
   typename Stream<DT, HD>::Pages now = x.pages(run0, ch * CHUNK + run0 * RUN), next;
   if constexpr (G::AHEAD) {
@@ -411,6 +412,7 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
         after = (ch + a.splits) * CHUNK;
         if (++ahead == 4) {
           entries(ch + a.splits);
+          x.entries_wait();
           ahead = 0;
         }
       }
@@ -501,13 +503,14 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
   int ch = start / CHUNK + split;
   if (ch >= ch1) return;
 
+  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, e_hi, lane, c, grp};
+  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK + wv * RUN, (int64_t)a.splits * CHUNK, 1, 0); };
+  entries(ch);   // (on its way with the queries)
   for (int i = wv; i < (ct1 - ct0) * G::NS; i += RUNS) {
     const int ct = i / G::NS, f = i % G::NS, col = min((ct0 + ct) * COLS + c, cols - 1);   // (columns past the last repeat it)
     sq[ct][f][lane] = *(const uint4*)((const uint8_t*)a.q + ((int64_t)(b * a.T + col / a.G) * a.ldq + (h * a.G + col % a.G) * HD) * ESZ + grp * 16 + f * 64);
   }
-  Stream<DT, HD> x{pc, pc.tables + b * pc.ldt, (const uint8_t*)pc.k + h * pc.kh * ESZ, (const uint8_t*)pc.v + h * pc.vh * ESZ, a.page_mul, start, e_hi, lane, c, grp};
-  auto entries = [&](int chunk) { x.entries_load((int64_t)chunk * CHUNK + wv * RUN, (int64_t)a.splits * CHUNK, 1, 0); };
-  entries(ch);
+  x.entries_wait();
   int ahead = 0;
   typename Stream<DT, HD>::Pages now = x.pages(0, ch * CHUNK + wv * RUN), next;
   x.load_k(now);
@@ -520,6 +523,7 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
     // (past the last chunk there are no pages, and requests read nothing)
     if (++ahead == 16) {
       entries(ch + a.splits);
+      x.entries_wait();
       ahead = 0;
     }
     next = x.pages(ahead, after);
@@ -694,10 +698,11 @@ __device__ __forceinline__ void join_runs(float2* ml, f32x4* x) {
   }
 }
 
-// At most JOIN_GROUPS chunks are held: every sum is one chunk's state.
-template <int HD, int ODT>
+// At most JOIN_GROUPS chunks are held: every sum is one chunk's state.  AT_ONCE are requested together
+// (64 sequences to 8192: 8.6 us with 16, 11.5 with 8; one of 2048, eight chunks: 4.4 and 3.9).
+template <int HD, int ODT, int AT_ONCE>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4, AT_ONCE = 16;
+  constexpr int LPS = HD / 4;
   const int64_t item = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
   if (item >= (int64_t)a.B * a.T * a.H) return;
   const int at = threadIdx.x % LPS, d = at * 4;
@@ -740,7 +745,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // 2^20 on in turn, since a launch holds less than 2^32 threads.
 template <int HD, int ODT>
 __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = 8;
+  constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = RUNS;
   __shared__ float sM[16], sL[JOIN_GROUPS];
   __shared__ __attribute__((aligned(16))) float sO[JOIN_GROUPS][HD];
   const int tid = threadIdx.x, set = tid / LPS, d = tid % LPS * 4;
@@ -842,10 +847,11 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
     constexpr int waves = stream_waves<DT, HD>();
     hipLaunchKernelGGL((attend_stream_kernel<DT, HD>), dim3((unsigned)((units + waves - 1) / waves)), dim3(waves * 64), 0, st, a);
   } else {
-    // Splits of the length first, some 512 workgroups where there are few column tiles to share
-    // out and 256 else, then of the column tiles to 512 (5 rows of 16 sequences of 4096, two
-    // tiles: 73 us, 92 from 256; 33 rows, nine: 181 us, 189 from 512).
-    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, (ctiles <= 4 ? 512 : 256) / heads));
+    // Splits of the length first, some 256 workgroups, or 512 of two to four column tiles, of
+    // which a CU holds two; then of the column tiles to 512 (one row of 8 sequences of 2048: 21 us,
+    // 24.6 from 512; 5 rows of 16 of 4096, two tiles: 73 from 512, 92 from 256; 33 rows, nine:
+    // 181, 189 from 512).
+    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, (ctiles > 1 && ctiles <= 4 ? 512 : 256) / heads));
     const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT));
     a.cgroups = (int)std::min<int64_t>(ctiles, std::max<int64_t>(least, 512 / (heads * a.splits)));
     a.ctw = (ctiles + a.cgroups - 1) / a.cgroups;
@@ -857,7 +863,8 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
   if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)std::min<int64_t>(items, 1 << 20)), dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL((attend_join_kernel<HD, ODT>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
+  else if (a.ring > 8) hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 16>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 8>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
