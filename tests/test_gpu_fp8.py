@@ -119,6 +119,36 @@ def test_quant_special_values(ee, block_rows, dtype):
 
 
 @pytest.mark.parametrize("block_rows", [1, 128])
+def test_quant_quotients_at_ties(ee, block_rows):
+    """Quotients at, just above and just below the middle between two codes, at scales from the
+    smallest to the largest: each rounds as the IEEE quotient does."""
+    g = _gen(11)
+    rows = 128 * 70
+    amax = torch.exp2(torch.linspace(-149, 127.9, rows // block_rows, dtype=torch.float64)) * (1 + torch.rand(rows // block_rows, generator=g).double())
+    amax = amax.float().clamp(max=3.4e38).repeat_interleave(block_rows)
+    scale = torch.maximum((amax.double() / 448).float(), torch.tensor(2.0 ** -126)).double()
+    codes = torch.arange(0, 126, dtype=torch.uint8)
+    low, high = codes.view(E4M3).double(), (codes + 1).view(E4M3).double()
+    mid = torch.cat([(low + high) / 2, high])[torch.randint(0, 252, (rows, 384), generator=g)]
+    x = (mid * scale[:, None]).float()
+    x = torch.where(x.abs() > amax[:, None], amax[:, None], x)
+    step = torch.randint(-2, 3, (rows, 384), generator=g)
+    x = (x.view(torch.int32) + step.to(torch.int32)).clamp(min=0).view(torch.float32)
+    x = torch.minimum(x, amax[:, None]) * (1 - 2 * torch.randint(0, 2, (rows, 384), generator=g))
+    x[:, ::128] = amax[:, None]
+    _quant_case(ee, x.cuda(), block_rows)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quant_many_blocks(ee, dtype):
+    x = _rand(_gen(12), 20001, 2064, std=3.0, dtype=DT[dtype])
+    x[::7] *= 2.0 ** -100
+    x[5::11, ::3] = -0.0
+    x[3, 7], x[20000, 2063], x[19999, 100] = float("nan"), float("inf"), -float("inf")
+    _quant_case(ee, x.cuda(), 1)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
 def test_quant_strides_and_outputs(ee, block_rows):
     g = _gen(4)
     for dtype, pad in (("bf16", 8), ("f32", 4), ("bf16", 40)):
