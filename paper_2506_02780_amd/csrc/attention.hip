@@ -146,7 +146,7 @@ hipError_t run_append(const AppendArgs& a, hipStream_t st) {
 
 constexpr int RUN = 64, RUNS = 4, CHUNK = RUN * RUNS;   // positions of a run, runs of a chunk
 constexpr int COLS = 16;                                // a tile's columns: (row, query head of the group) pairs
-static_assert(CHUNK == ATTEND_CHUNK, "");
+static_assert(CHUNK == ATTEND_CHUNK && RUNS * 64 == COLS * 16, "");
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -616,21 +616,28 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
                   f32x4{o[np * G::EPV + e][r], o[np * G::EPV + e + 1][r], o[np * G::EPV + e + 2][r], o[np * G::EPV + e + 3][r]};
       __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
       barrier_only();                       // (the next run's requests go on)
-      for (int i = threadIdx.x; i < ncol * (HD / 4); i += RUNS * 64) {
-        const int y = i / (HD / 4), d = i % (HD / 4) * 4;
+      // Sixteen threads a column, whose factors they form once.
+      if (const int y = threadIdx.x / 16; y < ncol) {
+        const int d = threadIdx.x % 16 * 4;
         float M = sm[buf][0][y], L = sl[buf][0][y];
-        f32x4 O = *(const f32x4*)&so[buf][0][y][d];
+        f32x4 O[HD / 64];
+#pragma unroll
+        for (int p = 0; p < HD / 64; ++p) O[p] = *(const f32x4*)&so[buf][0][y][d + 64 * p];
 #pragma unroll
         for (int w = 1; w < RUNS; ++w) {
           const float mw = sm[buf][w][y], N = fmaxf(M, mw), fa = join_scale(M, N), fb = join_scale(mw, N);
           L = fmaf(sl[buf][w][y], fb, L * fa);
           M = N;
-          const f32x4 z = *(const f32x4*)&so[buf][w][y][d];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) O[e] = fmaf(z[e], fb, O[e] * fa);
+          for (int p = 0; p < HD / 64; ++p) {
+            const f32x4 z = *(const f32x4*)&so[buf][w][y][d + 64 * p];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) O[p][e] = fmaf(z[e], fb, O[p][e] * fa);
+          }
         }
         const int64_t state = ((int64_t)(b * a.ring + ch % a.ring) * a.Hkv + h) * cols + ct * COLS + y;
-        *(f32x4*)(a.o + state * HD + d) = O;
+#pragma unroll
+        for (int p = 0; p < HD / 64; ++p) *(f32x4*)(a.o + state * HD + d + 64 * p) = O[p];
         if (d == 0) a.ml[state] = make_float2(M, L);
       }
       if constexpr (BUFFERS == 1) {
