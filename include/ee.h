@@ -648,8 +648,8 @@ int32_t ee_kv_append(const ee_kv_append_args* args, void* hip_stream);
  * first.  out = sum_j softmax_j(scale q . k_j) v_j per query head, which reads KV head
  * head / (n_heads / n_kv_heads); lse = the natural log of the sum of e^(scale q . k_j).
  * A row that sees nothing (or only scores of -inf) is zeros with lse -inf; what a row does not
- * see does not matter, NaN included.  (Of visible ones, NaN gives NaN, and an infinite value an
- * infinity or, in bf16, where weights are multiplied as two parts, NaN.)  lens are cut to [0, max_pages * page_size].
+ * see does not matter, NaN included.  Of what it sees, NaN gives NaN, and an infinite value its infinity
+ * (NaN beside one of the other sign, or where its weight is 0 in fp32).  lens are cut to [0, max_pages * page_size].
  * Scores, weights and sums are fp32; a row's result depends on what it sees alone, so
  * a block of rows equals its rows one by one.  rows 1 is a decoding step; at most 1024,
  * n_seqs * rows * n_heads at most 2^24.

@@ -350,6 +350,30 @@ template <int DT, int ND, class X> __device__ __forceinline__ void weigh(const W
   }
 }
 
+// Whether some sum of weights and values is no number.  Finite values leave numbers whatever the
+// weights, so only then is the sum formed again with care: a weight of 0 does not remove an infinity or NaN
+// that a row does not see, and an infinite value is left to the upper part of its weight, since the
+// lower one may be 0 or of the other sign.  (16 instructions a run of head_dim 128; looking
+// at the values instead took 33 rows of 4 sequences to 4096 43 us, 37.5 so.)
+template <int ND> __device__ __forceinline__ bool no_number(const f32x4 (&o)[ND]) {
+  float most = 0.f;   // (a maximum that NaN goes through)
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int r = 0; r < 4; r += 2) most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(most, o[d][r]), o[d][r + 1]);
+  return __ballot(most != most) != 0;
+}
+// The word of a pair of bf16 values without its infinities.
+__device__ __forceinline__ uint32_t without_infinities(uint32_t y) {
+  return y & (((y & 0x7fffu) == 0x7f80u ? 0u : 0xffffu) | ((y & 0x7fff0000u) == 0x7f800000u ? 0u : 0xffff0000u));
+}
+template <int DT> __device__ __forceinline__ f32x4 weigh_careful(const Weights<DT>& w, const uint32_t (&y)[4], f32x4 acc) {   // (in the order of weigh)
+  acc = mma<DT>(w.hi, make_uint4(y[0], y[1], y[2], y[3]), acc);
+  if constexpr (DT == DT_BF16)
+    acc = mma<DT>(w.lo, make_uint4(without_infinities(y[0]), without_infinities(y[1]), without_infinities(y[2]), without_infinities(y[3])), acc);
+  return acc;
+}
+
 // One row per sequence.  What bounds it is the cache's stream (64 sequences up to 8192, 32
 // heads over 8 of 128: 1.07 GB): a wave takes a KV head's chunks split, split + splits, ...
 // of a sequence, run after run, and requests the next run's keys and values as soon
@@ -396,6 +420,26 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
     x.load_k(now);
     x.load_v(now, ch * CHUNK + run0 * RUN);
   }
+  // A chunk's state takes in a run's.
+  auto take_in = [&](bool first, const f32x4 (&one)[G::ND], float mr, float lr, f32x4 (&o)[G::ND], float& m, float& l) {
+    if (first) {
+      m = mr;
+      l = lr;
+#pragma unroll
+      for (int i = 0; i < G::ND; ++i) o[i] = one[i];
+    } else {
+      // m, l and the scales belong to column c, the values to columns 4 grp + r
+      const float M = fmaxf(m, mr), fa = join_scale(m, M), fb = join_scale(mr, M);
+      l = fmaf(lr, fb, l * fa);
+      m = M;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float ra = __shfl(fa, 4 * grp + r), rb = __shfl(fb, 4 * grp + r);
+#pragma unroll
+        for (int i = 0; i < G::ND; ++i) o[i][r] = fmaf(one[i][r], rb, o[i][r] * ra);
+      }
+    }
+  };
   for (; ch < ch1; ch += a.splits) {
     f32x4 o[G::ND];
     float m = -INFINITY, l = 0.f;
@@ -434,25 +478,44 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
       for (int st = 0; st < G::STEPS; ++st)
         weigh<DT>(operand_weights<DT>(s, st), [&](int d) { return make_uint4(x.turned(st, d, 0), x.turned(st, d, 1), x.turned(st, d, 2), x.turned(st, d, 3)); }, one);
       if constexpr (G::AHEAD) x.load_v(next, after);
-      if (run == run0) {
-        m = mr;
-        l = lr;
-#pragma unroll
-        for (int i = 0; i < G::ND; ++i) o[i] = one[i];
-      } else {
-        // m, l and the scales belong to column c, the values to columns 4 grp + r
-        const float M = fmaxf(m, mr), fa = join_scale(m, M), fb = join_scale(mr, M);
-        l = fmaf(lr, fb, l * fa);
-        m = M;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float ra = __shfl(fa, 4 * grp + r), rb = __shfl(fb, 4 * grp + r);
-#pragma unroll
-          for (int i = 0; i < G::ND; ++i) o[i][r] = fmaf(one[i][r], rb, o[i][r] * ra);
-        }
-      }
+      take_in(run == run0, one, mr, lr, o, m, l);
       now = next;
     }
+    if constexpr (DT == DT_BF16)
+      if (__builtin_expect(no_number(o), 0)) {   // the chunk once more, then the next one's requests
+        entries(ch);
+        x.entries_wait();
+        for (int run = run0; run < run0 + runs; ++run) {
+          const int base = ch * CHUNK + run * RUN;
+          const typename Stream<DT, HD>::Pages p = x.pages(run, base);
+          x.load_k(p);
+          x.load_v(p, base);
+          uint4 q[G::NS];
+#pragma unroll
+          for (int f = 0; f < G::NS; ++f) q[f] = qs[f][lane];
+          f32x4 s[4];
+          x.scores(q, s);
+          float mr, lr;
+          x.weights(p, base, start, len, false, a.scale_log2, s, mr, lr);
+          f32x4 one[G::ND];
+#pragma unroll
+          for (int d = 0; d < G::ND; ++d) {
+            one[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < G::STEPS; ++st) {
+              const uint32_t y[4] = {x.turned(st, d, 0), x.turned(st, d, 1), x.turned(st, d, 2), x.turned(st, d, 3)};
+              one[d] = weigh_careful<DT>(operand_weights<DT>(s, st), y, one[d]);
+            }
+          }
+          take_in(run == run0, one, mr, lr, o, m, l);
+        }
+        entries(ch + a.splits * (1 - ahead));
+        x.entries_wait();
+        if constexpr (G::AHEAD) {
+          x.load_k(now);
+          x.load_v(now, (ch + a.splits) * CHUNK);
+        }
+      }
     const int64_t state = ((int64_t)(b * a.ring + (runs == 1 ? split : ch % a.ring)) * a.Hkv + h) * a.G + ct * COLS;
     if (grp == 0 && c < ncol) a.ml[state + c] = make_float2(m, l);
     // o[np EPV + e] of lane (grp, c): columns 4 grp + r, dimension np 16 EPV + c EPV + e
@@ -536,24 +599,7 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
 #pragma unroll
         for (int j = 0; j < 4; ++j) vt[st][d][j] = x.turned(st, d, j);
     if constexpr (AHEAD) x.load_v(next, after);
-    // Where some row does not see what another does, and a value there is no finite number, its
-    // weight of 0 would not remove it: row by row then.
     const bool whole = base + RUN <= e_lo && base >= (a.window ? max(0, e_hi - a.window) : 0);
-    bool mixed = a.T > 1 && !whole;
-    if (mixed) {
-      bool odd = false;
-#pragma unroll
-      for (int st = 0; st < G::STEPS; ++st)
-#pragma unroll
-        for (int d = 0; d < G::ND; ++d)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t y = vt[st][d][j];
-            if constexpr (DT == DT_BF16) odd |= (y & 0x7f80u) == 0x7f80u || (y & 0x7f800000u) == 0x7f800000u;
-            else odd |= (y & 0x7f800000u) == 0x7f800000u;
-          }
-      mixed = __ballot(odd) != 0;
-    }
     for (int ct = ct0; ct < ct1; ++ct, buf ^= BUFFERS - 1) {
       const int ncol = min(COLS, cols - ct * COLS), t = min(ct * COLS + c, cols - 1) / a.G;
       const int end = before + t, first = a.window ? max(0, end - a.window) : 0;
@@ -567,20 +613,18 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
       f32x4 o[G::ND];
 #pragma unroll
       for (int i = 0; i < G::ND; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (!mixed) {
 #pragma unroll
-        for (int st = 0; st < G::STEPS; ++st)
-          weigh<DT>(operand_weights<DT>(s, st), [&](int d) { return make_uint4(vt[st][d][0], vt[st][d][1], vt[st][d][2], vt[st][d][3]); }, o);
-      } else {
+      for (int st = 0; st < G::STEPS; ++st)
+        weigh<DT>(operand_weights<DT>(s, st), [&](int d) { return make_uint4(vt[st][d][0], vt[st][d][1], vt[st][d][2], vt[st][d][3]); }, o);
+      if (__builtin_expect(no_number(o), 0)) {   // row by row, of what it sees
         const int t_lo = ct * COLS / a.G, t_hi = (ct * COLS + ncol - 1) / a.G;
         for (int tt = t_lo; tt <= t_hi; ++tt) {
           const int to = before + tt, from = a.window ? max(0, to - a.window) : 0;
 #pragma unroll
           for (int d = 0; d < G::ND; ++d) {
-            f32x4 one = {0.f, 0.f, 0.f, 0.f};   // (a tile's parts in the order of weigh)
+            f32x4 one = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int st = 0; st < G::STEPS; ++st) {
-              const Weights<DT> w = operand_weights<DT>(s, st);
               uint32_t y[4];
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
@@ -591,8 +635,7 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
                 if constexpr (DT == DT_BF16) y[j] = vt[st][d][j] & ((in(2 * j) ? 0xffffu : 0u) | (in(2 * j + 1) ? 0xffff0000u : 0u));
                 else y[j] = in(j) ? vt[st][d][j] : 0u;
               }
-              one = mma<DT>(w.hi, make_uint4(y[0], y[1], y[2], y[3]), one);
-              if constexpr (DT == DT_BF16) one = mma<DT>(w.lo, make_uint4(y[0], y[1], y[2], y[3]), one);
+              one = weigh_careful<DT>(operand_weights<DT>(s, st), y, one);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r)

@@ -380,6 +380,38 @@ def test_attend_infinities(ee, dtype):
     assert (y == 0).all() and one.item() == -float("inf")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("rows,lens,most", [
+    (1, [700, 90, 300], None),           # chunks to workgroups
+    (1, [700, 90, 1300], 300_000),       # runs to waves
+    (1, [2100, 700] + [600] * 70, 2112),  # chunks to waves
+    (7, [700, 90, 300], None),
+    (40, [700, 90, 300], None),
+])
+def test_attend_infinite_values(ee, rows, lens, most, hd, dtype):
+    """An infinite value that a row sees is the infinity of its sign in the row's result, values of both
+    signs are NaN; who does not see it, and the other dimensions, keep their bits."""
+    kv = 2
+    s = _attend_case(ee, lens=lens, heads=3 * kv, kv=kv, hd=hd, dtype=dtype, rows=rows, most=most // 64 if most else None, seed=hd)
+    clean = s["y"].reshape(len(lens), rows, kv, 3, hd)
+    want = clean.clone()
+    inf = float("inf")
+    for b, head, dim, at, value in ((0, 0, 5, (lens[0] - 3,), inf), (0, 1, hd - 1, (0,), -inf), (0, 1, 17, (130, 131, 400), inf),
+                                    (1, 0, 0, (2, 70), -inf), (1, 1, 33, tuple(range(64)), inf)):
+        for p in at:
+            s["v_cache"][int(s["tables"][b, p // 64]), p % 64, head, dim] = value
+        for t in range(rows):
+            if lens[b] - rows + t >= at[0]:
+                want[b, t, head, :, dim] = value
+    for p, value in ((10, inf), (250, -inf)):       # of both signs
+        s["v_cache"][int(s["tables"][2, p // 64]), p % 64, 0, 9] = value
+    want[2, :, 0, :, 9] = float("nan")
+    got = ee.paged_attention(s["q"], s["k_cache"], s["v_cache"], s["tables"], s["lens"]).reshape(want.shape)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got.nan_to_num(7.0, inf, -inf), want.nan_to_num(7.0, inf, -inf))
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64), ("bf16", 256)])
 @pytest.mark.parametrize("window", [0, 50])
 def test_attend_a_block_equals_its_rows(ee, dtype, hd, window):
