@@ -295,6 +295,56 @@ def test_linear_products_of_very_different_size(ee):
         _linear_case(ee, rows, 512, 96, "f32", seed=rows, spread=4.0)
 
 
+def _dropped(x, xs, w, ws):
+    """What the 8-bit instruction may drop, [rows, out] in float64: of every eight columns' products those with bits
+    below 2^-13 of the largest one's power of two lose less than that each."""
+    x64, w64 = x.float().double(), w.float().double()
+    rows, k = x.shape
+    out = torch.zeros(rows, w.shape[0], dtype=torch.float64, device=x.device)
+    for c in range(0, k, 8):
+        p = (x64[:, None, c:c + 8] * w64[None, :, c:c + 8]).abs()
+        cut = torch.exp2(torch.floor(torch.log2(p.amax(-1).clamp(min=2.0 ** -18))) - 13)      # (2^-18: the least product)
+        part = (p / cut[..., None]).frac().ne(0).sum(-1)
+        out += part * cut * xs[:, c // 128, None].double() * ws[torch.arange(len(w), device=w.device) // 128, c // 128].double()
+    return out
+
+
+@pytest.mark.parametrize("rows", [1, 33, 200])
+@pytest.mark.parametrize("k", [8 * 16, 272, 1040])
+def test_linear_drops_no_more_than_its_instruction(ee, rows, k):
+    """Random codes, product by product."""
+    for spread in (0.0, 1.0, 3.0):
+        x, xs, w, ws = _operands(_gen(rows + k), rows, k, 70, spread)
+        y = ee.fp8_linear(x, xs, w, ws).double()
+        a, b = _scaled64(x, xs, 1), _scaled64(w, ws, 128)
+        want = torch.mm(a, b.T.contiguous())
+        err = (128 + k // 128 + 4) * U32 * torch.mm(a.abs(), b.abs().T.contiguous()) + _dropped(x, xs, w, ws)
+        assert ((y - want).abs() <= err + UBF * (want.abs() + err)).all()
+
+
+@pytest.mark.parametrize("rows", [1, 33, 200])
+def test_linear_loud_columns(ee, rows):
+    """One product of 2^16 beside seven of 7.5 in every eight columns, which is where bf16's shortened sums lose most (7 2^-13 of the
+    largest); then the loud ones cancel, and what is left is what an output in float32 keeps."""
+    k, n = 256, 40
+    quiet, ones = torch.full((rows, k), 7.5), torch.ones(n, k)
+    scale = torch.ones(rows, 2, device="cuda"), torch.ones(1, 2, device="cuda")
+    for cancel in (False, True):
+        for at in range(8):
+            x, w = quiet.clone(), ones.clone()
+            x[:, at::8], w[:, at::8] = 256.0, 256.0
+            if cancel:
+                w[:, at + 8::16] = -256.0
+            want = torch.mm(x.double(), w.double().T)
+            most = float(torch.mm(x.double().abs(), w.double().abs().T).max())
+            x8, w8 = x.to(E4M3).cuda(), w.to(E4M3).cuda()
+            exact = ee.fp8_linear(x8, scale[0], w8, scale[1], out_dtype=torch.float32).cpu().double()
+            assert ((exact - want).abs() <= (128 + 2 + 4) * U32 * most).all()
+            y = ee.fp8_linear(x8, scale[0], w8, scale[1]).cpu().double()
+            bound = 7 * 2.0 ** -13 * (k // 8) * 65536.0
+            assert ((y - want).abs() <= bound + UBF * (want.abs() + bound)).all(), (at, cancel)
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 def test_linear_nan_stays_in_its_row_and_column(ee, out):
     x, xs, w, ws = _operands(_gen(4), 40, 320, 150)
