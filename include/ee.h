@@ -653,8 +653,8 @@ int32_t ee_kv_append(const ee_kv_append_args* args, void* hip_stream);
  * see does not matter, NaN included.  Of what it sees, NaN gives NaN, and an infinite value its infinity
  * (NaN beside one of the other sign, or where its weight is 0 in fp32).  lens are cut to [0, max_pages * page_size].
  * Scores, weights and sums are fp32; a row's result depends on what it sees alone, so
- * a block of rows equals its rows one by one.  rows 1 is a decoding step; at most 1024,
- * n_seqs * rows * n_heads at most 2^24.
+ * a block of rows equals its rows one by one.  rows 1 is a decoding step; in [1, 1024] (no work is
+ * n_seqs 0), n_seqs * rows * n_heads at most 2^24.
  * workspace: at least ee_paged_attention_workspace_bytes (0 for invalid sizes), 256-byte aligned, in
  * use until the call's work is done; calls that may overlap need one each.  The bytes never
  * fall as n_seqs, rows or max_pages grow. */

@@ -579,7 +579,10 @@ def paged_attention(q, k_cache, v_cache, tables, lens, window: int = 0, scale=No
     cache, page, heads, hd, most, n = _cache(k_cache, v_cache, tables, q.dtype, dev)
     if hd < 1 or qd % hd or (total % n if n else total):
         raise EEError(EE_EINVAL, f"q must be [{n} * rows, heads * {hd}]")
-    rows = total // n if n else 1
+    if total:
+        seqs, rows = n, total // n
+    else:   # no rows of however many sequences: the same checks, and no work
+        seqs, rows, cache = 0, 1, (*cache[:10], 0, *cache[11:])
     odt = _out_type(out_dtype, out, q)
     shape = (total, qd)
     given = out is not None
@@ -589,7 +592,7 @@ def paged_attention(q, k_cache, v_cache, tables, lens, window: int = 0, scale=No
         out, ldo = q.new_empty(shape, dtype=odt), qd
     window, n_heads = int(window), qd // hd
     if workspace is None:
-        workspace = q.new_empty(_attention_workspace(n, rows, n_heads, heads, hd, page, most, window), dtype=torch.uint8)
+        workspace = q.new_empty(_attention_workspace(seqs, rows, n_heads, heads, hd, page, most, window), dtype=torch.uint8)
     elif (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or workspace.get_device() != dev
           or not workspace.is_contiguous()):
         raise EEError(EE_EINVAL, f"workspace must be contiguous uint8 on cuda:{dev}")

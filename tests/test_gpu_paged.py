@@ -348,6 +348,14 @@ def test_attend_negative_lengths_and_empty_batches(ee):
     assert y.shape == (0, 64)
 
 
+def test_attend_no_rows(ee):
+    kc, vc = _cache(_gen(0), 2, 16, 1, 64, torch.bfloat16)
+    for n in (0, 1, 3):
+        tables = torch.zeros(n, 3, dtype=torch.int32, device="cuda")
+        q = torch.zeros(0, 128, dtype=torch.bfloat16, device="cuda")
+        assert ee.paged_attention(q, kc, vc, tables, tables[:, 0].contiguous()).shape == (0, 128)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attend_sharp_and_flat_scores(ee, dtype):
     _attend_case(ee, lens=[1000, 700], heads=4, kv=2, hd=128, dtype=dtype, std=30.0)

@@ -215,6 +215,27 @@ def test_outputs_given_count_as_written(ee, monkeypatch):
     assert out._version == lse._version == 1 and kc._version == 1
 
 
+def test_attention_of_no_rows_is_no_work(ee, monkeypatch):
+    """A batch that has no new rows is checked as any other, and answered with no rows, as the other operators do.
+    (Without a GPU: the C call returns before it would launch anything.)"""
+    import torch
+
+    def operator(op, dev, *args):
+        pack, call = op
+        ee._check(call(pack(*args), None))
+    monkeypatch.setattr(ee, "_operand", lambda t, what: (-1, ee.EE_F32, *t.shape, t.stride(0)))
+    monkeypatch.setattr(ee, "_operator", operator)
+    q, kc, vc = torch.zeros(0, 256), torch.zeros(2, 16, 2, 64), torch.zeros(2, 16, 2, 64)
+    for n in (0, 1, 3):
+        t, lens, out, lse = torch.zeros(n, 4, dtype=torch.int32), torch.zeros(n, dtype=torch.int32), torch.zeros(0, 256), torch.zeros(0, 4)
+        assert ee.paged_attention(q, kc, vc, t, lens).shape == (0, 256)
+        assert ee.paged_attention(q, kc, vc, t, lens, out=out, lse=lse, window=7) is out and out._version == lse._version == 1
+        for kw in (dict(window=-1), dict(lens=lens.long()), dict(scale=float("nan")), dict(out=torch.zeros(0, 255)), dict(k_cache=kc[..., :48], v_cache=vc[..., :48])):
+            with pytest.raises(ee.EEError) as e:
+                ee.paged_attention(**{**dict(q=q, k_cache=kc, v_cache=vc, tables=t, lens=lens), **kw})
+            assert e.value.code == ee.EE_EINVAL, kw
+
+
 def test_tangents_are_refused(ee):
     import torch
     from torch.autograd import forward_ad
