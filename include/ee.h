@@ -609,7 +609,8 @@ int32_t ee_fp8_linear(const ee_fp8_linear_args* args, void* hip_stream);
  * tables[s][p / page_size].  Vector (page, slot, head) of k starts at element page *
  * k_page + slot * k_slot + head * k_head, so pages may be [slot][head] or [head][slot], k and v
  * one allocation or two.  Strides are multiples of 16 bytes; page_size is a multiple of 16.
- * A table's entry outside [0, n_pages) is no page: its positions hold nothing. */
+ * A table's entry outside [0, n_pages) is no page: its positions hold nothing.  k and v may be NULL
+ * where n_pages is 0, tables where max_pages is. */
 typedef struct {
   void* k;                  /* dtype, 16-byte aligned                         */
   void* v;

@@ -213,7 +213,8 @@ static const char* cache_shape(const ee_paged_cache& c, int32_t n_heads, int32_t
   return nullptr;
 }
 static const char* cache_memory(const ee_paged_cache& c, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
-  if (!c.k || !c.v || !c.tables) return "the cache's k, v and tables must be non-NULL";
+  // (a pool of no pages and tables of no columns have no memory: their sequences hold nothing)
+  if ((c.n_pages && (!c.k || !c.v)) || (c.max_pages && !c.tables)) return "the cache's k, v and tables must be non-NULL";
   const int64_t e = esz(dtype), strides[6] = {c.k_page, c.k_slot, c.k_head, c.v_page, c.v_slot, c.v_head};
   for (int64_t s : strides)
     if (s < 0 || s >= int64_t(1) << 40 || s * e % 16) return "the cache's strides must be multiples of 16 bytes, not negative and below 2^40";
@@ -268,7 +269,7 @@ int32_t ee_kv_append(const ee_kv_append_args* p, void* stream) {
   if (!apart(c.k_page, c.n_pages, c.k_slot, c.page_size, c.k_head, q.n_kv_heads, q.head_dim) ||
       !apart(c.v_page, c.n_pages, c.v_slot, c.page_size, c.v_head, q.n_kv_heads, q.head_dim))
     return bad("the cache's vectors must not share memory");
-  if (c.k == c.v) return bad("the cache's k and v must not be the same");
+  if (c.k && c.k == c.v) return bad("the cache's k and v must not be the same");
   for (const void* in : {q.k, q.v, (const void*)q.positions, (const void*)q.seqs, (const void*)q.inv_freq, (const void*)c.tables}) {
     if (in && (c.k == in || c.v == in)) return bad("the cache must not be an input");
     if (in && q.q_out == in) return bad("q_out must not be an input, except q with its stride");
@@ -323,7 +324,7 @@ int32_t ee_paged_attention(const ee_paged_attention_args* p, void* stream) {
   if (q.workspace_bytes < ee::attend_workspace(c.n_seqs, q.rows, q.n_heads, q.head_dim, positions, q.window))
     return op_fail(EE_ECAPACITY, "workspace smaller than ee_paged_attention_workspace_bytes");
   for (const void* in : {q.q, (const void*)c.k, (const void*)c.v, (const void*)c.tables, (const void*)q.lens}) {
-    if (q.out == in || q.lse == in) return bad("out and lse must not be an input");
+    if (in && (q.out == in || q.lse == in)) return bad("out and lse must not be an input");
     if (q.workspace == in) return bad("the workspace must not be an input");
   }
   if (q.out == (const void*)q.lse || q.workspace == q.out || q.workspace == (const void*)q.lse) return bad("out, lse and the workspace must not be each other");

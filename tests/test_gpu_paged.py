@@ -348,6 +348,26 @@ def test_attend_negative_lengths_and_empty_batches(ee):
     assert y.shape == (0, 64)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pages,most", [(0, 0), (0, 5), (3, 0)])
+def test_empty_pools_and_tables(ee, pages, most, dtype):
+    """Sequences that hold nothing, from memory that there is none of: rows are rotated and not stored, and see nothing."""
+    dt = DT[dtype]
+    kc, vc = (torch.ones(pages, 16, 2, 64, dtype=dt, device="cuda") for _ in range(2))
+    tables = torch.zeros(3, most, dtype=torch.int32, device="cuda")
+    pos = torch.tensor([0, 17, 100], dtype=torch.int32, device="cuda")
+    q, k, v = (_rand(_gen(i), 3, n, dtype=dt).cuda() for i, n in enumerate((256, 128, 128)))
+    full = tuple(torch.empty(9, 16, 2, 64, dtype=dt, device="cuda") for _ in range(2))
+    want = ee.kv_append(k, v, *full, torch.arange(24, dtype=torch.int32, device="cuda").reshape(3, 8), pos, q=q, inv_freq=_freq(64))
+    assert torch.equal(ee.kv_append(k, v, kc, vc, tables, pos, q=q, inv_freq=_freq(64)), want)
+    assert (kc == 1).all() and (vc == 1).all()
+    for rows in (1, 3):
+        for window in (0, 9):
+            lens, lse = pos[:3 // rows].contiguous(), torch.empty(3, 4, device="cuda")
+            y = ee.paged_attention(q, kc, vc, tables[:3 // rows], lens, window=window, lse=lse)
+            assert (y == 0).all() and (lse == -float("inf")).all()
+
+
 def test_attend_no_rows(ee):
     kc, vc = _cache(_gen(0), 2, 16, 1, 64, torch.bfloat16)
     for n in (0, 1, 3):
