@@ -657,7 +657,9 @@ int32_t ee_kv_append(const ee_kv_append_args* args, void* hip_stream);
  * a block of rows equals its rows one by one.  rows 1 is a decoding step; in [1, 1024] (no work is
  * n_seqs 0), n_seqs * rows * n_heads at most 2^24.
  * workspace: at least ee_paged_attention_workspace_bytes (0 for invalid sizes), 256-byte aligned, in
- * use until the call's work is done; calls that may overlap need one each.  The bytes never
+ * use until the call's work is done; calls that may overlap need one each.  It holds head_dim + 2 floats
+ * for every row, head and 256 positions of the tables' width (or of the window), but no more than 2 GiB, or what
+ * one row of one sequence takes: a larger call goes through its sequences, or rows, in parts.  The bytes never
  * fall as n_seqs, rows or max_pages grow. */
 typedef struct {
   const void* q;            /* [n_seqs * rows][ldq] dtype, 16-byte aligned rows */

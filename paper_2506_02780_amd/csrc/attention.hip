@@ -393,7 +393,7 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
   const int per = a.Hkv * a.cgroups, share = unit / per, h = unit % per / a.cgroups, ct = unit % a.cgroups;
   if (share >= a.splits * a.B) return;
   const int split = share % a.splits, b = by_length(a.lens, a.B, share / a.splits, lane);
-  const int len = min(max(a.lens[b], 0), pc.max_pages * pc.page), start = a.window ? max(0, len - a.window) : 0;
+  const int len = max(min(max(a.lens[b], 0), pc.max_pages * pc.page) - a.behind, 0), start = a.window ? max(0, len - a.window) : 0;
   const int ch1 = (len + CHUNK - 1) / CHUNK;
   int ch = start / CHUNK + split, run0 = 0, runs = RUNS;
   // Few chunks for the waves that share them (tables much wider than the sequence): a run each, joined
@@ -556,7 +556,7 @@ __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel
   const int share = turn / per * 8 + (int)(blockIdx.x & 7), h = turn % per / a.cgroups, cg = turn % a.cgroups;
   if (share >= a.splits * a.B) return;
   const int split = share % a.splits, b = by_length(a.lens, a.B, share / a.splits, lane);
-  const int cols = a.T * a.G, len = min(max(a.lens[b], 0), pc.max_pages * pc.page);
+  const int cols = a.T * a.G, len = min(max(a.lens[b], 0), pc.max_pages * pc.page) - a.behind;
   const int ct0 = cg * a.ctw, ct1 = min(ct0 + a.ctw, (cols + COLS - 1) / COLS);   // column tiles
   const int before = len - a.T + 1;                                              // the end of row 0
   const int e_lo = before + ct0 * COLS / a.G, e_hi = before + (min(ct1 * COLS, cols) - 1) / a.G;   // of the first and last row
@@ -708,7 +708,7 @@ __device__ __forceinline__ Joined joined(const AttendArgs& a, int64_t item) {
   j.row = item / a.H;
   j.head = (int)(item % a.H);
   const int b = (int)(j.row / a.T), t = (int)(j.row % a.T);
-  const int len = min(max(a.lens[b], 0), a.c.max_pages * a.c.page), end = len - a.T + 1 + t;
+  const int len = min(max(a.lens[b], 0), a.c.max_pages * a.c.page) - a.behind, end = len - a.T + 1 + t;
   j.c0 = (a.window ? max(0, end - a.window) : 0) / CHUNK;
   j.n = end > 0 ? (end + CHUNK - 1) / CHUNK - j.c0 : 0;
   j.step = (int64_t)a.T * a.H;
@@ -791,74 +791,70 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   join_store<HD, ODT>(a, j, d, M, l, o);
 }
 
-// More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us), from
-// 2^20 on in turn, since a launch holds less than 2^32 threads.
+// More: a workgroup per row and head (512 chunks of one row in one of 256 threads: 30 us).
 template <int HD, int ODT>
 __global__ __launch_bounds__(1024) void attend_join_long_kernel(AttendArgs a) {
   constexpr int LPS = HD / 4, SETS = 1024 / LPS < JOIN_GROUPS ? 1024 / LPS : JOIN_GROUPS, PER = JOIN_GROUPS / SETS, AT_ONCE = RUNS;
   __shared__ float sM[16], sL[JOIN_GROUPS];
   __shared__ __attribute__((aligned(16))) float sO[JOIN_GROUPS][HD];
   const int tid = threadIdx.x, set = tid / LPS, d = tid % LPS * 4;
-  for (int64_t item = blockIdx.x; item < (int64_t)a.B * a.T * a.H; item += gridDim.x) {
-    const Joined j = joined(a, item);
-    const bool apart = j.n <= a.apart;
-    const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1;   // states of a chunk
-    auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
-    float M = -INFINITY;
-    for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
+  const Joined j = joined(a, blockIdx.x);
+  const bool apart = j.n <= a.apart;
+  const int n = apart ? j.n * RUNS : j.n, per = apart ? RUNS : 1;   // states of a chunk
+  auto state = [&](int i) { return j.state0 + (apart ? i : (j.c0 + i) % a.ring) * j.step; };
+  float M = -INFINITY;
+  for (int i = tid; i < n; i += 1024) M = fmaxf(M, a.ml[state(i)].x);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
-    if ((tid & 63) == 0) sM[tid >> 6] = M;
-    __syncthreads();
+  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) sM[tid >> 6] = M;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) M = fmaxf(M, sM[i]);
-    const float mu = M == -INFINITY ? 0.f : M;
-    if (set < SETS)
+  for (int i = 0; i < 16; ++i) M = fmaxf(M, sM[i]);
+  const float mu = M == -INFINITY ? 0.f : M;
+  if (set < SETS)
 #pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        const int g = set * PER + p;
-        float l = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        // (apart: AT_ONCE / RUNS chunks of the group, the runs of each side by side)
-        for (int c0 = g; c0 < j.n; c0 += AT_ONCE / per * JOIN_GROUPS) {
-          float2 ml[AT_ONCE];
-          f32x4 x[AT_ONCE];
+    for (int p = 0; p < PER; ++p) {
+      const int g = set * PER + p;
+      float l = 0.f;
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+      // (apart: AT_ONCE / RUNS chunks of the group, the runs of each side by side)
+      for (int c0 = g; c0 < j.n; c0 += AT_ONCE / per * JOIN_GROUPS) {
+        float2 ml[AT_ONCE];
+        f32x4 x[AT_ONCE];
 #pragma unroll
-          for (int i = 0; i < AT_ONCE; ++i) {
-            const int64_t s = state(min(apart ? (c0 + i / RUNS * JOIN_GROUPS) * RUNS + i % RUNS : c0 + i * JOIN_GROUPS, n - 1));
-            ml[i] = a.ml[s];
-            x[i] = *(const f32x4*)(a.o + s * HD + d);
-          }
-          if (apart)
-#pragma unroll
-            for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
-#pragma unroll
-          for (int i = 0; i < AT_ONCE; ++i) {
-            if (c0 + i / per * JOIN_GROUPS >= j.n || (apart && i % RUNS)) continue;
-            const float f = exp2_(ml[i].x - mu);
-            l = fmaf(f, ml[i].y, l);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
-          }
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const int64_t s = state(min(apart ? (c0 + i / RUNS * JOIN_GROUPS) * RUNS + i % RUNS : c0 + i * JOIN_GROUPS, n - 1));
+          ml[i] = a.ml[s];
+          x[i] = *(const f32x4*)(a.o + s * HD + d);
         }
-        *(f32x4*)&sO[g][d] = o;
-        if (d == 0) sL[g] = l;
-      }
-    __syncthreads();
-    if (set == 0) {
-      float l = sL[0];
-      f32x4 o = *(const f32x4*)&sO[0][d];
-      // (groups that hold no chunk were left at +0, which adds nothing: no sum is -0 but one of such)
-#pragma unroll 8
-      for (int i = 1; i < JOIN_GROUPS; ++i) {
-        l += sL[i];
-        const f32x4 y = *(const f32x4*)&sO[i][d];
+        if (apart)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += y[e];
+          for (int i = 0; i < AT_ONCE; i += RUNS) join_runs(ml + i, x + i);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+          if (c0 + i / per * JOIN_GROUPS >= j.n || (apart && i % RUNS)) continue;
+          const float f = exp2_(ml[i].x - mu);
+          l = fmaf(f, ml[i].y, l);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[i][e], o[e]);
+        }
       }
-      join_store<HD, ODT>(a, j, d, M, l, o);
+      *(f32x4*)&sO[g][d] = o;
+      if (d == 0) sL[g] = l;
     }
-    __syncthreads();
+  __syncthreads();
+  if (set == 0) {
+    float l = sL[0];
+    f32x4 o = *(const f32x4*)&sO[0][d];
+    // (groups that hold no chunk were left at +0, which adds nothing: no sum is -0 but one of such)
+#pragma unroll 8
+    for (int i = 1; i < JOIN_GROUPS; ++i) {
+      l += sL[i];
+      const f32x4 y = *(const f32x4*)&sO[i][d];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += y[e];
+    }
+    join_store<HD, ODT>(a, j, d, M, l, o);
   }
 }
 
@@ -868,9 +864,20 @@ int attend_ring(int64_t positions, int T, int window) {
   if (window) n = std::min<int64_t>(n, ((int64_t)window + T + CHUNK - 2) / CHUNK + 1);
   return (int)std::max<int64_t>(n, 1);
 }
+static size_t states_bytes(int64_t states, int hd) { return ((size_t)states * 8 + 255) / 256 * 256 + (size_t)states * hd * 4; }
+static size_t states_bytes(int B, int T, int H, int hd, int64_t positions, int window) {
+  return states_bytes((int64_t)B * attend_ring(positions, T, window) * T * H, hd);
+}
+// States take as much room as the tables are wide, whatever the sequences hold: what takes more than
+// this (or one row of a sequence, where that does) is done in parts, one after another in the same room.
+// (64 sequences of 33 rows, 32 heads of 128, tables for 131072 positions: 18 GB at once.  1024 rows of 8192
+// positions in such tables: 1040 us at once, 766 in parts, whose states the caches hold for the joining.)
+constexpr size_t STATES_BYTES = size_t(2) << 30;
+static size_t most_bytes(int H, int hd, int64_t positions, int window) {
+  return std::max(STATES_BYTES, states_bytes(1, 1, H, hd, positions, window));
+}
 size_t attend_workspace(int B, int T, int H, int hd, int64_t positions, int window) {
-  const size_t states = (size_t)B * attend_ring(positions, T, window) * T * H;
-  return (states * 8 + 255) / 256 * 256 + states * hd * 4;
+  return std::min(states_bytes(B, T, H, hd, positions, window), most_bytes(H, hd, positions, window));
 }
 
 template <int DT, int HD, int ODT>
@@ -901,8 +908,11 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
     // which a CU holds two; then of the column tiles to 512 (one row of 8 sequences of 2048: 21 us,
     // 24.6 from 512; 5 rows of 16 of 4096, two tiles: 73 from 512, 92 from 256; 33 rows, nine:
     // 181, 189 from 512).
-    a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, (ctiles > 1 && ctiles <= 4 ? 512 : 256) / heads));
-    const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT));
+    // A part of a call that fills the chip with the whole call's splits takes those (1024 rows of 16
+    // sequences of 2048, in two parts: 1600 us, 1785 with twice the splits).
+    const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT)), some = ctiles > 1 && ctiles <= 4 ? 512 : 256;
+    const int64_t of_all = std::max<int64_t>(1, some / ((int64_t)a.all * a.Hkv));
+    a.splits = (int)std::min<int64_t>(a.ring, heads * least * of_all >= 512 ? of_all : std::max<int64_t>(1, some / heads));
     a.cgroups = (int)std::min<int64_t>(ctiles, std::max<int64_t>(least, 512 / (heads * a.splits)));
     a.ctw = (ctiles + a.cgroups - 1) / a.cgroups;
     a.cgroups = (ctiles + a.ctw - 1) / a.ctw;
@@ -912,7 +922,7 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
-  if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)std::min<int64_t>(items, 1 << 20)), dim3(1024), 0, st, a);
+  if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)items), dim3(1024), 0, st, a);
   else if (a.ring > 8) hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 16>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 8>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
@@ -924,8 +934,41 @@ static hipError_t attend_hd(const AttendArgs& a, hipStream_t st) {
   return a.odt == DT_F32 ? attend_t<DT_BF16, HD, DT_F32>(a, st) : attend_t<DT_BF16, HD, DT_BF16>(a, st);
 }
 
-hipError_t run_attend(const AttendArgs& a, hipStream_t st) {
+static hipError_t attend(const AttendArgs& a, hipStream_t st) {
   return a.hd == 64 ? attend_hd<64>(a, st) : a.hd == 128 ? attend_hd<128>(a, st) : attend_hd<256>(a, st);
+}
+
+// In parts of equally many sequences, or of rows of one, whose states fit (a row's bits depend on
+// that row alone).
+hipError_t run_attend(const AttendArgs& a, hipStream_t st) {
+  const int64_t positions = (int64_t)a.c.max_pages * a.c.page;
+  const size_t most = most_bytes(a.H, a.hd, positions, a.window);
+  auto parts = [](int n, size_t fit) {   // of n, of at most `fit` each
+    const int64_t k = std::max<int64_t>(1, std::min<int64_t>(n, (int64_t)fit)), count = (n + k - 1) / k;
+    return (int)((n + count - 1) / count);
+  };
+  int seqs = a.B, rows = a.T;
+  if (states_bytes(a.B, a.T, a.H, a.hd, positions, a.window) > most) {
+    seqs = parts(a.B, most / states_bytes(1, a.T, a.H, a.hd, positions, a.window));
+    if (seqs == 1) rows = parts(a.T, most / states_bytes((int64_t)attend_ring(positions, a.T, a.window) * a.H, a.hd));
+  }
+  for (int b = 0; b < a.B; b += seqs)
+    for (int t = 0; t < a.T; t += rows) {
+      AttendArgs p = a;
+      const int64_t row = (int64_t)b * a.T + t;
+      p.B = std::min(seqs, a.B - b);
+      p.T = std::min(rows, a.T - t);
+      p.behind = a.T - t - p.T;
+      p.all = a.B;
+      p.q = (const uint8_t*)a.q + row * a.ldq * esz_of(a.dt);
+      p.out = (uint8_t*)a.out + row * a.ldo * esz_of(a.odt);
+      p.lse = a.lse ? a.lse + row * a.H : nullptr;
+      p.lens = a.lens + b;
+      p.c.tables = a.c.tables + b * a.c.ldt;
+      const hipError_t e = attend(p, st);
+      if (e != hipSuccess) return e;
+    }
+  return hipSuccess;
 }
 
 }  // namespace ee

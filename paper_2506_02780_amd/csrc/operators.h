@@ -112,6 +112,8 @@ struct AttendArgs {
   int B, T, H, Hkv, G, hd, dt, odt, window;
   float scale_log2;     // of scores, times log2 e
   // (filled in by run_attend)
+  int behind;           // rows of the sequences that follow the T here
+  int all;              // sequences of the whole call
   float2* ml;           // [B][ring][Hkv][T G] largest score and sum of the chunks' states
   float* o;             // [..][hd] their weighted values
   int ring, splits;     // chunks held; workgroups that share a sequence's

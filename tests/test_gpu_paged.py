@@ -559,6 +559,35 @@ def test_attend_workspaces(ee):
     assert e.value.code == ee.EE_ECAPACITY
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,rows,heads,page,positions,window", [
+    ([0, 1, 33, 300, 2, 700, 40, 257, 20, 1000, 32, 0, 64, 90, 34, 5, 600, 31, 256, 1500], 33, 8, 64, 1 << 20, 0),   # parts of 7 sequences
+    ([700, 350, 0], 600, 8, 64, 1 << 20, 0),            # parts of 200 rows, those of the second before its first position
+    ([70_000, 1, 2], 2, 64, 65536, 1 << 25, 0),         # of one row: a row's states are more than 2 GiB
+    ([400_000, 50], 600, 8, 1024, 1 << 20, 300_000),    # of one sequence, which a window decides
+])
+def test_attend_in_parts(ee, lens, rows, heads, page, positions, window, dtype):
+    """Calls whose tables are so wide that their states would not fit: bit for bit as alone with tables
+    no wider than the sequence, in a workspace of the size that is asked for and no further."""
+    g, dt, kv = _gen(rows), DT[dtype], 1
+    tables, n_pages = _tables(g, lens, page)
+    kc, vc = _cache(g, n_pages, page, kv, 64, dt)
+    wide = torch.full((len(lens), positions // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :tables.shape[1]] = tables
+    q = _rand(g, len(lens) * rows, heads * 64, dtype=dt).cuda()
+    n = ee.ee_paged_attention_workspace_bytes(len(lens), rows, heads, kv, 64, page, positions // page, window)
+    ws = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+    length, lse = _i32(lens), torch.full((len(lens) * rows, heads), 7.0, device="cuda")
+    y = ee.paged_attention(q, kc, vc, wide, length, window=window, lse=lse, workspace=ws[:n], out=torch.full_like(q, 7.0))
+    assert (ws[n:] == 77).all()
+    for b in range(len(lens)):
+        at = slice(b * rows, (b + 1) * rows)
+        pages = max(1, -(-lens[b] // page))
+        ends = torch.empty(rows, heads, device="cuda")
+        one = ee.paged_attention(q[at], kc, vc, tables[b:b + 1, :pages].contiguous(), length[b:b + 1], window=window, lse=ends)
+        assert torch.equal(y[at], one) and torch.equal(lse[at], ends), b
+
+
 def test_two_streams(ee):
     a = _attend_case(ee, lens=[3000, 40], heads=8, kv=2, hd=128, seed=1)
     b = _attend_case(ee, lens=[1500, 2500], heads=8, kv=2, hd=128, seed=2)

@@ -169,6 +169,20 @@ def test_an_attention_workspace_serves_smaller_calls(ee, window):
             last = n
 
 
+@pytest.mark.parametrize("kw", [
+    dict(n_seqs=64, rows=33, max_pages=8192), dict(n_seqs=1, rows=1024, max_pages=8192), dict(n_seqs=8, rows=1024, max_pages=8192),
+    dict(n_seqs=64, rows=1024, max_pages=512, n_heads=8), dict(n_seqs=4096, rows=1, max_pages=8192), dict(n_seqs=64, rows=33, max_pages=8192, window=100_000),
+])
+def test_attention_workspace_of_wide_tables(ee, kw):
+    """It stays below 2 GiB however many rows and sequences share tables of up to 131072 positions, where all their chunks'
+    states at once took up to 70 GB; below that it is what they take."""
+    at = dict(n_heads=32, n_kv_heads=8, head_dim=128, page_size=16)
+    assert 0 < _workspace(ee, **{**at, **kw}) <= 2 << 30
+    assert _workspace(ee, **{**at, "n_seqs": 64, "rows": 1, "max_pages": 8192}) == 64 * 512 * 32 * 520
+    # (a row of one sequence is not parted)
+    assert _workspace(ee, **{**at, "n_seqs": 3, "rows": 7, "max_pages": 1 << 25}) == (1 << 21) * 32 * 520
+
+
 @pytest.mark.parametrize("op,name", [("_OP_FP8_QUANT", "EEFp8QuantArgs"), ("_OP_FP8_LINEAR", "EEFp8LinearArgs"),
                                      ("_OP_KV_APPEND", "EEKvAppendArgs"), ("_OP_PAGED_ATTENTION", "EEPagedAttentionArgs")])
 def test_packed_arguments_are_the_struct(ee, op, name):
