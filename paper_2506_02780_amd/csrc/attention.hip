@@ -871,7 +871,7 @@ static size_t states_bytes(int B, int T, int H, int hd, int64_t positions, int w
 // States take as much room as the tables are wide, whatever the sequences hold: what takes more than
 // this (or one row of a sequence, where that does) is done in parts, one after another in the same room.
 // (64 sequences of 33 rows, 32 heads of 128, tables for 131072 positions: 18 GB at once.  1024 rows of 8192
-// positions in such tables: 1040 us at once, 766 in parts, whose states the caches hold for the joining.)
+// positions in such tables: 1040 us at once, 766 in parts.)
 constexpr size_t STATES_BYTES = size_t(2) << 30;
 static size_t most_bytes(int H, int hd, int64_t positions, int window) {
   return std::max(STATES_BYTES, states_bytes(1, 1, H, hd, positions, window));

@@ -395,6 +395,23 @@ def test_linear_of_every_tile(ee, rows, n, k):
             assert torch.equal(part, y[lo:hi]), (out, lo)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("n", [2048, 2049, 2052])
+def test_linear_epilogues_of_all_kernels(ee, n, act, out):
+    """Bit for bit, each activation with and without bias and residual: rows alone (blocks of the reduction spread over waves)
+    and among 150 (tiles; their stores 16 and 8 bytes wide and one value at a time)."""
+    g = _gen(n)
+    x, xs, w, ws = _operands(g, 150, 272, n)
+    b, r = _rand(g, n).cuda(), _rand(g, 150, n, dtype=DT[out]).cuda()
+    for bias, residual in itertools.product((None, b), (None, r)):
+        y = ee.fp8_linear(x, xs, w, ws, bias=bias, act=act, residual=residual, out_dtype=DT[out])
+        for lo, hi in ((0, 1), (63, 67), (148, 150)):
+            part = ee.fp8_linear(x[lo:hi], xs[lo:hi], w, ws, bias=bias, act=act, residual=None if residual is None else r[lo:hi],
+                                 out_dtype=DT[out])
+            assert torch.equal(part, y[lo:hi]), (bias is not None, residual is not None, lo)
+
+
 def test_linear_residual_in_place(ee):
     x, xs, w, ws = _operands(_gen(3), 33, 256, 96)
     h = _rand(_gen(1), 33, 96, dtype=torch.bfloat16).cuda()
