@@ -207,38 +207,29 @@ __device__ __forceinline__ int first_block(int K, int n) { return K % BLOCK ? 0 
 
 // ------------------------------------------------------- product, few rows --
 
-// At most 16 MT rows: the weights stream past them once, and what bounds the call is
-// how much of them is on its way.  A workgroup owns 16 NT features; its waves
-// share the blocks of the reduction, ROUND of them at a time: wave w multiplies
-// blocks w, w + W, ... and leaves every D_b in LDS, where threads then add a result's
-// terms in the order of the blocks.  The next round's operands are requested before that.
-constexpr int ROWS_WAVES = 8;
-template <bool EXACT, int MT, int NT, int U>
+// Sixteen rows by sixteen features a workgroup: the weights stream past the rows once, and what bounds
+// the call is how much of them is on its way.  A workgroup's waves share the blocks of the reduction,
+// ROUND of them at a time: wave w multiplies blocks w, w + W, ... and leaves every D_b in LDS, where 256 threads
+// then add a result's terms in the order of the blocks.  The next round's operands are requested before that.
+constexpr int ROWS_WAVES = 8, ROWS_EACH = 4;   // blocks of a wave in a round
+template <bool EXACT>
 __global__ __launch_bounds__(ROWS_WAVES * 64, 2) void fp8_rows_kernel(Fp8LinearArgs a) {
-  constexpr int W = ROWS_WAVES, ROUND = W * U, VALUES = MT * NT * 256, PER = (VALUES + W * 64 - 1) / (W * 64);
+  constexpr int W = ROWS_WAVES, U = ROWS_EACH, ROUND = W * U;
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, grp = lane >> 4;
-  __shared__ uint4 sd[2][ROUND][MT * NT][64];   // D_b; lane quads of group grp at place lane ^ 4 grp, so that 16 features of 4 rows are on all banks
-  __shared__ float ss[2][ROUND][MT * NT][16];   // xs_b ws_b of the rows
-  const int f0 = blockIdx.x * (16 * NT), K = a.l.K, kb = (K + BLOCK - 1) / BLOCK;
-  const int t0 = blockIdx.y * (16 * MT);
+  __shared__ uint4 sd[2][ROUND][64];   // D_b; lane quads of group grp at place lane ^ 4 grp, so that 16 features of 4 rows are on all banks
+  __shared__ float ss[2][ROUND][16];   // xs_b ws_b of the rows
+  const int f0 = blockIdx.x * 16, K = a.l.K, kb = (K + BLOCK - 1) / BLOCK;
+  const int t0 = blockIdx.y * 16;
   const int start = first_block(K, a.n0 + f0);
   const auto wr = make_rsrc((const uint8_t*)a.l.w + f0 * a.l.ldw, 0x7fffffffu);
   const auto xr = make_rsrc((const uint8_t*)a.l.x + t0 * a.l.ldx, 0x7fffffffu);
-  unsigned wo[NT], xo[MT];
-  const float *xs[MT], *ws[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    wo[n] = (unsigned)min(n * 16 + c, a.l.N - 1 - f0) * (unsigned)a.l.ldw + grp * 16;
-    ws[n] = a.ws + (int64_t)(min(f0 + n * 16, a.l.N - 1) / BLOCK) * kb;
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int t = min(m * 16 + c, a.l.T - 1 - t0);
-    xo[m] = (unsigned)t * (unsigned)a.l.ldx + grp * 16;
-    xs[m] = a.xs + (int64_t)(t0 + t) * kb;
-  }
-  Codes wf[U][NT], xf[U][MT];
-  float xv[U][MT], wsv[U][NT];
+  const unsigned wo = (unsigned)min(c, a.l.N - 1 - f0) * (unsigned)a.l.ldw + grp * 16;
+  const float* ws = a.ws + (int64_t)(min(f0, a.l.N - 1) / BLOCK) * kb;
+  const int tc = min(c, a.l.T - 1 - t0);
+  const unsigned xo = (unsigned)tc * (unsigned)a.l.ldx + grp * 16;
+  const float* xs = a.xs + (int64_t)(t0 + tc) * kb;
+  Codes wf[U], xf[U];
+  float xv[U], wsv[U];
   auto load = [&](int b0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -250,67 +241,49 @@ __global__ __launch_bounds__(ROWS_WAVES * 64, 2) void fp8_rows_kernel(Fp8LinearA
       for (int h = 0; h < 2; ++h) {
         const unsigned k = b * BLOCK + h * 64;
         const bool in = some && k + grp * 16 < (unsigned)K;   // (past the reduction: zeros)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) wf[u][n].u[h] = bload<0>(wr, in ? wo[n] + k : OOB);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) xf[u][m].u[h] = bload<0>(xr, in ? xo[m] + k : OOB);
+        wf[u].u[h] = bload<0>(wr, in ? wo + k : OOB);
+        xf[u].u[h] = bload<0>(xr, in ? xo + k : OOB);
       }
       const int bc = some ? b : 0;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) xv[u][m] = xs[m][bc];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) wsv[u][n] = ws[n][bc];
+      xv[u] = xs[bc];
+      wsv[u] = ws[bc];
     }
   };
-  float acc[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) acc[i] = 0.f;
+  const int f = threadIdx.x & 15, t = threadIdx.x >> 4;   // a thread's result, of those that have one
+  float acc = 0.f;
   load(0);
   int buf = 0;
   for (int b0 = 0; b0 < kb; b0 += ROUND) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const f32x4 d = block_product<EXACT>(wf[u][n], xf[u][m]);
-          sd[buf][u * W + wv][m * NT + n][lane ^ (4 * grp)] = __builtin_bit_cast(uint4, d);
-          if (grp == 0) ss[buf][u * W + wv][m * NT + n][c] = xv[u][m] * wsv[u][n];
-        }
+    for (int u = 0; u < U; ++u) {
+      sd[buf][u * W + wv][lane ^ (4 * grp)] = __builtin_bit_cast(uint4, block_product<EXACT>(wf[u], xf[u]));
+      if (grp == 0) ss[buf][u * W + wv][c] = xv[u] * wsv[u];
+    }
     if (b0 + ROUND < kb) load(b0 + ROUND);
     __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     barrier_only();
     const int terms = min(ROUND, kb - b0);
+    if (t < 16) {
+      const float* d = (const float*)&sd[buf][0][((f >> 2) * 16 + t) ^ (f & 12)] + (f & 3);
+      const float* s = &ss[buf][0][t];
+      if (terms == ROUND) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = threadIdx.x + i * (W * 64), tile = e / 256, f = e & 15, t = (e >> 4) & 15;
-      if (VALUES % (W * 64) == 0 || e < VALUES) {
-        const float* d = (const float*)&sd[buf][0][tile][((f >> 2) * 16 + t) ^ (f & 12)] + (f & 3);
-        const float* s = &ss[buf][0][tile][t];
-        if (terms == ROUND) {
-#pragma unroll
-          for (int j = 0; j < ROUND; ++j) acc[i] = fmaf(d[j * MT * NT * 256], s[j * MT * NT * 16], acc[i]);
-        } else {
-          for (int j = 0; j < terms; ++j) acc[i] = fmaf(d[j * MT * NT * 256], s[j * MT * NT * 16], acc[i]);
-        }
+        for (int j = 0; j < ROUND; ++j) acc = fmaf(d[j * 256], s[j * 16], acc);
+      } else {
+        for (int j = 0; j < terms; ++j) acc = fmaf(d[j * 256], s[j * 16], acc);
       }
     }
     buf ^= 1;
   }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = threadIdx.x + i * (W * 64), tile = e / 256;
-    const int n = f0 + tile % NT * 16 + (e & 15), t = t0 + tile / NT * 16 + ((e >> 4) & 15);
-    if (e >= VALUES || n >= a.l.N || t >= a.l.T) continue;
-    float v = activate(a.l.bias ? acc[i] + a.l.bias[n] : acc[i] + 0.f, a.l.act);
-    if (a.l.odt == DT_BF16) {
-      v += a.l.res ? load_elt<DT_BF16>(a.l.res, (size_t)t * a.l.ldr + n) : 0.f;
-      store_elt<DT_BF16>(a.l.y, (size_t)t * a.l.ldy + n, v);
-    } else {
-      v += a.l.res ? load_elt<DT_F32>(a.l.res, (size_t)t * a.l.ldr + n) : 0.f;
-      store_elt<DT_F32>(a.l.y, (size_t)t * a.l.ldy + n, v);
-    }
+  const int n = f0 + f, row = t0 + t;
+  if (t >= 16 || n >= a.l.N || row >= a.l.T) return;
+  float v = activate(a.l.bias ? acc + a.l.bias[n] : acc + 0.f, a.l.act);
+  if (a.l.odt == DT_BF16) {
+    v += a.l.res ? load_elt<DT_BF16>(a.l.res, (size_t)row * a.l.ldr + n) : 0.f;
+    store_elt<DT_BF16>(a.l.y, (size_t)row * a.l.ldy + n, v);
+  } else {
+    v += a.l.res ? load_elt<DT_F32>(a.l.res, (size_t)row * a.l.ldr + n) : 0.f;
+    store_elt<DT_F32>(a.l.y, (size_t)row * a.l.ldy + n, v);
   }
 }
 
@@ -584,10 +557,9 @@ __global__ __launch_bounds__(WR * WF * 64, WR * WF >= 4 ? 2 : 1) void fp8_tile_k
   }
 }
 
-template <bool EXACT, int MT, int NT, int U>
+template <bool EXACT>
 static hipError_t rows_t(const Fp8LinearArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((fp8_rows_kernel<EXACT, MT, NT, U>), dim3((unsigned)((a.l.N + 16 * NT - 1) / (16 * NT)), (unsigned)((a.l.T + 16 * MT - 1) / (16 * MT))),
-                     dim3(ROWS_WAVES * 64), 0, st, a);
+  hipLaunchKernelGGL((fp8_rows_kernel<EXACT>), dim3((unsigned)((a.l.N + 15) / 16), (unsigned)((a.l.T + 15) / 16)), dim3(ROWS_WAVES * 64), 0, st, a);
   return hipGetLastError();
 }
 template <bool EXACT, int BM, int BN, int WR, int WF, int NST>
@@ -640,7 +612,7 @@ template <bool EXACT> static hipError_t fp8_linear_t(Fp8LinearArgs a, hipStream_
   // Few rows, or few features: the blocks of the reduction spread over waves (16 rows, 4096 ->
   // 4096 7.5 us, 9.8 on tiles of 16 x 64; 24 rows, 11008 -> 4096 23.4, 28.8; 16 rows, 4096 -> 22016
   // 30.3, 22.7).
-  if (a.l.T <= 4 || (int64_t)((a.l.N + 15) / 16) * ((a.l.T + 15) / 16) <= 512) return rows_t<EXACT, 1, 1, 4>(a, st);
+  if (a.l.T <= 4 || (int64_t)((a.l.N + 15) / 16) * ((a.l.T + 15) / 16) <= 512) return rows_t<EXACT>(a, st);
   const Fp8Tile *best = nullptr, *rest = nullptr;
   const double all = fp8_best<EXACT>(a.l.T, a.l.N, &best);
   // Whole turns of the largest tile, and the features that are left on the tile that
