@@ -532,13 +532,16 @@ __global__ __launch_bounds__((stream_waves<DT, HD>() * 64), (stream_waves<DT, HD
 }
 
 // Several rows per sequence, or one where there are few chunks (8 KV heads of 128, one row of a
-// sequence of 8192: 18 us so, 33 by the waves above; of 32768 39 and 44; of 65536 68 and
-// 63).  The four waves of a workgroup take the runs of a chunk, whose states they
+// sequence of 8192: 18 us so, 32 by the waves above; of 32768 37 and 39; of 65536 65 and
+// 58).  The four waves of a workgroup take the runs of a chunk, whose states they
 // join through LDS, and keep its keys and values in registers for all of the workgroup's
-// column tiles: read anew for each, 33 rows of 4 sequences to 4096 took 88 us, so 59.
+// column tiles (read anew for each, 33 rows of 4 sequences to 4096 took 88 us; so 59 as first built, 37 now).
+// Some of them stand in scratch: 18 registers of a bf16 cache with head_dim 128 and several
+// tiles, 6 with 256; the keys and values of an fp32 run of 256 do not fit a wave (394 registers, 132
+// in the kernel above).
 constexpr int att_tiles(int row_bytes) { return std::max(1, 32768 / (COLS * row_bytes)); }   // whose queries LDS holds
 // For one column tile the next run's are requested ahead; for several, two workgroups share a
-// CU instead, each working while the other waits (33 rows 45 us; one row of 8192 20).
+// CU instead, each working while the other waits (33 rows 38.7 us, 52 with one).
 template <int DT, int HD, bool SEVERAL>
 __global__ __launch_bounds__(RUNS * 64, SEVERAL ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   using G = AttGeo<DT, HD>;
@@ -749,10 +752,10 @@ __device__ __forceinline__ void join_runs(float2* ml, f32x4* x) {
 }
 
 // At most JOIN_GROUPS chunks are held: every sum is one chunk's state.  AT_ONCE are requested together
-// (64 sequences to 8192: 8.6 us with 16, 11.5 with 8; one of 2048, eight chunks: 4.4 and 3.9).
-template <int HD, int ODT, int AT_ONCE>
+// (64 sequences to 8192: 9.2 us, 8.5 with 16; 33 rows of 4 to 4096: 6.9 and 7.7; one of 2048: 3.8 and 4.3).
+template <int HD, int ODT>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  constexpr int LPS = HD / 4;
+  constexpr int LPS = HD / 4, AT_ONCE = 8;
   const int64_t item = (int64_t)blockIdx.x * (256 / LPS) + threadIdx.x / LPS;
   if (item >= (int64_t)a.B * a.T * a.H) return;
   const int at = threadIdx.x % LPS, d = at * 4;
@@ -896,7 +899,7 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   a.apart = 0;
   if (a.T == 1 && heads * ctiles * a.ring > 1024) {
     // Some 4096 waves, twice what the chip holds at once (64 sequences to 8192: 228 us; 2048
-    // waves 273, 6144 233).
+    // waves 273, 6144 231).
     a.cgroups = ctiles;
     a.splits = (int)std::min<int64_t>(a.ring, std::max<int64_t>(1, 4096 / (heads * ctiles)));
     a.apart = a.splits / RUNS;
@@ -906,8 +909,8 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   } else {
     // Splits of the length first, some 256 workgroups, or 512 of two to four column tiles, of
     // which a CU holds two; then of the column tiles to 512 (one row of 8 sequences of 2048: 21 us,
-    // 24.6 from 512; 5 rows of 16 of 4096, two tiles: 73 from 512, 92 from 256; 33 rows, nine:
-    // 181, 189 from 512).
+    // 24.3 from 512; 5 rows of 16 of 4096, two tiles: 78 from 512, 94 from 256; 33 rows, nine:
+    // 158, 160 from 512).
     // A part of a call that fills the chip with the whole call's splits takes those (1024 rows of 16
     // sequences of 2048, in two parts: 1600 us, 1785 with twice the splits).
     const int64_t least = (ctiles + att_tiles(HD * esz_of(DT)) - 1) / att_tiles(HD * esz_of(DT)), some = ctiles > 1 && ctiles <= 4 ? 512 : 256;
@@ -923,8 +926,7 @@ static hipError_t attend_t(AttendArgs a, hipStream_t st) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   const int64_t items = (int64_t)a.B * a.T * a.H, per = 256 / (HD / 4);
   if (a.ring > JOIN_GROUPS) hipLaunchKernelGGL((attend_join_long_kernel<HD, ODT>), dim3((unsigned)items), dim3(1024), 0, st, a);
-  else if (a.ring > 8) hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 16>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((attend_join_kernel<HD, ODT, 8>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((attend_join_kernel<HD, ODT>), dim3((unsigned)((items + per - 1) / per)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
