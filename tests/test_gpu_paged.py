@@ -440,6 +440,23 @@ def test_attend_infinite_values(ee, rows, lens, most, hd, dtype):
     assert torch.equal(got.nan_to_num(7.0, inf, -inf), want.nan_to_num(7.0, inf, -inf))
 
 
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("window", [0, 3000])
+def test_attend_an_infinite_value_of_each_chunk(ee, hd, window):
+    """One head has it in its first chunk, the next one in its second and so on, where waves take ten chunks in turn."""
+    kv, length = 32, 5000
+    s = _attend_case(ee, lens=[length] + [3] * 63, heads=kv, kv=kv, hd=hd, window=window, most=80, seed=hd)
+    want, inf = s["y"].reshape(64, kv, hd).clone(), float("inf")
+    for h in range(kv):
+        for p in (h % 20 * 256 + 17, h % 20 * 256 + 130):
+            if p < length:
+                s["v_cache"][int(s["tables"][0, p // 64]), p % 64, h, 5] = inf
+                if not window or p >= length - window:
+                    want[0, h, 5] = inf
+    got = ee.paged_attention(s["q"], s["k_cache"], s["v_cache"], s["tables"], s["lens"], window=window).reshape(want.shape)
+    assert torch.isinf(want).any() and torch.equal(got, want)
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64), ("bf16", 256)])
 @pytest.mark.parametrize("window", [0, 50])
 def test_attend_a_block_equals_its_rows(ee, dtype, hd, window):
